@@ -85,6 +85,11 @@ def _load() -> ctypes.CDLL:
     L.sparq_conv_gemm_sparse24.restype = ctypes.c_int
     L.sparq_set_tuning.argtypes = [ctypes.c_char_p]
     L.sparq_set_tuning.restype = ctypes.c_int
+    for name, args in (("code_bytes", [i32, i32]), ("scale_bytes", [i32]), ("gemm_workspace_bytes", [i64, i32, i32]),
+                       ("linear_workspace_bytes", [i64, i32, i32]), ("linear_dx_workspace_bytes", [i64, i32, i32]),
+                       ("linear_dw_workspace_bytes", [i64, i32, i32]), ("norm_grad_workspace_bytes", [i64, i32])):
+        f = getattr(L, "sparq_mx_" + name)
+        f.argtypes, f.restype = args, sz
     L.sparq_strerror.argtypes = [ctypes.c_int]
     L.sparq_strerror.restype = ctypes.c_char_p
     return L
@@ -101,6 +106,8 @@ def _load_native():
         raise ImportError(f"_sparq_native.so not built; run `python -c 'import __graft_entry__ as g; g.build()'` ({e})") from e
     names = ("trim", "conv_gemm", "conv_gemm_u8", "conv_gemm_packed", "conv_gemm_sparse24", "dequant", "requant", "pack_act", "unpack_act")
     n.bind(tuple(ctypes.cast(getattr(lib, "sparq_" + k), ctypes.c_void_p).value for k in names), SparqMode, SparqConvDesc, SparqError)
+    names = ("quantize", "dequantize", "gemm", "linear", "linear_dx", "linear_dw", "act", "act_grad", "norm", "norm_grad", "code_bytes", "scale_bytes")
+    n.bind_mx(tuple(ctypes.cast(getattr(lib, "sparq_mx_" + k), ctypes.c_void_p).value for k in names))
     return n
 
 
@@ -114,6 +121,16 @@ sparq_dequant = _native.sparq_dequant
 sparq_requant = _native.sparq_requant
 sparq_pack_act = _native.sparq_pack_act
 sparq_unpack_act = _native.sparq_unpack_act
+sparq_mx_quantize = _native.sparq_mx_quantize
+sparq_mx_dequantize = _native.sparq_mx_dequantize
+sparq_mx_gemm = _native.sparq_mx_gemm
+sparq_mx_linear = _native.sparq_mx_linear
+sparq_mx_linear_dx = _native.sparq_mx_linear_dx
+sparq_mx_linear_dw = _native.sparq_mx_linear_dw
+sparq_mx_act = _native.sparq_mx_act
+sparq_mx_act_grad = _native.sparq_mx_act_grad
+sparq_mx_norm = _native.sparq_mx_norm
+sparq_mx_norm_grad = _native.sparq_mx_norm_grad
 
 
 def strerror(status: int) -> str:
@@ -236,3 +253,33 @@ def sparq_pack_weights_sparse24(w_vals: torch.Tensor, w_idx: torch.Tensor, d: Sp
 def sparq_set_tuning(spec: Optional[str] = None) -> None:
     """Test / tuning hook: force the kernel choice ("path=patch,patch_tn=128,patch_ws=1", "form=rows", ...); None clears it."""
     _check(lib.sparq_set_tuning(spec.encode() if spec else None), "sparq_set_tuning")
+
+
+def sparq_mx_code_bytes(K: int, bits: int) -> int:
+    """Bytes of one row of 4- or 8-bit codes (0: no such row)."""
+    return int(lib.sparq_mx_code_bytes(int(K), int(bits)))
+
+
+def sparq_mx_scale_bytes(K: int) -> int:
+    """Bytes of one row of scales."""
+    return int(lib.sparq_mx_scale_bytes(int(K)))
+
+
+def sparq_mx_gemm_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.sparq_mx_gemm_workspace_bytes(int(M), int(N), int(K)))
+
+
+def sparq_mx_linear_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.sparq_mx_linear_workspace_bytes(int(M), int(N), int(K)))
+
+
+def sparq_mx_linear_dx_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.sparq_mx_linear_dx_workspace_bytes(int(M), int(N), int(K)))
+
+
+def sparq_mx_linear_dw_workspace_bytes(M: int, N: int, K: int) -> int:
+    return int(lib.sparq_mx_linear_dw_workspace_bytes(int(M), int(N), int(K)))
+
+
+def sparq_mx_norm_grad_workspace_bytes(rows: int, K: int) -> int:
+    return int(lib.sparq_mx_norm_grad_workspace_bytes(int(rows), int(K)))

@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparq.so")
 PROBE_SRC = os.path.join(CSRC, "probe", "sparq_probe.hip")
 PROBE_LIB = os.path.join(HERE, "libsparq_probe.so")   # machine-ceiling micro-benchmarks (include/sparq_probe.h)
-NATIVE_SRC = os.path.join(CSRC, "binding", "sparq_native.cpp")
+NATIVE_SRCS = [os.path.join(CSRC, "binding", f) for f in ("sparq_native.cpp", "sparq_native_mx.cpp")]
 NATIVE_LIB = os.path.join(HERE, "_sparq_native.so")   # argument marshalling of the hot entry points (binding.py)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
@@ -33,11 +33,11 @@ def build_native() -> str:
     cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", "-isystem", os.path.join(T, "include"),
            "-isystem", os.path.join(T, "include", "torch", "csrc", "api", "include"), "-isystem", os.path.join(rocm, "include"),
-           "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"], NATIVE_SRC, "-o", NATIVE_LIB,
+           "-isystem", "/opt/rocm/include", "-isystem", sysconfig.get_paths()["include"], *NATIVE_SRCS, "-o", NATIVE_LIB,
            "-L" + os.path.join(T, "lib"), "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_python"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
-        raise RuntimeError(f"g++ failed on {NATIVE_SRC}:\n{r.stdout}\n{r.stderr}")
+        raise RuntimeError(f"g++ failed on {NATIVE_SRCS}:\n{r.stdout}\n{r.stderr}")
     return NATIVE_LIB
 
 

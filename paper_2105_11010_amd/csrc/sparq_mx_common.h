@@ -1,0 +1,205 @@
+// What the kernels of the microscaled formats share: element types, rows of codes and scales, both quantisers in
+// registers, and the argument checks of their entry points.
+#pragma once
+#include "../../include/sparq_mx.h"
+#include "sparq_common.h"
+#include "sparq_fastdiv.h"
+
+namespace sparq {
+namespace mx {
+
+constexpr int kBlock = 32;           // values that share a scale
+constexpr int kCodeUnit = 128;       // values: rows of codes are whole units (one step of the 16-row matrix instruction, two of the 32-row one)
+constexpr int kScaleUnit = 512;      // ... and rows of scales (16 bytes)
+constexpr int kMaxK = 1 << 28;
+
+inline int64_t code_pitch(int K, int bits) { return round_up(K, kCodeUnit) * bits / 8; }
+inline int64_t scale_pitch(int K) { return round_up(K, kScaleUnit) / kBlock; }
+
+typedef int v4i __attribute__((ext_vector_type(4)));
+typedef int v8i __attribute__((ext_vector_type(8)));
+typedef unsigned int v2u __attribute__((ext_vector_type(2)));
+typedef unsigned int v4u __attribute__((ext_vector_type(4)));
+typedef float v2f __attribute__((ext_vector_type(2)));
+typedef float v4f __attribute__((ext_vector_type(4)));
+typedef float v16f __attribute__((ext_vector_type(16)));
+typedef __bf16 v2bf __attribute__((ext_vector_type(2)));
+typedef __bf16 v8bf __attribute__((ext_vector_type(8)));
+typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+
+inline size_t type_bytes(int type) { return type == SPARQ_MX_F32 ? 4 : 2; }
+inline bool type_valid(int type) { return type == SPARQ_MX_F32 || type == SPARQ_MX_F16 || type == SPARQ_MX_BF16; }
+// A tensor argument: present, of whole elements, rows at least as far apart as they are long.
+inline bool tensor_ok(const void* p, int type, int64_t ld, int64_t length) {
+    return p && type_valid(type) && aligned(p, type_bytes(type)) && ld >= length && ld <= (INT64_MAX >> 4);
+}
+inline bool coded_ok(const void* codes, const void* scales) { return codes && scales && aligned(codes, 16) && aligned(scales, 16); }
+inline bool coded_ok_or_none(const void* codes, const void* scales) { return codes || scales ? coded_ok(codes, scales) : true; }
+inline bool sizes_ok(int64_t rows, int64_t K) { return rows >= 0 && K >= 1 && K <= kMaxK; }
+// rows * pitch bytes and rows * ld elements stay inside 64 bits
+inline bool extent_ok(int64_t rows, int64_t ld) { return rows == 0 || ld <= (INT64_MAX / 8) / rows; }
+
+template <class F>
+inline void with_type(int type, F&& f) {
+    if (type == SPARQ_MX_F32) f(float{});
+    else if (type == SPARQ_MX_F16) f(_Float16{});
+    else f(__bf16{});
+}
+
+#if defined(__HIPCC__)
+// ---- eight neighbouring elements, from any address of an element -----------------
+typedef v4u v4u_at4 __attribute__((aligned(4)));
+typedef v4u v4u_at2 __attribute__((aligned(2)));
+
+__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
+    const v4u a = *reinterpret_cast<const v4u_at4*>(p), b = *reinterpret_cast<const v4u_at4*>(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[i] = __uint_as_float(a[i]);
+        v[4 + i] = __uint_as_float(b[i]);
+    }
+}
+__device__ __forceinline__ void load8(const __bf16* p, float (&v)[8]) {
+    const v4u a = *reinterpret_cast<const v4u_at2*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        v[2 * i] = __uint_as_float(a[i] << 16);
+        v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
+    }
+}
+__device__ __forceinline__ void load8(const _Float16* p, float (&v)[8]) {
+    const v4u a = *reinterpret_cast<const v4u_at2*>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t w = a[i];                     // (a copy: the bits of a vector's element cannot be taken in place)
+        const v2h h = __builtin_bit_cast(v2h, w);
+        v[2 * i] = (float)h[0];
+        v[2 * i + 1] = (float)h[1];
+    }
+}
+// ... of which the first n are there
+template <class T>
+__device__ __forceinline__ void load_upto8(const T* p, int n, float (&v)[8]) {
+    if (n >= 8) load8(p, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+    }
+}
+
+// Rounded to nearest even by the conversion instructions.
+__device__ __forceinline__ uint32_t pack2(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b}); }
+__device__ __forceinline__ uint32_t pack2(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, v2h{(_Float16)a, (_Float16)b}); }
+template <class T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+    v4u a;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a[i] = pack2(v[2 * i], v[2 * i + 1], T{});
+    *reinterpret_cast<v4u_at2*>(p) = a;
+}
+__device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
+    v4u a, b;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        a[i] = __float_as_uint(v[i]);
+        b[i] = __float_as_uint(v[4 + i]);
+    }
+    *reinterpret_cast<v4u_at4*>(p) = a;
+    *reinterpret_cast<v4u_at4*>(p + 4) = b;
+}
+template <class T>
+__device__ __forceinline__ void store_upto8(T* p, int n, const float (&v)[8]) {
+    if (n >= 8) store8(p, v);
+    else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+            if (i < n) p[i] = (T)v[i];
+    }
+}
+
+// ---- the formats: a lane holds eight values, four neighbouring lanes a block -------
+// Largest magnitude of the block as the bits of a float: integer order is the order of magnitudes, and NaN and
+// infinity lie above every number.
+__device__ __forceinline__ uint32_t block_top(const float (&v)[8]) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const uint32_t m = __float_as_uint(v[i]) & 0x7FFFFFFFu;
+        top = m > top ? m : top;
+    }
+    const uint32_t b = (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0xB1, 0xF, 0xF, true);       // lane ^ 1
+    top = b > top ? b : top;
+    const uint32_t c = (uint32_t)__builtin_amdgcn_mov_dpp((int)top, 0x4E, 0xF, 0xF, true);       // lane ^ 2
+    return c > top ? c : top;
+}
+// The scale's byte.  The exponent field of the largest magnitude is floor(log2) + 127; 0 stands for zero and for
+// everything below 2^-126, whose clamped exponent is -127 in both forms.
+__device__ __forceinline__ uint32_t scale4_of(uint32_t top) {
+    const uint32_t e = top >> 23;
+    return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
+}
+__device__ __forceinline__ uint32_t scale8_of(uint32_t top) { return top >> 23; }
+// 2^s as a float: byte 0 is 2^-127 (a subnormal), 255 is NaN
+__device__ __forceinline__ float scale_value(uint32_t byte) {
+    const uint32_t bits = byte ? byte << 23 : 0x00400000u;
+    return __uint_as_float(byte == 255 ? 0x7FC00000u : bits);
+}
+// Eight 4-bit codes: the conversion instruction divides by the scale, rounds to nearest even and saturates at 6.
+__device__ __forceinline__ uint32_t codes4_of(const float (&v)[8], uint32_t byte) {
+    const float s = scale_value(byte);
+    uint32_t w = 0;
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
+    w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
+    return byte == 255 ? 0u : w;
+}
+// Eight 8-bit codes
+__device__ __forceinline__ v2u codes8_of(const float (&v)[8], uint32_t byte) {
+    const int up = 133 - (int)byte;                  // 64 / 2^s
+    uint32_t q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const float r = __builtin_rintf(__builtin_amdgcn_ldexpf(v[i], up));
+        q[i] = (uint32_t)(int)__builtin_amdgcn_fmed3f(r, -127.0f, 127.0f);
+    }
+    v2u w;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t lo = __builtin_amdgcn_perm(q[4 * h + 1], q[4 * h], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(q[4 * h + 3], q[4 * h + 2], 0x04000C0Cu);
+        w[h] = byte == 255 ? 0u : lo | hi;
+    }
+    return w;
+}
+// The values of eight codes
+__device__ __forceinline__ void values4_of(uint32_t w, uint32_t byte, float (&v)[8]) {
+    const float s = scale_value(byte);
+    const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
+    const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
+    v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
+    if (byte == 255) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = s;
+    }
+}
+__device__ __forceinline__ void values8_of(v2u w, uint32_t byte, float (&v)[8]) {
+    const int e = (int)byte - 133;                   // 2^s / 64
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int q = (int)(w[i >> 2] << (24 - 8 * (i & 3))) >> 24;
+        v[i] = __builtin_amdgcn_ldexpf((float)q, e);
+    }
+    if (byte == 255) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
+    }
+}
+#endif
+
+// Implemented in sparq_mx_codec.hip: the arguments are checked already.
+sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows, int K, void* codes4, void* scales4, void* codes8,
+                             void* scales8, hipStream_t stream);
+
+}  // namespace mx
+}  // namespace sparq
