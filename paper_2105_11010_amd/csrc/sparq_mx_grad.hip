@@ -1,100 +1,125 @@
-// The product's backward pass: dx over the 4-bit weights, dw over the 8-bit checkpoint (include/sparq_mx.h).
-#include "sparq_mx_common.h"
+// The product's backward pass: entry points, the choice of tiles, and the sums that join a divided reduction.
+#include "sparq_mx_grad.h"
 
 namespace sparq {
 namespace mx {
 
 constexpr int kThreads = 256;
 
-struct GradParams {
-    const void* dy;
-    const uint8_t *codes, *scales;
-    int64_t lddy, code_pitch, scale_pitch, ldo;
-    int64_t J, R;                        // results [J][K], sums of R products
-    int32_t K;
-};
-
-// The bf16 parts of a value: their sum is the value (8 significand bits a part; 11 of fp16, 24 of fp32).
-template <class T> constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
-template <> constexpr int kParts<__bf16> = 1;
-template <int P>
-__device__ __forceinline__ void split(float v, __bf16 (&part)[P]) {
-    part[0] = (__bf16)v;
+// out = the parts' sum, part after part; four values a thread.
+template <class O>
+__global__ __launch_bounds__(kThreads) void grad_join_kernel(const float* __restrict__ partial, O* __restrict__ out, int64_t J, int K, int64_t ldo, int parts) {
+    const int k = (blockIdx.x * kThreads + threadIdx.x) * 4;
+    if (k >= K) return;
+    const int n = K - k < 4 ? K - k : 4;
+    for (int64_t j = blockIdx.y; j < J; j += gridDim.y) {
+        float s[4] = {};
+        for (int i = 0; i < parts; ++i) {
+            const float* at = partial + (i * J + j) * K + k;
 #pragma unroll
-    for (int i = 1; i < P; ++i) {
-        v -= (float)part[i - 1];
-        part[i] = (__bf16)v;
-    }
-    if (P > 1 && !(__builtin_fabsf((float)part[0]) < __builtin_inff())) {    // NaN, infinity: nothing to add
+            for (int e = 0; e < 4; ++e)
+                if (e < n) s[e] += at[e];
+        }
+        O* to = out + j * ldo + k;
 #pragma unroll
-        for (int i = 1; i < P; ++i) part[i] = (__bf16)0.0f;
+        for (int e = 0; e < 4; ++e)
+            if (e < n) to[e] = (O)s[e];
     }
 }
 
-// out[j][k] = sum_r dy(j, r) * V[r][k].  DW: j = n, r = m, V = the 8-bit checkpoint; else j = m, r = n, V = the 4-bit weights.
-// A wavefront makes 32 x 32 results; decoded values are bf16 exactly.
-template <class T, class O, bool DW>
-__global__ __launch_bounds__(kThreads) void grad_kernel(O* __restrict__ out, const GradParams p) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, g = lane >> 5;
-    const int k0 = (blockIdx.x * 2 + (wave & 1)) * 32, k = k0 + c < p.K ? k0 + c : p.K - 1;
-    const int64_t j = ((int64_t)blockIdx.y * 2 + (wave >> 1)) * 32 + c, ja = j < p.J ? j : p.J - 1;
-    const T* dy = static_cast<const T*>(p.dy);
-    v16f acc = {};
-    for (int64_t r0 = 0; r0 < p.R; r0 += 16) {
-        v8bf V, D[kParts<T>];
+// Sums of dy's columns over a slab of its rows: a workgroup takes 256 columns, eight a thread, and eight rows at a time.
+template <class T>
+__global__ __launch_bounds__(kThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
+    __shared__ float shared[8][256 + 8];
+    const int t = threadIdx.x, c = (blockIdx.x * 32 + (t & 31)) * 8;
+    const int64_t begin = blockIdx.y * slab, end = begin + slab < rows ? begin + slab : rows;
+    float s[8] = {};
+    if (c < n)
+        for (int64_t r = begin + (t >> 5); r < end; r += 8) {
+            float v[8];
+            load_upto8(dy + r * ld + c, n - c, v);
 #pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            const int64_t r = r0 + 8 * g + t;
-            float v = 0.0f, d = 0.0f;
-            if (r < p.R) {
-                const uint32_t byte = p.scales[r * p.scale_pitch + (k >> 5)];
-                if constexpr (DW) v = byte == 255 ? scale_value(byte) : __builtin_amdgcn_ldexpf((float)(int8_t)p.codes[r * p.code_pitch + k], (int)byte - 133);
-                else {
-                    const uint32_t q = p.codes[r * p.code_pitch + (k >> 1)] >> (4 * (k & 1));
-                    v = byte == 255 ? scale_value(byte) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(q, scale_value(byte), 0)[0];
-                }
-                d = (float)(DW ? dy[r * p.lddy + ja] : dy[ja * p.lddy + r]);
-            }
-            V[t] = (__bf16)v;
-            __bf16 part[kParts<T>];
-            split(d, part);
-#pragma unroll
-            for (int i = 0; i < kParts<T>; ++i) D[i][t] = part[i];
+            for (int i = 0; i < 8; ++i) s[i] += v[i];
         }
 #pragma unroll
-        for (int i = 0; i < kParts<T>; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(V, D[i], acc, 0, 0, 0);
-    }
-    if (j >= p.J) return;
+    for (int i = 0; i < 8; ++i) shared[t >> 5][(t & 31) * 8 + i] = s[i];
+    __syncthreads();
+    const int col = blockIdx.x * 256 + t;
+    if (col >= n) return;
+    float total = shared[0][t];
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int kk = k0 + 8 * (i >> 2) + 4 * g + (i & 3);
-        if (kk < p.K) out[j * p.ldo + kk] = (O)acc[i];
+    for (int i = 1; i < 8; ++i) total += shared[i][t];
+    sum[(int64_t)blockIdx.y * n + col] = total;
+}
+
+// ---- plan ----------------------------------------------------------------------------
+struct GradPlan {
+    int tile;                // 256 or 128: results a workgroup makes along either side
+    int parts;               // of the reduction
+    int slabs;               // of rows for the column sums
+    size_t partial_bytes, bytes;
+};
+static GradPlan grad_plan(int dy_type, int64_t J, int64_t R, int K, bool dw) {
+    GradPlan p = {};
+    const auto tiles = [&](int t) { return ((J + t - 1) / t) * ((K + t - 1) / t); };
+    p.tile = dy_type == SPARQ_MX_BF16 && tiles(256) >= 192 ? 256 : 128;
+    const int64_t n = tiles(p.tile), steps = (R + kGradStep - 1) / kGradStep;
+    int64_t parts = p.tile == 256 ? 1 : 512 / n;
+    if (parts > steps / 4) parts = steps / 4;
+    p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    p.slabs = !dw ? 0 : (int)(R < 64 ? 1 : R / 64 < 64 ? R / 64 : 64);
+    p.partial_bytes = p.parts > 1 ? (size_t)round_up(p.parts * J * K * 4, 256) : 0;
+    p.bytes = p.partial_bytes + (p.slabs > 1 ? (size_t)round_up((int64_t)p.slabs * J * 4, 256) : 0);
+    return p;
+}
+// The workspace does not depend on dy's type: the largest of the three.
+static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
+    size_t most = 0;
+    for (int t : {SPARQ_MX_F32, SPARQ_MX_BF16}) {
+        const size_t b = grad_plan(t, J, R, K, dw).bytes;
+        most = b > most ? b : most;
     }
+    return most;
 }
 
-template <class T>
-__global__ __launch_bounds__(kThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, float* __restrict__ sum) {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= n) return;
-    float s = 0.0f;
-    for (int64_t r = 0; r < rows; ++r) s += (float)dy[r * ld + c];
-    sum[c] = s;
+template <class O>
+static void launch_join(const float* partial, O* out, int64_t J, int K, int64_t ldo, int parts, hipStream_t stream) {
+    const unsigned gx = (unsigned)((K + 4 * kThreads - 1) / (4 * kThreads));
+    grad_join_kernel<O><<<dim3(gx, (unsigned)(J < 65535 ? J : 65535)), kThreads, 0, stream>>>(partial, out, J, K, ldo, parts);
 }
 
-template <bool DW>
-static sparq_status launch_grad(const GradParams& p, int dy_type, void* out, int out_type, hipStream_t stream) {
-    const dim3 grid((p.K + 63) / 64, (unsigned)((p.J + 63) / 64));
-    with_type(dy_type, [&](auto t) {
-        with_type(out_type, [&](auto o) {
-            typedef decltype(t) T;
-            typedef decltype(o) O;
-            grad_kernel<T, O, DW><<<grid, kThreads, 0, stream>>>(static_cast<O*>(out), p);
-        });
+static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
+                         int64_t ldo, int64_t J, int64_t R, int K, const GradPlan& plan, void* workspace, hipStream_t stream) {
+    const int t = plan.tile;
+    GradParams p = {};
+    p.dy = dy;
+    p.codes = static_cast<const uint8_t*>(codes);
+    p.scales = static_cast<const uint8_t*>(scales);
+    p.lddy = lddy;
+    p.code_pitch = code_pitch(K, bits);
+    p.scale_pitch = scale_pitch(K);
+    p.J = J;
+    p.R = R;
+    p.K = K;
+    p.K128 = (int)round_up(K, kCodeUnit);
+    const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
+    if (tiles_j * tiles_k >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    p.tiles_j = (int)tiles_j;
+    p.tiles_k = (int)tiles_k;
+    p.steps_per_part = (int)((steps + plan.parts - 1) / plan.parts);
+    const bool parted = plan.parts > 1;
+    p.ldo = parted ? K : ldo;
+    p.part_stride = parted ? J * K : 0;
+    const sparq_status s = launch_grad(p, plan.parts, t, dy_type, bits == 8, parted ? workspace : out, parted ? SPARQ_MX_F32 : out_type, stream);
+    if (s != SPARQ_OK || !parted) return s;
+    with_type(out_type, [&](auto o) {
+        typedef decltype(o) O;
+        launch_join<O>(static_cast<const float*>(workspace), static_cast<O*>(out), J, K, ldo, plan.parts, stream);
     });
     return launch_status();
 }
 
-static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK; }
+static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40); }
 
 }  // namespace mx
 }  // namespace sparq
@@ -102,8 +127,12 @@ static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, 
 using namespace sparq;
 using namespace sparq::mx;
 
-extern "C" size_t sparq_mx_linear_dx_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
-extern "C" size_t sparq_mx_linear_dw_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+extern "C" size_t sparq_mx_linear_dx_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+    return grad_sizes_ok(M, N, K) && extent_ok(M, K) && M > 0 ? grad_bytes(M, N, K, false) : 0;
+}
+extern "C" size_t sparq_mx_linear_dw_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+    return grad_sizes_ok(M, N, K) ? grad_bytes(N, M, K, true) : 0;
+}
 
 extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int64_t lddy, const void* w_codes, const void* w_scales,
                                            void* dx, int32_t dx_type, int64_t lddx, int64_t M, int32_t N, int32_t K,
@@ -111,11 +140,11 @@ extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int6
     if (!grad_sizes_ok(M, N, K) || !type_valid(dy_type) || !type_valid(dx_type)) return SPARQ_EINVAL;
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
-    if (!extent_ok(M, lddy) || !extent_ok(M, lddx)) return SPARQ_EINVAL;
-    if (M > 65535 * 64ll) return SPARQ_EUNSUPPORTED;
-    const GradParams p = {dy, static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), lddy, code_pitch(K, 4),
-                          scale_pitch(K), lddx, M, N, K};
-    return launch_grad<false>(p, dy_type, dx, dx_type, static_cast<hipStream_t>(stream));
+    if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
+    const GradPlan plan = grad_plan(dy_type, M, N, K, false);
+    if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
+    if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
+    return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
 }
 
 extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int64_t lddy, const void* x_codes, const void* x_scales,
@@ -125,14 +154,18 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (!tensor_ok(dw, dw_type, lddw, K) || !extent_ok(N, lddw) || !aligned(db, 4)) return SPARQ_EINVAL;
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K)))
         return SPARQ_EINVAL;
-    if (N > 65535 * 64) return SPARQ_EUNSUPPORTED;
+    const GradPlan plan = grad_plan(dy_type, N, M, K, true);
+    if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
+    if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (db)
+    if (db) {
+        float* sums = plan.slabs > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes) : db;
         with_type(dy_type, [&](auto t) {
             typedef decltype(t) T;
-            column_sum_kernel<T><<<(N + kThreads - 1) / kThreads, kThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N, db);
+            column_sum_kernel<T><<<dim3((N + 255) / 256, plan.slabs), kThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
+                                                                                        (M + plan.slabs - 1) / plan.slabs, sums);
         });
-    const GradParams p = {dy, static_cast<const uint8_t*>(x_codes), static_cast<const uint8_t*>(x_scales), lddy, code_pitch(K, 8),
-                          scale_pitch(K), lddw, N, M, K};
-    return launch_grad<true>(p, dy_type, dw, dw_type, s);
+        if (plan.slabs > 1) launch_join<float>(sums, db, 1, N, N, plan.slabs, s);
+    }
+    return grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, N, M, K, plan, workspace, s);
 }

@@ -1,0 +1,351 @@
+// The product's gradients: out[j][k] = sum_r dy(j, r) V[r][k] on v_mfma_f32_32x32x16_bf16.
+//   dx: j = m, r = n, V = the 4-bit weights;   dw: j = n, r = m, V = the 8-bit checkpoint.
+// V's codes and scales go through registers into bf16 (their values are bf16 exactly: at most eight significand bits and a
+// power of two) and, turned so that the reduction index is the fast one, into LDS; dy goes the same way, as one bf16 part
+// (bf16), two (fp16) or three (fp32) whose sum is the value.
+// A workgroup of four wavefronts makes TJ x TK results in steps of 64 products, a wavefront a quarter of them.  Two tiles in LDS
+// and two sets of registers: while the matrix instructions work on step s, step s + 1 is converted and written to the other tile
+// and step s + 2 is on its way from memory; one barrier a step.
+#pragma once
+#include "sparq_mx_common.h"
+
+namespace sparq {
+namespace mx {
+
+struct GradParams {
+    const void* dy;
+    const uint8_t *codes, *scales;
+    int64_t lddy, code_pitch, scale_pitch, ldo;
+    int64_t J, R;                        // results [J][K], sums of R products
+    int64_t part_stride;                 // results of a part of the reduction lie this far apart (parts > 1)
+    int32_t K, K128, blocks;             // row length, the same in whole units of codes, bytes of a row of scales
+    int32_t tiles_j, tiles_k;
+    int32_t steps_per_part;              // steps of 64 products
+};
+
+constexpr int kGradThreads = 256;
+constexpr int kGradStep = 64;
+
+// The bf16 parts of a value: their sum is the value (8 significand bits a part; fp16 has 11, fp32 24).
+template <class T> inline constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
+template <> inline constexpr int kParts<__bf16> = 1;
+template <int P>
+__device__ __forceinline__ void split(float v, float (&part)[P]) {
+    part[0] = v;
+#pragma unroll
+    for (int i = 1; i < P; ++i) {
+        const float rounded = (float)(__bf16)part[i - 1];
+        const float rest = part[i - 1] - rounded;
+        part[i - 1] = rounded;
+        part[i] = __builtin_fabsf(rounded) < __builtin_inff() ? rest : 0.0f;       // NaN, infinity: nothing to add
+    }
+}
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return pack2(a, b, __bf16{}); }
+
+// C neighbouring elements
+template <int BYTES> struct Word;
+template <> struct Word<2> { typedef uint16_t Type; };
+template <> struct Word<4> { typedef uint32_t Type; };
+template <> struct Word<8> { typedef v2u Type; };
+
+// 16-byte unit of a tile: rows of 64 bf16 are eight of them, permuted so that neither eight rows at one place of the reduction
+// (the matrix operands' reads) nor every eighth row (the writes of turned blocks) meet in the same banks.
+__device__ __forceinline__ int unit_at(int row, int chunk) { return row * 8 + (chunk ^ ((row ^ (row >> 3)) & 7)); }
+
+// An element of type T in a register's low (half 0) or high half
+template <class T>
+__device__ __forceinline__ float element(uint32_t w, int half) {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+    else {
+        const uint16_t h = (uint16_t)(half ? w >> 16 : w);
+        return (float)__builtin_bit_cast(T, h);
+    }
+}
+// COUNT neighbouring elements as they lie in memory, of which the first n are there
+template <class T, int COUNT>
+__device__ __forceinline__ void fetch(uint32_t (&w)[COUNT * sizeof(T) / 4], const T* at, bool whole, int64_t n) {
+    constexpr int W = COUNT * sizeof(T) / 4;
+    if (whole) __builtin_memcpy(w, at, sizeof(w));
+    else {
+#pragma unroll
+        for (int i = 0; i < W; ++i) {
+            if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, at[i]) : 0u;
+            else {
+                const uint32_t lo = 2 * i < n ? __builtin_bit_cast(uint16_t, at[2 * i]) : 0u;
+                const uint32_t hi = 2 * i + 1 < n ? __builtin_bit_cast(uint16_t, at[2 * i + 1]) : 0u;
+                w[i] = lo | hi << 16;
+            }
+        }
+    }
+}
+
+// dy's side of a tile.  TURN: dy [r][j], a thread takes 8 r x N j; else dy [j][r], a thread takes N runs of 8 r.
+template <class T, int TJ, bool TURN>
+struct DyTile {
+    static constexpr int P = kParts<T>, N = TJ / 32;
+    static constexpr int kRuns = TURN ? 8 : N, kLength = TURN ? N : 8, kPer = 4 / sizeof(T);        // elements a word
+    uint32_t v[kRuns][kLength / kPer];
+
+    int row;                                                 // of the tile, of the thread's first column (TURN) or run
+
+    // WHOLE: the step lies inside dy.  TURN: a thread whose columns would reach past the last one takes the last N instead, some of
+    // them beside a neighbour who writes the same; rows of the tile past the last column are then left as they are: the
+    // results they make are not stored.
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const GradParams& p, int64_t j0, int64_t r0) {
+        const T* dy = static_cast<const T*>(p.dy);
+        const int t = threadIdx.x;
+        if constexpr (TURN) {
+            int64_t j = j0 + (t & 31) * N;
+            if (WHOLE) j = j < p.J - N ? j : p.J - N;
+            row = (int)(j - j0);
+            const int64_t r = r0 + (t >> 5) * 8;
+            const T* at = dy + r * p.lddy + j;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                fetch<T, N>(v[i], at, WHOLE, r + i < p.R ? p.J - j : 0);
+                at += p.lddy;
+            }
+        } else {
+            const int64_t r = r0 + (t & 7) * 8;
+            row = t >> 3;
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                int64_t j = j0 + row + 32 * i;
+                j = j < p.J ? j : p.J - 1;                   // (rows past the last one: as above)
+                fetch<T, 8>(v[i], dy + j * p.lddy + r, WHOLE, p.R - r);
+            }
+        }
+    }
+    // column or run c into the parts' tiles
+    __device__ __forceinline__ void store(v4u* lds, int c) const {
+        const int t = threadIdx.x;
+        const int at_row = TURN ? row + c : row + 32 * c, chunk = TURN ? t >> 5 : t & 7;
+        if (TURN && at_row < 0) return;
+        const int at = unit_at(at_row, chunk);
+        if constexpr (P == 1) {
+            v4u w;
+#pragma unroll
+            for (int a = 0; a < 4; ++a)
+                w[a] = TURN ? __builtin_amdgcn_perm(v[2 * a + 1][c / 2], v[2 * a][c / 2], c & 1 ? 0x07060302u : 0x05040100u) : v[c][a];
+            lds[at] = w;
+        } else {
+            float part[8][P];
+#pragma unroll
+            for (int a = 0; a < 8; ++a) split<P>(TURN ? element<T>(v[a][c / kPer], c % kPer) : element<T>(v[c][a / kPer], a % kPer), part[a]);
+#pragma unroll
+            for (int i = 0; i < P; ++i) {
+                v4u w;
+#pragma unroll
+                for (int a = 0; a < 4; ++a) w[a] = pack_bf16(part[2 * a][i], part[2 * a + 1][i]);
+                lds[i * TJ * 8 + at] = w;
+            }
+        }
+    }
+};
+
+// The coded side: a thread takes 8 r x COLS k.
+template <int BITS, int TK>
+struct CodedTile {
+    static constexpr int N = TK / 32;
+    typedef typename Word<N * BITS / 8>::Type Raw;
+    Raw raw[8];
+    uint32_t scale[8];
+
+    template <bool WHOLE>
+    __device__ __forceinline__ void load(const GradParams& p, int k0, int64_t r0) {
+        const int t = threadIdx.x;
+        int k = k0 + (t & 31) * N;
+        k = k < p.K128 ? k : p.K128 - N;                     // (columns past the last one make results that are not stored)
+        const int64_t r = r0 + (t >> 5) * 8;
+        const uint8_t *at = p.codes + r * p.code_pitch + k * BITS / 8, *sc = p.scales + r * p.scale_pitch + (k >> 5);
+        if constexpr (WHOLE) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                raw[i] = *reinterpret_cast<const Raw*>(at);
+                scale[i] = *sc;
+                at += p.code_pitch;
+                sc += p.scale_pitch;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                raw[i] = Raw{};
+                scale[i] = 127;
+                if (r + i < p.R) {
+                    raw[i] = *reinterpret_cast<const Raw*>(at + i * p.code_pitch);
+                    scale[i] = sc[i * p.scale_pitch];
+                }
+            }
+        }
+    }
+    // columns 2 q and 2 q + 1
+    __device__ __forceinline__ void store(v4u* lds, int q) const {
+        const int t = threadIdx.x, row = (t & 31) * N + 2 * q, chunk = t >> 5;
+        v4u even, odd;
+        if constexpr (BITS == 4) {
+            uint32_t pair[8];                                // columns 2 q (low) and 2 q + 1 of a row
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float s = scale_value(scale[i]);
+                const v2bf b = q == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 0)
+                               : q == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 1)
+                               : q == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 2)
+                                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 3);
+                pair[i] = scale[i] == 255 ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, b);
+            }
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                even[a] = __builtin_amdgcn_perm(pair[2 * a + 1], pair[2 * a], 0x05040100u);
+                odd[a] = __builtin_amdgcn_perm(pair[2 * a + 1], pair[2 * a], 0x07060302u);
+            }
+        } else {
+            float v[8][2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t w;
+                if constexpr (N == 8) w = raw[i][q >> 1];
+                else w = raw[i];
+                const float s = __builtin_amdgcn_ldexpf(scale[i] == 255 ? __uint_as_float(0x7FC00000u) : 1.0f, (int)scale[i] - 133);
+                v[i][0] = (float)(int8_t)(w >> (16 * (q & 1))) * s;
+                v[i][1] = (float)(int8_t)(w >> (16 * (q & 1) + 8)) * s;
+            }
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+                even[a] = pack_bf16(v[2 * a][0], v[2 * a + 1][0]);
+                odd[a] = pack_bf16(v[2 * a][1], v[2 * a + 1][1]);
+            }
+        }
+        lds[unit_at(row, chunk)] = even;
+        lds[unit_at(row + 1, chunk)] = odd;
+    }
+};
+
+// Tiles in an order that keeps what the workgroups of one XCD (every eighth) work on at a time close together: each XCD gets a run of
+// tiles, eight columns of them wide.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_j, uint32_t tiles_k, uint32_t& tj, uint32_t& tk) {
+    const uint32_t n = tiles_j * tiles_k, x = id & 7, per = n >> 3, more = n & 7;
+    id = x * per + (x < more ? x : more) + (id >> 3);
+    const uint32_t width = 8, group = id / (width * tiles_j), first = group * width, w = tiles_k - first < width ? tiles_k - first : width;
+    const uint32_t in = id - group * width * tiles_j;
+    tj = in / w;
+    tk = first + in - tj * w;
+}
+
+template <class T, class O, bool DW, int TJ, int TK>
+__global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
+    constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
+    constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
+    extern __shared__ v4u lds[];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, g = lane >> 5;
+    const int wj = (wave >> 1) * (TJ / 2), wk = (wave & 1) * (TK / 2);
+    uint32_t tj, tk;
+    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
+    const int64_t j0 = (int64_t)tj * TJ;
+    const int k0 = (int)tk * TK;
+    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
+    const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all;
+    // steps before this one are whole
+    const int64_t whole = DW && p.J < TJ / 32 ? 0 : p.R / kGradStep, s_fast = whole < s_end ? whole : s_end;
+
+    v16f acc[FK][FJ];
+#pragma unroll
+    for (int a = 0; a < FK; ++a)
+#pragma unroll
+        for (int b = 0; b < FJ; ++b) acc[a][b] = v16f{};
+
+    constexpr int kDyParts = TJ / 32, kCodedParts = TK / 64;
+    typedef DyTile<T, TJ, DW> Dy;
+    typedef CodedTile<BITS, TK> Coded;
+    // quarter q of a step into a tile
+    auto convert = [&](const Dy& dy, const Coded& coded, v4u* tile, int q) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < kDyParts / 4; ++i) dy.store(tile, q * (kDyParts / 4) + i);
+        if (kCodedParts >= 4 || (q & 1) == 0) coded.store(tile + P * TJ * 8, kCodedParts >= 4 ? q : q >> 1);
+    };
+    // products of quarter q of a tile
+    auto multiply = [&](const v4u* tile, int q) __attribute__((always_inline)) {
+        const v4u* tile_k = tile + P * TJ * 8;
+        v8bf a[FK], b[P][FJ];
+#pragma unroll
+        for (int f = 0; f < FK; ++f) a[f] = __builtin_bit_cast(v8bf, tile_k[unit_at(wk + 32 * f + c, 2 * q + g)]);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int f = 0; f < FJ; ++f) b[i][f] = __builtin_bit_cast(v8bf, tile[i * TJ * 8 + unit_at(wj + 32 * f + c, 2 * q + g)]);
+#pragma unroll
+        for (int i = 0; i < P; ++i)
+#pragma unroll
+            for (int x = 0; x < FK; ++x)
+#pragma unroll
+                for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[i][y], acc[x][y], 0, 0, 0);
+    };
+
+    if (s_begin < s_fast) {
+        Dy dy[2];
+        Coded coded[2];
+        auto load = [&](int64_t s, int set) __attribute__((always_inline)) {
+            s = s < s_fast ? s : s_fast - 1;                 // (past the end: the last step again, into registers nobody reads)
+            dy[set].template load<true>(p, j0, s * kGradStep);
+            coded[set].template load<true>(p, k0, s * kGradStep);
+        };
+        auto step = [&](int64_t s, int set) __attribute__((always_inline)) {
+            load(s + 2, set);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                multiply(lds + set * kUnits, q);
+                convert(dy[set ^ 1], coded[set ^ 1], lds + (set ^ 1) * kUnits, q);
+            }
+            __syncthreads();
+        };
+        load(s_begin, 0);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) convert(dy[0], coded[0], lds, q);
+        load(s_begin + 1, 1);
+        __syncthreads();
+        for (int64_t s = s_begin; s < s_fast; s += 2) {
+            step(s, 0);
+            if (s + 1 < s_fast) step(s + 1, 1);
+        }
+    }
+    // what is left: the last products where their number is no multiple of a step
+    for (int64_t s = s_begin < s_fast ? s_fast : s_begin; s < s_end; ++s) {
+        Dy dy;
+        Coded coded;
+        dy.template load<false>(p, j0, s * kGradStep);
+        coded.template load<false>(p, k0, s * kGradStep);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) convert(dy, coded, lds, q);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) multiply(lds, q);
+    }
+
+    out += blockIdx.y * p.part_stride;
+#pragma unroll
+    for (int y = 0; y < FJ; ++y) {
+        const int64_t j = j0 + wj + 32 * y + c;
+        if (j >= p.J) continue;
+        O* row = out + j * p.ldo;
+#pragma unroll
+        for (int x = 0; x < FK; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = k0 + wk + 32 * x + 8 * i + 4 * g;
+                if (k + 4 <= p.K) {
+                    O v[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) v[e] = (O)acc[x][y][4 * i + e];
+                    __builtin_memcpy(row + k, v, sizeof(v));
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (k + e < p.K) row[k + e] = (O)acc[x][y][4 * i + e];
+                }
+            }
+    }
+}
+
+}  // namespace mx
+}  // namespace sparq
