@@ -56,7 +56,7 @@ sparq_status sparq_mx_dequantize(const void *codes, const void *scales, int32_t 
                                  void *y, int32_t type, int64_t ldy, int64_t rows, int32_t K, void *stream);
 
 /* y[m][n] = sum_k A[m][k] W[n][k] + bias[n] over 4-bit A [M][K] and W [N][K] on the block-scaled matrix instruction.
- * bias: fp32 [N] or NULL. */
+ * bias: fp32 [N] or NULL.  K up to 2^23. */
 size_t sparq_mx_gemm_workspace_bytes(int64_t M, int32_t N, int32_t K);
 sparq_status sparq_mx_gemm(const void *a_codes, const void *a_scales, const void *w_codes, const void *w_scales,
                            const float *bias, void *y, int32_t type, int64_t ldy, int64_t M, int32_t N, int32_t K,

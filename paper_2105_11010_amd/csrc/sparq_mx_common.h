@@ -195,11 +195,26 @@ __device__ __forceinline__ void values8_of(v2u w, uint32_t byte, float (&v)[8]) 
         for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
     }
 }
+
+// Tiles in an order that keeps what the workgroups of one XCD (every eighth) work on at a time close together: each XCD gets a run of
+// tiles, eight columns of them wide.
+__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_j, uint32_t tiles_k, uint32_t& tj, uint32_t& tk) {
+    const uint32_t n = tiles_j * tiles_k, x = id & 7, per = n >> 3, more = n & 7;
+    id = x * per + (x < more ? x : more) + (id >> 3);
+    const uint32_t width = 8, group = id / (width * tiles_j), first = group * width, w = tiles_k - first < width ? tiles_k - first : width;
+    const uint32_t in = id - group * width * tiles_j;
+    tj = in / w;
+    tk = first + in - tj * w;
+}
 #endif
 
 // Implemented in sparq_mx_codec.hip: the arguments are checked already.
 sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows, int K, void* codes4, void* scales4, void* codes8,
                              void* scales8, hipStream_t stream);
+
+// Implemented in sparq_mx_join.hip: out[j][k] = the sum over the parts of partial [parts][J][K], part after part, + bias[k]
+// (NULL: none), rounded to the type.
+sparq_status launch_join(const float* partial, const float* bias, void* out, int type, int64_t J, int K, int64_t ldo, int parts, hipStream_t stream);
 
 }  // namespace mx
 }  // namespace sparq

@@ -1,54 +1,75 @@
 // The product of 4-bit operands (include/sparq_mx.h).
-#include "sparq_mx_common.h"
+#include "sparq_mx_gemm_kernel.h"
 
 namespace sparq {
 namespace mx {
 
-constexpr int kThreads = 256;
-
-struct GemmParams {
-    const uint8_t *a, *as, *w, *ws;
-    const float* bias;
-    int64_t M, ldy, code_pitch, scale_pitch;
-    int32_t N, steps;                    // steps of 64 values
+struct GemmPlan {
+    int tile;                // 256 or 128: results a workgroup makes along either side
+    int parts;               // of the reduction
+    size_t bytes;            // of partial results
 };
-
-// y[m][n] = sum_k W[n][k] A[m][k] on v_mfma_scale_f32_32x32x64: a lane feeds 32 values of one row, i.e. one block and its
-// scale.  The weights are the instruction's first operand, so that a lane ends with four neighbouring n of one m.
-// A wavefront makes 32 x 32 results from operands read where they are.
-template <class T>
-__global__ __launch_bounds__(kThreads) void gemm_kernel(T* __restrict__ y, const GemmParams p) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, r = lane & 31, g = lane >> 5;
-    const int64_t m = ((int64_t)blockIdx.y * 2 + (wave >> 1)) * 32 + r;
-    const int n0 = (blockIdx.x * 2 + (wave & 1)) * 32;
-    const int64_t ma = m < p.M ? m : p.M - 1;
-    const int na = n0 + r < p.N ? n0 + r : p.N - 1;
-    const uint8_t *a = p.a + ma * p.code_pitch + 16 * g, *as = p.as + ma * p.scale_pitch + g;
-    const uint8_t *w = p.w + na * p.code_pitch + 16 * g, *ws = p.ws + na * p.scale_pitch + g;
-    v16f acc = {};
-    for (int s = 0; s < p.steps; ++s) {
-        const v4i av = *reinterpret_cast<const v4i*>(a + 32 * (int64_t)s), wv = *reinterpret_cast<const v4i*>(w + 32 * (int64_t)s);
-        const v8i A = {av[0], av[1], av[2], av[3], 0, 0, 0, 0}, W = {wv[0], wv[1], wv[2], wv[3], 0, 0, 0, 0};
-        acc = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(W, A, acc, 4, 4, 0, ws[2 * s], 0, as[2 * s]);
-    }
-    if (m >= p.M) return;
-#pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        const int n = n0 + 8 * (i >> 2) + 4 * g + (i & 3);
-        if (n < p.N) y[m * p.ldy + n] = (T)(acc[i] + (p.bias ? p.bias[n] : 0.0f));
-    }
+static GemmPlan gemm_plan(int64_t M, int N, int K) {
+    GemmPlan p = {};
+    const auto tiles = [&](int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+    p.tile = tiles(256) >= 192 ? 256 : 128;
+    const int64_t n = tiles(p.tile), steps = (K + kCodeUnit - 1) / kCodeUnit;
+    int64_t parts = p.tile == 256 ? 1 : 512 / n;
+    if (parts > steps / 8) parts = steps / 8;
+    p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    p.bytes = p.parts > 1 ? (size_t)round_up(p.parts * M * N * 4, 256) : 0;
+    return p;
 }
 
-sparq_status launch_gemm(const GemmParams& p, void* y, int type, hipStream_t stream) {
-    const dim3 grid((p.N + 63) / 64, (unsigned)((p.M + 63) / 64));
-    with_type(type, [&](auto t) {
-        typedef decltype(t) T;
-        gemm_kernel<T><<<grid, kThreads, 0, stream>>>(static_cast<T*>(y), p);
-    });
+template <class O, int TILE>
+static sparq_status launch_tile(const GemmParams& p, int parts, void* y, hipStream_t stream) {
+    const auto kernel = gemm_kernel<O, TILE, TILE>;
+    constexpr int lds_bytes = 4 * 2 * TILE * 64 + 2 * 2 * TILE * 16;
+    static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
+    static std::atomic<bool> allowed[kMaxDevices];           // the attribute is set once per device (twice at worst)
+    const int slot = current_device_slot();
+    if (!allowed[slot].load(std::memory_order_relaxed) || slot == kMaxDevices - 1) {
+        if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes) != hipSuccess)
+            return SPARQ_ELAUNCH;
+        allowed[slot].store(true, std::memory_order_relaxed);
+    }
+    kernel<<<dim3(p.tiles_m * p.tiles_n, parts), kGemmThreads, lds_bytes, stream>>>(static_cast<O*>(y), p);
     return launch_status();
 }
 
-static bool gemm_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK; }
+static sparq_status gemm(const void* a, const void* as, const void* w, const void* ws, const float* bias, void* y, int type, int64_t ldy,
+                         int64_t M, int N, int K, const GemmPlan& plan, void* workspace, hipStream_t stream) {
+    const int t = plan.tile;
+    const int64_t tiles_m = (M + t - 1) / t, tiles_n = (N + t - 1) / t;
+    if (tiles_m * tiles_n >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    const bool parted = plan.parts > 1;
+    GemmParams p = {};
+    p.a = static_cast<const uint8_t*>(a);
+    p.as = static_cast<const uint8_t*>(as);
+    p.w = static_cast<const uint8_t*>(w);
+    p.ws = static_cast<const uint8_t*>(ws);
+    p.bias = parted ? nullptr : bias;
+    p.M = M;
+    p.N = N;
+    p.ldy = parted ? N : ldy;
+    p.part_stride = parted ? M * N : 0;
+    p.code_pitch = (uint32_t)code_pitch(K, 4);
+    p.scale_pitch = (uint32_t)scale_pitch(K);
+    p.tiles_m = (uint32_t)tiles_m;
+    p.tiles_n = (uint32_t)tiles_n;
+    p.steps = (K + kCodeUnit - 1) / kCodeUnit;
+    p.steps_per_part = (int)round_up((p.steps + plan.parts - 1) / plan.parts, 4);
+    sparq_status s = SPARQ_OK;
+    with_type(parted ? SPARQ_MX_F32 : type, [&](auto o) {
+        typedef decltype(o) O;
+        void* to = parted ? workspace : y;
+        s = t == 256 ? launch_tile<O, 256>(p, plan.parts, to, stream) : launch_tile<O, 128>(p, plan.parts, to, stream);
+    });
+    if (s != SPARQ_OK || !parted) return s;
+    return launch_join(static_cast<const float*>(workspace), bias, y, type, M, N, ldy, plan.parts, stream);
+}
+
+static bool gemm_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40) && K <= kGemmMaxK; }
 
 }  // namespace mx
 }  // namespace sparq
@@ -56,7 +77,9 @@ static bool gemm_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, 
 using namespace sparq;
 using namespace sparq::mx;
 
-extern "C" size_t sparq_mx_gemm_workspace_bytes(int64_t, int32_t, int32_t) { return 0; }
+extern "C" size_t sparq_mx_gemm_workspace_bytes(int64_t M, int32_t N, int32_t K) {
+    return gemm_sizes_ok(M, N, K) && M > 0 ? gemm_plan(M, N, K).bytes : 0;
+}
 
 extern "C" sparq_status sparq_mx_gemm(const void* a_codes, const void* a_scales, const void* w_codes, const void* w_scales,
                                       const float* bias, void* y, int32_t type, int64_t ldy, int64_t M, int32_t N, int32_t K,
@@ -65,16 +88,16 @@ extern "C" sparq_status sparq_mx_gemm(const void* a_codes, const void* a_scales,
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(a_codes, a_scales) || !coded_ok(w_codes, w_scales) || !aligned(bias, 4)) return SPARQ_EINVAL;
     if (!tensor_ok(y, type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K)) return SPARQ_EINVAL;
-    if (M > 65535 * 64ll) return SPARQ_EUNSUPPORTED;
-    const GemmParams p = {static_cast<const uint8_t*>(a_codes), static_cast<const uint8_t*>(a_scales), static_cast<const uint8_t*>(w_codes),
-                          static_cast<const uint8_t*>(w_scales), bias, M, ldy, code_pitch(K, 4), scale_pitch(K), N, (K + 63) / 64};
-    return launch_gemm(p, y, type, static_cast<hipStream_t>(stream));
+    const GemmPlan plan = gemm_plan(M, N, K);
+    if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
+    if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
+    return gemm(a_codes, a_scales, w_codes, w_scales, bias, y, type, ldy, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
 }
 
 static size_t coded_bytes(int64_t M, int K) { return (size_t)(round_up(M * code_pitch(K, 4), 256) + round_up(M * scale_pitch(K), 256)); }
 
 extern "C" size_t sparq_mx_linear_workspace_bytes(int64_t M, int32_t N, int32_t K) {
-    return gemm_sizes_ok(M, N, K) && extent_ok(M, K) ? coded_bytes(M, K) : 0;
+    return gemm_sizes_ok(M, N, K) && M > 0 ? coded_bytes(M, K) + gemm_plan(M, N, K).bytes : 0;
 }
 
 extern "C" sparq_status sparq_mx_linear(const void* x, int32_t x_type, int64_t ldx, const void* w_codes, const void* w_scales,
@@ -86,13 +109,12 @@ extern "C" sparq_status sparq_mx_linear(const void* x, int32_t x_type, int64_t l
     if (!tensor_ok(x, x_type, ldx, K) || !extent_ok(M, ldx) || !tensor_ok(y, y_type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K))
         return SPARQ_EINVAL;
     if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
-    if (workspace_bytes < coded_bytes(M, K)) return SPARQ_EWORKSPACE;
-    if (M > 65535 * 64ll) return SPARQ_EUNSUPPORTED;
+    const GemmPlan plan = gemm_plan(M, N, K);
+    const size_t coded = coded_bytes(M, K);
+    if (workspace_bytes < coded + plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     uint8_t *codes = static_cast<uint8_t*>(workspace), *scales = codes + round_up(M * code_pitch(K, 4), 256);
     const sparq_status q = launch_quantize(x, x_type, ldx, M, K, codes, scales, nullptr, nullptr, s);
     if (q != SPARQ_OK) return q;
-    const GemmParams p = {codes, scales, static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), bias, M, ldy,
-                          code_pitch(K, 4), scale_pitch(K), N, (K + 63) / 64};
-    return launch_gemm(p, y, y_type, s);
+    return gemm(codes, scales, w_codes, w_scales, bias, y, y_type, ldy, M, N, K, plan, codes + coded, s);
 }

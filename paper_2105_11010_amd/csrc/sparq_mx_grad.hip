@@ -6,27 +6,6 @@ namespace mx {
 
 constexpr int kThreads = 256;
 
-// out = the parts' sum, part after part; four values a thread.
-template <class O>
-__global__ __launch_bounds__(kThreads) void grad_join_kernel(const float* __restrict__ partial, O* __restrict__ out, int64_t J, int K, int64_t ldo, int parts) {
-    const int k = (blockIdx.x * kThreads + threadIdx.x) * 4;
-    if (k >= K) return;
-    const int n = K - k < 4 ? K - k : 4;
-    for (int64_t j = blockIdx.y; j < J; j += gridDim.y) {
-        float s[4] = {};
-        for (int i = 0; i < parts; ++i) {
-            const float* at = partial + (i * J + j) * K + k;
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) s[e] += at[e];
-        }
-        O* to = out + j * ldo + k;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < n) to[e] = (O)s[e];
-    }
-}
-
 // Sums of dy's columns over a slab of its rows: a workgroup takes 256 columns, eight a thread, and eight rows at a time.
 template <class T>
 __global__ __launch_bounds__(kThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
@@ -82,12 +61,6 @@ static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
     return most;
 }
 
-template <class O>
-static void launch_join(const float* partial, O* out, int64_t J, int K, int64_t ldo, int parts, hipStream_t stream) {
-    const unsigned gx = (unsigned)((K + 4 * kThreads - 1) / (4 * kThreads));
-    grad_join_kernel<O><<<dim3(gx, (unsigned)(J < 65535 ? J : 65535)), kThreads, 0, stream>>>(partial, out, J, K, ldo, parts);
-}
-
 static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
                          int64_t ldo, int64_t J, int64_t R, int K, const GradPlan& plan, void* workspace, hipStream_t stream) {
     const int t = plan.tile;
@@ -112,11 +85,7 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     p.part_stride = parted ? J * K : 0;
     const sparq_status s = launch_grad(p, plan.parts, t, dy_type, bits == 8, parted ? workspace : out, parted ? SPARQ_MX_F32 : out_type, stream);
     if (s != SPARQ_OK || !parted) return s;
-    with_type(out_type, [&](auto o) {
-        typedef decltype(o) O;
-        launch_join<O>(static_cast<const float*>(workspace), static_cast<O*>(out), J, K, ldo, plan.parts, stream);
-    });
-    return launch_status();
+    return launch_join(static_cast<const float*>(workspace), nullptr, out, out_type, J, K, ldo, plan.parts, stream);
 }
 
 static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40); }
@@ -165,7 +134,10 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
             column_sum_kernel<T><<<dim3((N + 255) / 256, plan.slabs), kThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
                                                                                         (M + plan.slabs - 1) / plan.slabs, sums);
         });
-        if (plan.slabs > 1) launch_join<float>(sums, db, 1, N, N, plan.slabs, s);
+        if (plan.slabs > 1) {
+            const sparq_status joined = launch_join(sums, nullptr, db, SPARQ_MX_F32, 1, N, N, plan.slabs, s);
+            if (joined != SPARQ_OK) return joined;
+        }
     }
     return grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, N, M, K, plan, workspace, s);
 }

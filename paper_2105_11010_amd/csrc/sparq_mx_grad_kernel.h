@@ -221,17 +221,6 @@ struct CodedTile {
     }
 };
 
-// Tiles in an order that keeps what the workgroups of one XCD (every eighth) work on at a time close together: each XCD gets a run of
-// tiles, eight columns of them wide.
-__device__ __forceinline__ void tile_of(uint32_t id, uint32_t tiles_j, uint32_t tiles_k, uint32_t& tj, uint32_t& tk) {
-    const uint32_t n = tiles_j * tiles_k, x = id & 7, per = n >> 3, more = n & 7;
-    id = x * per + (x < more ? x : more) + (id >> 3);
-    const uint32_t width = 8, group = id / (width * tiles_j), first = group * width, w = tiles_k - first < width ? tiles_k - first : width;
-    const uint32_t in = id - group * width * tiles_j;
-    tj = in / w;
-    tk = first + in - tj * w;
-}
-
 template <class T, class O, bool DW, int TJ, int TK>
 __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
     constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
