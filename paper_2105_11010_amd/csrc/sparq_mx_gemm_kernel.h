@@ -7,7 +7,7 @@
 #pragma once
 #include <type_traits>
 
-#include "sparq_mx_common.h"
+#include "sparq_mx_store.h"
 
 namespace sparq {
 namespace mx {
@@ -37,7 +37,8 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
     constexpr int FM = TM / 64, FN = TN / 64;                // 32 x 32 results a wavefront makes along either side
     constexpr int kBuffer = (TM + TN) * 64, kScaleBuffer = (TM + TN) * 16;
     constexpr int kLoads = (TM + TN) / 64;                   // of a step, a wavefront
-    extern __shared__ uint8_t lds[];                         // four buffers of codes, two of scales
+    static_assert(4 * kTurnBytes<O, FN * 32> <= 4 * kBuffer + 2 * kScaleBuffer, "results are turned where the operands were");
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds[];                         // four buffers of codes, two of scales
     uint8_t* const lds_scales = lds + 4 * kBuffer;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
     const int wm = (wave >> 1) * (TM / 2), wn = (wave & 1) * (TN / 2);
@@ -159,29 +160,9 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         __builtin_amdgcn_s_waitcnt(vmcnt(0));                // nothing is on its way to LDS when the wavefront ends
     }
 
-    y += blockIdx.y * p.part_stride;
-#pragma unroll
-    for (int j = 0; j < FM; ++j) {
-        const int64_t m = m0 + wm + 32 * j + c;
-        if (m >= p.M) continue;
-        O* row = y + m * p.ldy;
-#pragma unroll
-        for (int i = 0; i < FN; ++i)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int n = n0 + wn + 32 * i + 8 * q + 4 * g;
-                if (n + 4 <= p.N) {
-                    O v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (O)(acc[i][j][4 * q + e] + (p.bias ? p.bias[n + e] : 0.0f));
-                    __builtin_memcpy(row + n, v, sizeof(v));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (n + e < p.N) row[n + e] = (O)(acc[i][j][4 * q + e] + (p.bias ? p.bias[n + e] : 0.0f));
-                }
-            }
-    }
+    __syncthreads();
+    const __amdgpu_buffer_rsrc_t bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.bias), 0, p.bias ? p.N * 4 : 0, 0x00020000);
+    store_results<O, FN, FM>(acc, y + blockIdx.y * p.part_stride, p.ldy, m0 + wm, p.M, n0 + wn, p.N, bias, lds + wave * kTurnBytes<O, FN * 32>);
 #endif
 }
 

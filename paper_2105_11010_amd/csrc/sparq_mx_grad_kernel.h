@@ -7,7 +7,7 @@
 // and two sets of registers: while the matrix instructions work on step s, step s + 1 is converted and written to the other tile
 // and step s + 2 is on its way from memory; one barrier a step.
 #pragma once
-#include "sparq_mx_common.h"
+#include "sparq_mx_store.h"
 
 namespace sparq {
 namespace mx {
@@ -223,10 +223,12 @@ struct CodedTile {
 
 template <class T, class O, bool DW, int TJ, int TK>
 __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
     constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
     constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
+    static_assert(4 * kTurnBytes<O, FK * 32> <= 2 * kUnits * 16, "results are turned where the tiles were");
     extern __shared__ v4u lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = lane & 31, g = lane >> 5;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
     const int wj = (wave >> 1) * (TJ / 2), wk = (wave & 1) * (TK / 2);
     uint32_t tj, tk;
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
@@ -311,29 +313,11 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
         for (int q = 0; q < 4; ++q) multiply(lds, q);
     }
 
-    out += blockIdx.y * p.part_stride;
-#pragma unroll
-    for (int y = 0; y < FJ; ++y) {
-        const int64_t j = j0 + wj + 32 * y + c;
-        if (j >= p.J) continue;
-        O* row = out + j * p.ldo;
-#pragma unroll
-        for (int x = 0; x < FK; ++x)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = k0 + wk + 32 * x + 8 * i + 4 * g;
-                if (k + 4 <= p.K) {
-                    O v[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) v[e] = (O)acc[x][y][4 * i + e];
-                    __builtin_memcpy(row + k, v, sizeof(v));
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (k + e < p.K) row[k + e] = (O)acc[x][y][4 * i + e];
-                }
-            }
-    }
+    __syncthreads();
+    const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
+    store_results<O, FK, FJ>(acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none,
+                             reinterpret_cast<uint8_t*>(lds) + wave * kTurnBytes<O, FK * 32>);
+#endif
 }
 
 }  // namespace mx
