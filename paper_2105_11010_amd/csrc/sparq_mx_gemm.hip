@@ -22,10 +22,10 @@ static GemmPlan gemm_plan(int64_t M, int N, int K) {
 }
 
 template <class O, int TILE>
-static sparq_status launch_tile(const GemmParams& p, int parts, void* y, hipStream_t stream) {
+static sparq_status launch_tile(const GemmParams& p, void* y, hipStream_t stream) {
     const auto kernel = gemm_kernel<O, TILE, TILE>;
-    constexpr int lds_bytes = 4 * 2 * TILE * 64 + 2 * 2 * TILE * 16;
-    static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
+    constexpr int lds_bytes = kGemmLds<TILE>, per_cu = 160 * 1024 / lds_bytes;
+    static_assert(per_cu >= 1, "LDS of a CU");
     static std::atomic<bool> allowed[kMaxDevices];           // the attribute is set once per device (twice at worst)
     const int slot = current_device_slot();
     if (!allowed[slot].load(std::memory_order_relaxed) || slot == kMaxDevices - 1) {
@@ -33,7 +33,8 @@ static sparq_status launch_tile(const GemmParams& p, int parts, void* y, hipStre
             return SPARQ_ELAUNCH;
         allowed[slot].store(true, std::memory_order_relaxed);
     }
-    kernel<<<dim3(p.tiles_m * p.tiles_n, parts), kGemmThreads, lds_bytes, stream>>>(static_cast<O*>(y), p);
+    const uint32_t places = (uint32_t)(device_cu_count() * per_cu);
+    kernel<<<p.items < places ? p.items : places, kGemmThreads, lds_bytes, stream>>>(static_cast<O*>(y), p);
     return launch_status();
 }
 
@@ -41,7 +42,7 @@ static sparq_status gemm(const void* a, const void* as, const void* w, const voi
                          int64_t M, int N, int K, const GemmPlan& plan, void* workspace, hipStream_t stream) {
     const int t = plan.tile;
     const int64_t tiles_m = (M + t - 1) / t, tiles_n = (N + t - 1) / t;
-    if (tiles_m * tiles_n >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    if (tiles_m > INT32_MAX || tiles_m * tiles_n > INT32_MAX) return SPARQ_EUNSUPPORTED;
     const bool parted = plan.parts > 1;
     GemmParams p = {};
     p.a = static_cast<const uint8_t*>(a);
@@ -57,16 +58,19 @@ static sparq_status gemm(const void* a, const void* as, const void* w, const voi
     p.scale_pitch = (uint32_t)scale_pitch(K);
     p.tiles_m = (uint32_t)tiles_m;
     p.tiles_n = (uint32_t)tiles_n;
-    p.steps = (K + kCodeUnit - 1) / kCodeUnit;
+    p.steps = (int)round_up((K + kCodeUnit - 1) / kCodeUnit, 4);
     p.steps_per_part = (int)round_up((p.steps + plan.parts - 1) / plan.parts, 4);
+    const int parts = (p.steps + p.steps_per_part - 1) / p.steps_per_part;       // (as the plan has it, or fewer)
+    if (tiles_m * tiles_n * parts >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    p.items = (uint32_t)(tiles_m * tiles_n * parts);
     sparq_status s = SPARQ_OK;
     with_type(parted ? SPARQ_MX_F32 : type, [&](auto o) {
         typedef decltype(o) O;
         void* to = parted ? workspace : y;
-        s = t == 256 ? launch_tile<O, 256>(p, plan.parts, to, stream) : launch_tile<O, 128>(p, plan.parts, to, stream);
+        s = t == 256 ? launch_tile<O, 256>(p, to, stream) : launch_tile<O, 128>(p, to, stream);
     });
     if (s != SPARQ_OK || !parted) return s;
-    return launch_join(static_cast<const float*>(workspace), bias, y, type, M, N, ldy, plan.parts, stream);
+    return launch_join(static_cast<const float*>(workspace), bias, y, type, M, N, ldy, parts, stream);
 }
 
 static bool gemm_sizes_ok(int64_t M, int64_t N, int64_t K) { return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40) && K <= kGemmMaxK; }

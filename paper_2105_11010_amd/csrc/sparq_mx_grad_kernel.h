@@ -226,7 +226,6 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
     constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
-    static_assert(4 * kTurnBytes<O, FK * 32> <= 2 * kUnits * 16, "results are turned where the tiles were");
     extern __shared__ v4u lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
     const int wj = (wave >> 1) * (TJ / 2), wk = (wave & 1) * (TK / 2);
@@ -315,8 +314,8 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, FK, FJ>(acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none,
-                             reinterpret_cast<uint8_t*>(lds) + wave * kTurnBytes<O, FK * 32>);
+    store_results<O, FK, FJ, 128>(acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none,
+                             reinterpret_cast<uint8_t*>(lds) + wave * 4096);
 #endif
 }
 
