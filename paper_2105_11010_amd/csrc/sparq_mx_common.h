@@ -139,20 +139,22 @@ __device__ __forceinline__ uint32_t scale4_of(uint32_t top) {
     return e == 255 ? 255u : e > 2 ? e - 2 : 0u;
 }
 __device__ __forceinline__ uint32_t scale8_of(uint32_t top) { return top >> 23; }
-// 2^s as a float: byte 0 is 2^-127 (a subnormal), 255 is NaN
-__device__ __forceinline__ float scale_value(uint32_t byte) {
-    const uint32_t bits = byte ? byte << 23 : 0x00400000u;
-    return __uint_as_float(byte == 255 ? 0x7FC00000u : bits);
-}
+// The scale as the 4-bit conversion instructions take it: they look at the exponent field alone, 0 standing for 2^-127 and 255 for
+// NaN, which makes every value NaN.
+__device__ __forceinline__ float scale_operand(uint32_t byte) { return __uint_as_float(byte << 23); }
 // Eight 4-bit codes: the conversion instruction divides by the scale, rounds to nearest even and saturates at 6.
 __device__ __forceinline__ uint32_t codes4_of(const float (&v)[8], uint32_t byte) {
-    const float s = scale_value(byte);
+    const float s = scale_operand(byte);
     uint32_t w = 0;
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[0], v[1], s, 0);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[2], v[3], s, 1);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[4], v[5], s, 2);
     w = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(w, v[6], v[7], s, 3);
     return byte == 255 ? 0u : w;
+}
+// 2^s / 64, the unit of the 8-bit codes (byte 255: NaN)
+__device__ __forceinline__ float unit8_of(uint32_t byte) {
+    return __builtin_amdgcn_ldexpf(byte == 255 ? __uint_as_float(0x7FC00000u) : 1.0f, (int)byte - 133);
 }
 // Eight 8-bit codes
 __device__ __forceinline__ v2u codes8_of(const float (&v)[8], uint32_t byte) {
@@ -174,26 +176,26 @@ __device__ __forceinline__ v2u codes8_of(const float (&v)[8], uint32_t byte) {
 }
 // The values of eight codes
 __device__ __forceinline__ void values4_of(uint32_t w, uint32_t byte, float (&v)[8]) {
-    const float s = scale_value(byte);
+    const float s = scale_operand(byte);
     const v2f a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 1);
     const v2f c = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(w, s, 3);
     v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1]; v[4] = c[0]; v[5] = c[1]; v[6] = d[0]; v[7] = d[1];
-    if (byte == 255) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = s;
-    }
 }
 __device__ __forceinline__ void values8_of(v2u w, uint32_t byte, float (&v)[8]) {
-    const int e = (int)byte - 133;                   // 2^s / 64
+    const float unit = unit8_of(byte);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        const int q = (int)(w[i >> 2] << (24 - 8 * (i & 3))) >> 24;
-        v[i] = __builtin_amdgcn_ldexpf((float)q, e);
+        const uint32_t h = w[i >> 2];
+        v[i] = (float)(int8_t)(h >> (8 * (i & 3))) * unit;
     }
-    if (byte == 255) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = __uint_as_float(0x7FC00000u);
-    }
+}
+// Two neighbouring 4-bit values (of four pairs in a word) as bf16, exactly
+__device__ __forceinline__ uint32_t pair4_of(uint32_t w, float scale, int pair) {
+    const v2bf b = pair == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 0)
+                   : pair == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 1)
+                   : pair == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 2)
+                               : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(w, scale, 3);
+    return __builtin_bit_cast(uint32_t, b);
 }
 
 // Tiles in an order that keeps what the workgroups of one XCD (every eighth) work on at a time close together: each XCD gets a run of
@@ -215,6 +217,11 @@ sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows,
 // Implemented in sparq_mx_join.hip: out[j][k] = the sum over the parts of partial [parts][J][K], part after part, + bias[k]
 // (NULL: none), rounded to the type.
 sparq_status launch_join(const float* partial, const float* bias, void* out, int type, int64_t J, int K, int64_t ldo, int parts, hipStream_t stream);
+
+typedef __attribute__((address_space(3))) void* LdsPtr;
+// The wait instruction's operand for at most n loads and stores on their way; for that and no access to LDS.
+constexpr int vmcnt(int n) { return (n & 15) | (n >> 4) << 14 | 0x0F70; }
+constexpr int vmcnt_and_lds(int n) { return vmcnt(n) & ~0x0F00; }
 
 }  // namespace mx
 }  // namespace sparq

@@ -28,11 +28,6 @@ struct GemmParams {
 constexpr int kGemmThreads = 256;
 constexpr int kGemmMaxK = 1 << 23;       // a tile's rows stay inside 32-bit offsets
 
-typedef __attribute__((address_space(3))) void* LdsPtr;
-// The wait instruction's operand for at most n loads on their way.
-constexpr int vmcnt(int n) { return (n & 15) | (n >> 4) << 14 | 0x0F70; }
-constexpr int kNoLds = ~0x0F00;          // ... and no access to LDS
-
 // Bytes of a row of results that a wavefront turns at a time: what is left of a CU's LDS, or of half of it.
 template <int TILE> constexpr int kTurnRow = TILE == 256 ? 128 : 64;
 template <int TILE> constexpr int kGemmLds = 4 * 2 * TILE * 64 + 2 * 2 * TILE * 16 + 4 * 32 * kTurnRow<TILE>;
@@ -169,8 +164,8 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         ++load_step;
         // This step's buffer has been read, here and, past the barrier, in the other wavefronts: it takes step s + 4.  And step s + 1 is
         // there: all but the loads of steps s + 2 and s + 3 are done.  (An item's first two steps: they were waited for before it began.)
-        if (place >= 2 || s >= 4) __builtin_amdgcn_s_waitcnt(vmcnt(2 * kLoads) & kNoLds);
-        else __builtin_amdgcn_s_waitcnt(vmcnt(63) & kNoLds);
+        if (place >= 2 || s >= 4) __builtin_amdgcn_s_waitcnt(vmcnt_and_lds(2 * kLoads));
+        else __builtin_amdgcn_s_waitcnt(vmcnt_and_lds(63));
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");

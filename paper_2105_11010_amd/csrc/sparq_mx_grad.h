@@ -2,7 +2,7 @@
 #pragma once
 #include <type_traits>
 
-#include "sparq_mx_grad_kernel.h"
+#include "sparq_mx_grad_wide_kernel.h"
 
 namespace sparq {
 namespace mx {
@@ -23,13 +23,10 @@ inline sparq_status launch_grad(const GradParams& p, int parts, int tile, int dy
     return f(p, parts, tile, out, out_type, stream);
 }
 
-template <class T, class O, bool DW, int TILE>
-sparq_status launch_grad_tile(const GradParams& p, int parts, void* out, hipStream_t stream) {
-    const auto kernel = grad_kernel<T, O, DW, TILE, TILE>;
-    constexpr int lds_bytes = 2 * (kParts<T> + 1) * TILE * kGradStep * 2;
-    static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
-    static std::atomic<bool> allowed[kMaxDevices];           // the attribute is set once per device (twice at worst)
-    const int slot = current_device_slot();
+template <class O, class F>
+sparq_status launch_grad_kernel(F* kernel, int lds_bytes, std::atomic<bool> (&allowed)[kMaxDevices], const GradParams& p, int parts, void* out,
+                                hipStream_t stream) {
+    const int slot = current_device_slot();                  // the attribute is set once per device (twice at worst)
     if (!allowed[slot].load(std::memory_order_relaxed) || slot == kMaxDevices - 1) {
         if (hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, lds_bytes) != hipSuccess)
             return SPARQ_ELAUNCH;
@@ -43,13 +40,16 @@ sparq_status launch_grad_types(const GradParams& p, int parts, int tile, void* o
     sparq_status s = SPARQ_OK;
     with_type(out_type, [&](auto o) {
         typedef decltype(o) O;
+        static std::atomic<bool> allowed[2][kMaxDevices];
         if constexpr (std::is_same_v<T, __bf16>) {
-            if (tile == 256) {
-                s = launch_grad_tile<T, O, DW, 256>(p, parts, out, stream);
+            if (tile == kWideTile) {
+                s = launch_grad_kernel<O>(grad_wide_kernel<O, DW>, kWideLds, allowed[0], p, parts, out, stream);
                 return;
             }
         }
-        s = launch_grad_tile<T, O, DW, 128>(p, parts, out, stream);
+        constexpr int lds_bytes = 2 * (kParts<T> + 1) * 128 * kGradStep * 2;
+        static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
+        s = launch_grad_kernel<O>(grad_kernel<T, O, DW, 128, 128>, lds_bytes, allowed[1], p, parts, out, stream);
     });
     return s;
 }

@@ -187,12 +187,7 @@ struct CodedTile {
             uint32_t pair[8];                                // columns 2 q (low) and 2 q + 1 of a row
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float s = scale_value(scale[i]);
-                const v2bf b = q == 0   ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 0)
-                               : q == 1 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 1)
-                               : q == 2 ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 2)
-                                        : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4((uint32_t)raw[i], s, 3);
-                pair[i] = scale[i] == 255 ? 0x7FC07FC0u : __builtin_bit_cast(uint32_t, b);
+                pair[i] = pair4_of(raw[i], scale_operand(scale[i]), q);
             }
 #pragma unroll
             for (int a = 0; a < 4; ++a) {
@@ -206,7 +201,7 @@ struct CodedTile {
                 uint32_t w;
                 if constexpr (N == 8) w = raw[i][q >> 1];
                 else w = raw[i];
-                const float s = __builtin_amdgcn_ldexpf(scale[i] == 255 ? __uint_as_float(0x7FC00000u) : 1.0f, (int)scale[i] - 133);
+                const float s = unit8_of(scale[i]);
                 v[i][0] = (float)(int8_t)(w >> (16 * (q & 1))) * s;
                 v[i][1] = (float)(int8_t)(w >> (16 * (q & 1) + 8)) * s;
             }
@@ -221,40 +216,25 @@ struct CodedTile {
     }
 };
 
-template <class T, class O, bool DW, int TJ, int TK>
-__global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
-    constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
-    extern __shared__ v4u lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = lane & 31, g = lane >> 5;
-    const int wj = (wave >> 1) * (TJ / 2), wk = (wave & 1) * (TK / 2);
-    uint32_t tj, tk;
-    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
-    const int64_t j0 = (int64_t)tj * TJ;
-    const int k0 = (int)tk * TK;
-    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
-    const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all;
-    // steps before this one are whole
-    const int64_t whole = DW && p.J < TJ / 32 ? 0 : p.R / kGradStep, s_fast = whole < s_end ? whole : s_end;
-
+// What a wavefront of four multiplies: a quarter of a tile, FK x FJ results of 32 x 32.
+template <int P, int TJ, int TK>
+struct Products {
+    static constexpr int FJ = TJ / 64, FK = TK / 64;
     v16f acc[FK][FJ];
-#pragma unroll
-    for (int a = 0; a < FK; ++a)
-#pragma unroll
-        for (int b = 0; b < FJ; ++b) acc[a][b] = v16f{};
+    int wj, wk;                                              // the wavefront's first row and column of the tile
 
-    constexpr int kDyParts = TJ / 32, kCodedParts = TK / 64;
-    typedef DyTile<T, TJ, DW> Dy;
-    typedef CodedTile<BITS, TK> Coded;
-    // quarter q of a step into a tile
-    auto convert = [&](const Dy& dy, const Coded& coded, v4u* tile, int q) __attribute__((always_inline)) {
+    __device__ __forceinline__ Products() {
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        wj = (wave >> 1) * (TJ / 2);
+        wk = (wave & 1) * (TK / 2);
 #pragma unroll
-        for (int i = 0; i < kDyParts / 4; ++i) dy.store(tile, q * (kDyParts / 4) + i);
-        if (kCodedParts >= 4 || (q & 1) == 0) coded.store(tile + P * TJ * 8, kCodedParts >= 4 ? q : q >> 1);
-    };
-    // products of quarter q of a tile
-    auto multiply = [&](const v4u* tile, int q) __attribute__((always_inline)) {
+        for (int a = 0; a < FK; ++a)
+#pragma unroll
+            for (int b = 0; b < FJ; ++b) acc[a][b] = v16f{};
+    }
+    // products of quarter q of a tile in LDS
+    __device__ __forceinline__ void multiply(const v4u* tile, int q) {
+        const int c = threadIdx.x & 31, g = (threadIdx.x >> 5) & 1;
         const v4u* tile_k = tile + P * TJ * 8;
         v8bf a[FK], b[P][FJ];
 #pragma unroll
@@ -269,7 +249,52 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
             for (int x = 0; x < FK; ++x)
 #pragma unroll
                 for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[i][y], acc[x][y], 0, 0, 0);
-    };
+    }
+};
+// quarter q of a step into a tile
+template <class Dy, class Coded, int TJ, int TK>
+__device__ __forceinline__ void convert(const Dy& dy, const Coded& coded, v4u* tile, int q) {
+    constexpr int kDyParts = TJ / 32, kCodedParts = TK / 64;
+#pragma unroll
+    for (int i = 0; i < kDyParts / 4; ++i) dy.store(tile, q * (kDyParts / 4) + i);
+    if (kCodedParts >= 4 || (q & 1) == 0) coded.store(tile + Dy::P * TJ * 8, kCodedParts >= 4 ? q : q >> 1);
+}
+// Steps that are not whole, or whose loads would not be: checked loads, one step after the other.
+template <class T, bool DW, int TJ, int TK>
+__device__ __forceinline__ void multiply_rest(Products<kParts<T>, TJ, TK>& products, const GradParams& p, v4u* lds, int64_t j0, int k0, int64_t s, int64_t s_end) {
+    typedef DyTile<T, TJ, DW> Dy;
+    typedef CodedTile<DW ? 8 : 4, TK> Coded;
+    for (; s < s_end; ++s) {
+        Dy dy;
+        Coded coded;
+        dy.template load<false>(p, j0, s * kGradStep);
+        coded.template load<false>(p, k0, s * kGradStep);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) convert<Dy, Coded, TJ, TK>(dy, coded, lds, q);
+        __syncthreads();
+#pragma unroll
+        for (int q = 0; q < 4; ++q) products.multiply(lds, q);
+    }
+}
+
+template <class T, class O, bool DW, int TJ, int TK>
+__global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
+    constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
+    extern __shared__ v4u lds[];
+    uint32_t tj, tk;
+    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
+    const int64_t j0 = (int64_t)tj * TJ;
+    const int k0 = (int)tk * TK;
+    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
+    const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all;
+    // steps before this one are whole
+    const int64_t whole = DW && p.J < TJ / 32 ? 0 : p.R / kGradStep, s_fast = whole < s_end ? whole : s_end;
+    typedef DyTile<T, TJ, DW> Dy;
+    typedef CodedTile<BITS, TK> Coded;
+    Products<P, TJ, TK> products;
 
     if (s_begin < s_fast) {
         Dy dy[2];
@@ -283,14 +308,14 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
             load(s + 2, set);
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                multiply(lds + set * kUnits, q);
-                convert(dy[set ^ 1], coded[set ^ 1], lds + (set ^ 1) * kUnits, q);
+                products.multiply(lds + set * kUnits, q);
+                convert<Dy, Coded, TJ, TK>(dy[set ^ 1], coded[set ^ 1], lds + (set ^ 1) * kUnits, q);
             }
             __syncthreads();
         };
         load(s_begin, 0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) convert(dy[0], coded[0], lds, q);
+        for (int q = 0; q < 4; ++q) convert<Dy, Coded, TJ, TK>(dy[0], coded[0], lds, q);
         load(s_begin + 1, 1);
         __syncthreads();
         for (int64_t s = s_begin; s < s_fast; s += 2) {
@@ -298,24 +323,12 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
             if (s + 1 < s_fast) step(s + 1, 1);
         }
     }
-    // what is left: the last products where their number is no multiple of a step
-    for (int64_t s = s_begin < s_fast ? s_fast : s_begin; s < s_end; ++s) {
-        Dy dy;
-        Coded coded;
-        dy.template load<false>(p, j0, s * kGradStep);
-        coded.template load<false>(p, k0, s * kGradStep);
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) convert(dy, coded, lds, q);
-        __syncthreads();
-#pragma unroll
-        for (int q = 0; q < 4; ++q) multiply(lds, q);
-    }
+    multiply_rest<T, DW, TJ, TK>(products, p, lds, j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, FK, FJ, 128>(acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none,
-                             reinterpret_cast<uint8_t*>(lds) + wave * 4096);
+    store_results<O, FK, FJ, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + products.wj, p.J, k0 + products.wk, p.K, none,
+                                  reinterpret_cast<uint8_t*>(lds) + (threadIdx.x >> 6) * 4096);
 #endif
 }
 

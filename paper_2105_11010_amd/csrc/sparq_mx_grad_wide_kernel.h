@@ -1,0 +1,215 @@
+// The gradients of large layers in bf16: 256 x 256 results a workgroup.
+// out[j][k] = sum_r dy(j, r) V[r][k] as in sparq_mx_grad_kernel.h.  V's rows are decoded as they lie, eight values of a row a thread, and dy's are
+// copied; the matrix instruction's operands, eight neighbouring r of one column, come out of LDS by reads that turn 4 x 16 values (V, and dy
+// where r is its row).  Sixteen lanes read four rows, 32 bytes each, at a time: a row's 16-byte units are permuted by the row so that four
+// neighbouring rows lie in different quarters of the banks.
+// A step is 64 r, four quarters of sixteen matrix instructions; one wavefront a SIMD has nobody else to fill the time an
+// instruction runs, so what goes between them is laid out here: the next quarter's reads, and of V and of dy two rows each, written to the
+// next step's tiles, and the request for their successors.  One barrier a step, before the last quarter: by then the step's tiles have been
+// read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, 392 us where
+// this takes TIME.)
+#pragma once
+#include "sparq_mx_grad_kernel.h"
+
+namespace sparq {
+namespace mx {
+
+constexpr int kWideTile = 256;
+constexpr int kWideBytes = kGradStep * kWideTile * 2;        // of one side's tile
+constexpr int kWideLds = 4 * kWideBytes;
+
+// A call this kernel is for: whole words of dy, rows whose distances fit the loads' 32-bit offsets, and no run of eight columns (DW) that the
+// last column cuts.
+template <bool DW>
+inline bool grad_wide_fits(const void* dy, int64_t lddy, int64_t J, int64_t code_pitch) {
+    return aligned(dy, 4) && lddy % 2 == 0 && lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J % 8 == 0);
+}
+
+template <class O, bool DW>
+__global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+    typedef typename Word<DW ? 8 : 4>::Type Raw;
+    typedef short v4s __attribute__((ext_vector_type(4)));
+    extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
+    uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * kWideBytes;
+    const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
+    uint32_t tj, tk;
+    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
+    const int64_t j0 = (int64_t)tj * kWideTile;
+    const int k0 = (int)tk * kWideTile;
+    const int s_begin = (int)blockIdx.y * p.steps_per_part, s_all = (int)((p.R + kGradStep - 1) / kGradStep), s_whole = (int)(p.R / kGradStep);
+    const int s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = s_whole < s_end ? s_whole : s_end;
+    Products<1, kWideTile, kWideTile> products;
+    const int wj = products.wj, wk = products.wk;
+
+    if (s_begin < s_fast) {
+        // ---- dy: a thread has eight 16-byte units: of rows 8 i + t / 32 (DW) or of rows 32 i + t / 8, 64 r each
+        v4u kept[8];
+        uint32_t dy_at[DW ? 1 : 8];
+        const uint16_t* dy_base;
+        uint32_t dy_step;
+        if constexpr (DW) {
+            int64_t j = j0 + 8 * (t & 31);
+            j = j < p.J ? j : p.J - 8;                       // (columns past the last one make results that are not stored)
+            dy_at[0] = (uint32_t)(((t >> 5) * p.lddy + (j - j0)) * 2);
+            dy_base = static_cast<const uint16_t*>(p.dy) + j0;
+            dy_step = (uint32_t)(kGradStep * p.lddy * 2);
+        } else {
+            const int64_t last = p.J - 1 - j0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int row = 32 * i + (t >> 3), from = row < last ? row : (int)last;
+                dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * 2);
+            }
+            dy_base = static_cast<const uint16_t*>(p.dy) + j0 * p.lddy;
+            dy_step = kGradStep * 2;
+        }
+        const auto dy_buffer = [&](int s) __attribute__((always_inline)) {
+            s = s < s_fast ? s : s_fast - 1;                 // (past the end: the last step again, for a tile nobody reads)
+            return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const uint8_t*>(dy_base) + (int64_t)s * dy_step), 0, 0x7FFFFFFF, 0x00020000);
+        };
+        auto load_dy = [&](const __amdgpu_buffer_rsrc_t& from, int i) __attribute__((always_inline)) {
+            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(from, dy_at[DW ? 0 : i], DW ? (int)(8 * i * p.lddy * 2) : 0, 0);
+        };
+        auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
+            if constexpr (DW) *reinterpret_cast<v4u*>(tile + (8 * i + (t >> 5)) * 512 + (((t & 31) ^ (((t >> 5) & 3) << 2)) << 4)) = kept[i];
+            else *reinterpret_cast<v4u*>(tile + 16 * unit_at(32 * i + (t >> 3), t & 7)) = kept[i];
+        };
+        // ---- V: a thread has eight rows of eight values
+        Raw raw[8];
+        uint32_t scale[8];
+        int k = k0 + 8 * (t & 31);
+        k = k < p.K128 ? k : p.K128 - 8;
+        const uint32_t v_at = (uint32_t)((t >> 5) * 8 * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)((t >> 5) * 8 * p.scale_pitch + (k >> 5));
+        const auto v_buffer = [&](const uint8_t* base, int64_t pitch, int s) __attribute__((always_inline)) {
+            s = s < s_fast ? s : s_fast - 1;
+            return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)s * kGradStep * pitch), 0, 0x7FFFFFFF, 0x00020000);
+        };
+        auto load_v = [&](const __amdgpu_buffer_rsrc_t& codes, const __amdgpu_buffer_rsrc_t& scales, int i) __attribute__((always_inline)) {
+            if constexpr (DW) raw[i] = __builtin_amdgcn_raw_buffer_load_b64(codes, v_at, (int)(i * p.code_pitch), 0);
+            else raw[i] = __builtin_amdgcn_raw_buffer_load_b32(codes, v_at, (int)(i * p.code_pitch), 0);
+            scale[i] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_at, (int)(i * p.scale_pitch), 0);
+        };
+        const int v_to = (t >> 5) * 8 * 512;
+        v4u decoded;
+        float unit;
+        // values 2 q and 2 q + 1 of row i
+        auto decode = [&](int i, int q) __attribute__((always_inline)) {
+            if (q == 0) unit = DW ? unit8_of(scale[i]) : scale_operand(scale[i]);
+            if constexpr (DW) {
+                const uint32_t w = raw[i][q >> 1] >> (16 * (q & 1));
+                decoded[q] = pack_bf16((float)(int8_t)w * unit, (float)(int8_t)(w >> 8) * unit);
+            } else {
+                decoded[q] = pair4_of(raw[i], unit, q);
+            }
+        };
+        auto write_v = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
+            *reinterpret_cast<v4u*>(tile + v_to + i * 512 + (((t & 31) ^ ((i & 3) << 2)) << 4)) = decoded;
+        };
+        // ---- operands: eight neighbouring r of one row or column; rows of turned tiles are 512 bytes
+        struct Operands {
+            v4u v[4], dy[4];
+        };
+        Operands set[2];
+        const int rr = (lane >> 2) & 3, turn_row = (8 * g + rr) * 512 + ((lane & 1) << 3);
+        // 16-byte unit of the lane's piece of fragment f, whose first column is a multiple of 128 + 32 f
+        const auto turn_unit = [&](int first, int f) __attribute__((always_inline)) {
+            return ((first / 8 + 4 * (f ^ rr) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) << 4);
+        };
+        auto read_turned = [&](v4u& to, const uint8_t* tile, int first, int f, int q, int h) __attribute__((always_inline)) {
+            typedef __attribute__((address_space(3))) v4s* P;
+            const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(tile + turn_row + turn_unit(first, f) + (16 * q + 4 * h) * 512));
+            const v2u w = __builtin_bit_cast(v2u, r);
+            to[2 * h] = w[0];
+            to[2 * h + 1] = w[1];
+        };
+        constexpr int kReads = DW ? 16 : 12;
+        // read n of a quarter's kReads, in the order the products need them: the first fragment of V, all of dy, the rest of V
+        auto read = [&](Operands& o, const uint8_t* dy_tile, const uint8_t* v_tile, int q, int n) __attribute__((always_inline)) {
+            constexpr int kDy = DW ? 8 : 4;
+            if (n < 2) read_turned(o.v[0], v_tile, wk, 0, q, n);
+            else if (n < 2 + kDy) {
+                n -= 2;
+                if constexpr (DW) read_turned(o.dy[n >> 1], dy_tile, wj, n >> 1, q, n & 1);
+                else o.dy[n] = *reinterpret_cast<const v4u*>(dy_tile + 16 * unit_at(wj + 32 * n + c, 2 * q + g));
+            } else {
+                n -= kDy;
+                read_turned(o.v[n >> 1], v_tile, wk, n >> 1, q, n & 1);
+            }
+        };
+
+        int now = 0;                                         // where this step's tiles are, kWideBytes or 0
+        // What is issued after matrix instruction i of quarter q of step s.  Between two barriers, quarters 3, 0, 1, 2, the tiles of the step
+        // after the later one's are written and those after them asked for.
+        auto between = [&](int s, int q, int i) __attribute__((always_inline)) {
+            const int part = (q + 1) & 3, row = 2 * part + (i >> 3), ahead = s + 2 + (q == 3 ? 1 : 0);
+            const int read_from = q == 3 ? now ^ kWideBytes : now, write_to = q == 3 ? now : now ^ kWideBytes;
+            for (int n = i * kReads / 16; n < (i + 1) * kReads / 16; ++n) read(set[(q + 1) & 1], lds_dy + read_from, lds_v + read_from, (q + 1) & 3, n);
+            if ((i & 1) == 0) decode(row, (i & 7) >> 1);
+            if ((i & 7) == 7) {
+                write_v(lds_v + write_to, row);
+                load_v(v_buffer(p.codes, p.code_pitch, ahead), v_buffer(p.scales, p.scale_pitch, ahead), row);
+            }
+            if ((i & 7) == 3) {
+                write_dy(lds_dy + write_to, row);
+                load_dy(dy_buffer(ahead), row);
+            }
+        };
+        auto barrier = [&]() __attribute__((always_inline)) {
+            __builtin_amdgcn_s_waitcnt(vmcnt_and_lds(63));
+            asm volatile("" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+        };
+
+        {
+            const __amdgpu_buffer_rsrc_t codes = v_buffer(p.codes, p.code_pitch, s_begin), scales = v_buffer(p.scales, p.scale_pitch, s_begin);
+            const __amdgpu_buffer_rsrc_t codes1 = v_buffer(p.codes, p.code_pitch, s_begin + 1), scales1 = v_buffer(p.scales, p.scale_pitch, s_begin + 1);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                load_v(codes, scales, i);
+                load_dy(dy_buffer(s_begin), i);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) decode(i, q);
+                write_v(lds_v, i);
+                load_v(codes1, scales1, i);
+                write_dy(lds_dy, i);
+                load_dy(dy_buffer(s_begin + 1), i);
+            }
+        }
+        barrier();
+        // as if the last quarter of a step before the first
+        now = kWideBytes;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) between(s_begin - 1, 3, i);
+        for (int s = s_begin; s < s_fast; ++s) {
+            now ^= kWideBytes;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                if (q == 3) barrier();                       // the next step's tiles are written, this step's read
+                const Operands& o = set[q & 1];
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int y = 0; y < 4; ++y) {
+                        products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[y]),
+                                                                                     products.acc[x][y], 0, 0, 0);
+                        between(s, q, 4 * x + y);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+            }
+        }
+    }
+    multiply_rest<__bf16, DW, kWideTile, kWideTile>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
+
+    __syncthreads();
+    const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
+    store_results<O, 4, 4, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
+#endif
+}
+
+}  // namespace mx
+}  // namespace sparq

@@ -29,6 +29,9 @@ def sq():
     return sq_
 
 
+R_quantised = R.quantised
+
+
 def rng(*seed):
     return np.random.default_rng([20210511, *seed])
 
@@ -180,6 +183,13 @@ def test_product(sq, M, N, K, t, bias, pad, at):
     guard(ws, view)
 
 
+# many results, so that the largest tiles are used: whole ones, cut ones, and reductions that end inside a step or before the first ends
+@pytest.mark.parametrize("M,N,K", [(4100, 3300, 100), (4096, 3328, 640), (3333, 4001, 1500)])
+@pytest.mark.parametrize("t,bias", [("bf16", True), ("f32", False)])
+def test_product_in_large_tiles(sq, M, N, K, t, bias):
+    test_product(sq, M, N, K, t, bias, 0, 0)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 40, 300), (40, 70, 300), (300, 300, 700)])
 def test_product_of_what_is_not_finite(sq, M, N, K):
     """A NaN or an infinity makes its row (of x) or column (of w) NaN and nothing else."""
@@ -225,6 +235,25 @@ def test_product_gradients(sq, M, N, K, t, o, pad, at):
     close(db[:N].double().cpu().numpy(), dy.sum(0), (M + 2) * u * np.abs(dy).sum(0), "f32")
     assert bool((db[N:] == 9).all())
     guard(ws, view)
+
+
+@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400)])
+@pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2)])
+def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at):
+    """dx [J][K] over R outputs, dw [J][K] over R rows."""
+    g = rng(13, J, R, K)
+    V, d = values(g, R, K, "bf16"), values(g, J, R, "bf16", 0.1)
+    for bits in (4, 8):
+        ref = R_quantised(V, bits)
+        out = Result(J, K, o, pad, at)
+        if bits == 4:
+            ws, view = workspace(sq.sparq_mx_linear_dx_workspace_bytes(J, R, K))
+            sq.sparq_mx_linear_dx(matrix(d, "bf16", pad, at), *stored(sq, V, 4), out.view, workspace=view)
+        else:
+            ws, view = workspace(sq.sparq_mx_linear_dw_workspace_bytes(R, J, K))
+            sq.sparq_mx_linear_dw(matrix(d.T, "bf16", pad, at), *stored(sq, V, 8), out.view, workspace=view)
+        close(out.get(), d @ ref, 2 * (R + 2) * u * (np.abs(d) @ np.abs(ref)), o)
+        guard(ws, view)
 
 
 def test_product_gradients_are_the_differences(sq):
