@@ -9,6 +9,8 @@
 // read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, 392 us where
 // this takes TIME.)
 #pragma once
+#include <type_traits>
+
 #include "sparq_mx_grad_kernel.h"
 
 namespace sparq {
@@ -28,7 +30,6 @@ inline bool grad_wide_fits(const void* dy, int64_t lddy, int64_t J, int64_t code
 template <class O, bool DW>
 __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    typedef typename Word<DW ? 8 : 4>::Type Raw;
     typedef short v4s __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
     uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * kWideBytes;
@@ -46,14 +47,10 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
         // ---- dy: a thread has eight 16-byte units: of rows 8 i + t / 32 (DW) or of rows 32 i + t / 8, 64 r each
         v4u kept[8];
         uint32_t dy_at[DW ? 1 : 8];
-        const uint16_t* dy_base;
-        uint32_t dy_step;
         if constexpr (DW) {
             int64_t j = j0 + 8 * (t & 31);
             j = j < p.J ? j : p.J - 8;                       // (columns past the last one make results that are not stored)
             dy_at[0] = (uint32_t)(((t >> 5) * p.lddy + (j - j0)) * 2);
-            dy_base = static_cast<const uint16_t*>(p.dy) + j0;
-            dy_step = (uint32_t)(kGradStep * p.lddy * 2);
         } else {
             const int64_t last = p.J - 1 - j0;
 #pragma unroll
@@ -61,64 +58,74 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
                 const int row = 32 * i + (t >> 3), from = row < last ? row : (int)last;
                 dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * 2);
             }
-            dy_base = static_cast<const uint16_t*>(p.dy) + j0 * p.lddy;
-            dy_step = kGradStep * 2;
         }
-        const auto dy_buffer = [&](int s) __attribute__((always_inline)) {
-            s = s < s_fast ? s : s_fast - 1;                 // (past the end: the last step again, for a tile nobody reads)
-            return __builtin_amdgcn_make_buffer_rsrc((void*)(reinterpret_cast<const uint8_t*>(dy_base) + (int64_t)s * dy_step), 0, 0x7FFFFFFF, 0x00020000);
+        // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32
+        constexpr int kWords = DW ? 8 : 4;
+        uint32_t raw[2][kWords], scale[2];
+        const int v_row = 4 * (lane >> 3) + wave;
+        int k = k0 + 32 * (lane & 7);
+        k = k < p.K128 ? k : p.K128 - 32;
+        const uint32_t v_at = (uint32_t)(v_row * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)(v_row * p.scale_pitch + (k >> 5));
+
+        // Where the next step to be asked for lies.  Past the last one it stays there, for tiles nobody reads.
+        const uint8_t* dy_from = static_cast<const uint8_t*>(p.dy) + (DW ? j0 + s_begin * (kGradStep * p.lddy) : j0 * p.lddy + (int64_t)s_begin * kGradStep) * 2;
+        const uint8_t *codes_from = p.codes + (int64_t)s_begin * kGradStep * p.code_pitch, *scales_from = p.scales + (int64_t)s_begin * kGradStep * p.scale_pitch;
+        const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * 2) : kGradStep * 2, codes_step = (uint32_t)(kGradStep * p.code_pitch);
+        const uint32_t scales_step = (uint32_t)(kGradStep * p.scale_pitch);
+        int left = s_fast - s_begin - 1;
+        auto advance = [&]() __attribute__((always_inline)) {
+            dy_from += left > 0 ? dy_step : 0;
+            codes_from += left > 0 ? codes_step : 0;
+            scales_from += left > 0 ? scales_step : 0;
+            --left;
         };
-        auto load_dy = [&](const __amdgpu_buffer_rsrc_t& from, int i) __attribute__((always_inline)) {
-            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(from, dy_at[DW ? 0 : i], DW ? (int)(8 * i * p.lddy * 2) : 0, 0);
+        const auto buffer = [](const uint8_t* from) __attribute__((always_inline)) { return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000); };
+        auto load_dy = [&](int i) __attribute__((always_inline)) {
+            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], DW ? (int)(8 * i * p.lddy * 2) : 0, 0);
+        };
+        auto load_v = [&](int run) __attribute__((always_inline)) {
+#pragma unroll
+            for (int h = 0; h < kWords / 4; ++h) {
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(codes_from), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) raw[run][4 * h + e] = w[e];
+            }
+            scale[run] = __builtin_amdgcn_raw_buffer_load_b8(buffer(scales_from), scale_at, (int)(32 * run * p.scale_pitch), 0);
+        };
+        // A tile's row of 512 bytes is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
+        const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
+            return row * 512 + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
         };
         auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
-            if constexpr (DW) *reinterpret_cast<v4u*>(tile + (8 * i + (t >> 5)) * 512 + (((t & 31) ^ (((t >> 5) & 3) << 2)) << 4)) = kept[i];
+            if constexpr (DW) *reinterpret_cast<v4u*>(tile + permuted(8 * i + (t >> 5), t & 31)) = kept[i];
             else *reinterpret_cast<v4u*>(tile + 16 * unit_at(32 * i + (t >> 3), t & 7)) = kept[i];
         };
-        // ---- V: a thread has eight rows of eight values
-        Raw raw[8];
-        uint32_t scale[8];
-        int k = k0 + 8 * (t & 31);
-        k = k < p.K128 ? k : p.K128 - 8;
-        const uint32_t v_at = (uint32_t)((t >> 5) * 8 * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)((t >> 5) * 8 * p.scale_pitch + (k >> 5));
-        const auto v_buffer = [&](const uint8_t* base, int64_t pitch, int s) __attribute__((always_inline)) {
-            s = s < s_fast ? s : s_fast - 1;
-            return __builtin_amdgcn_make_buffer_rsrc((void*)(base + (int64_t)s * kGradStep * pitch), 0, 0x7FFFFFFF, 0x00020000);
-        };
-        auto load_v = [&](const __amdgpu_buffer_rsrc_t& codes, const __amdgpu_buffer_rsrc_t& scales, int i) __attribute__((always_inline)) {
-            if constexpr (DW) raw[i] = __builtin_amdgcn_raw_buffer_load_b64(codes, v_at, (int)(i * p.code_pitch), 0);
-            else raw[i] = __builtin_amdgcn_raw_buffer_load_b32(codes, v_at, (int)(i * p.code_pitch), 0);
-            scale[i] = __builtin_amdgcn_raw_buffer_load_b8(scales, scale_at, (int)(i * p.scale_pitch), 0);
-        };
-        const int v_to = (t >> 5) * 8 * 512;
+        // values 2 e and 2 e + 1 of the eight of piece 0..7 (two runs of four)
         v4u decoded;
         float unit;
-        // values 2 q and 2 q + 1 of row i
-        auto decode = [&](int i, int q) __attribute__((always_inline)) {
-            if (q == 0) unit = DW ? unit8_of(scale[i]) : scale_operand(scale[i]);
+        auto decode = [&](int piece, int e) __attribute__((always_inline)) {
+            const int run = piece >> 2, at = piece & 3;
+            if (at == 0 && e == 0) unit = DW ? unit8_of(scale[run]) : scale_operand(scale[run]);
             if constexpr (DW) {
-                const uint32_t w = raw[i][q >> 1] >> (16 * (q & 1));
-                decoded[q] = pack_bf16((float)(int8_t)w * unit, (float)(int8_t)(w >> 8) * unit);
+                const uint32_t w = raw[run][2 * at + (e >> 1)] >> (16 * (e & 1));
+                decoded[e] = pack_bf16((float)(int8_t)w * unit, (float)(int8_t)(w >> 8) * unit);
             } else {
-                decoded[q] = pair4_of(raw[i], unit, q);
+                decoded[e] = pair4_of(raw[run][at], unit, e);
             }
         };
-        auto write_v = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
-            *reinterpret_cast<v4u*>(tile + v_to + i * 512 + (((t & 31) ^ ((i & 3) << 2)) << 4)) = decoded;
+        auto write_v = [&](uint8_t* tile, int piece) __attribute__((always_inline)) {
+            *reinterpret_cast<v4u*>(tile + permuted(v_row + 32 * (piece >> 2), 4 * (lane & 7) + (piece & 3))) = decoded;
         };
-        // ---- operands: eight neighbouring r of one row or column; rows of turned tiles are 512 bytes
+        // ---- operands: eight neighbouring r of one row or column
         struct Operands {
             v4u v[4], dy[4];
         };
         Operands set[2];
-        const int rr = (lane >> 2) & 3, turn_row = (8 * g + rr) * 512 + ((lane & 1) << 3);
-        // 16-byte unit of the lane's piece of fragment f, whose first column is a multiple of 128 + 32 f
-        const auto turn_unit = [&](int first, int f) __attribute__((always_inline)) {
-            return ((first / 8 + 4 * (f ^ rr) + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1)) << 4);
-        };
+        // A lane's half of operand f: r = 16 q + 8 g + 4 h + (lane / 4) % 4, columns first + 32 f + 16 ((lane / 16) % 2) + 4 (lane % 4) and on.
         auto read_turned = [&](v4u& to, const uint8_t* tile, int first, int f, int q, int h) __attribute__((always_inline)) {
             typedef __attribute__((address_space(3))) v4s* P;
-            const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(tile + turn_row + turn_unit(first, f) + (16 * q + 4 * h) * 512));
+            const int row = 8 * g + 4 * h + ((lane >> 2) & 3), chunk = first / 8 + 4 * f + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
+            const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(tile + permuted(row, chunk) + ((lane & 1) << 3) + q * 16 * 512));
             const v2u w = __builtin_bit_cast(v2u, r);
             to[2 * h] = w[0];
             to[2 * h + 1] = w[1];
@@ -138,21 +145,22 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
             }
         };
 
-        int now = 0;                                         // where this step's tiles are, kWideBytes or 0
-        // What is issued after matrix instruction i of quarter q of step s.  Between two barriers, quarters 3, 0, 1, 2, the tiles of the step
-        // after the later one's are written and those after them asked for.
-        auto between = [&](int s, int q, int i) __attribute__((always_inline)) {
-            const int part = (q + 1) & 3, row = 2 * part + (i >> 3), ahead = s + 2 + (q == 3 ? 1 : 0);
+        // What is issued after matrix instruction i of quarter q of a step whose tiles are the first or second of each side.  Between two
+        // barriers, quarters 3, 0, 1, 2, the tiles of the step after the later one's are written and those after them asked for.
+        auto between = [&](auto now_, int q, int i) __attribute__((always_inline)) {
+            constexpr int now = decltype(now_)::value * kWideBytes;
+            const int part = (q + 1) & 3, piece = 2 * part + (i >> 3);
+            if (q == 3 && i == 0) advance();
             const int read_from = q == 3 ? now ^ kWideBytes : now, write_to = q == 3 ? now : now ^ kWideBytes;
             for (int n = i * kReads / 16; n < (i + 1) * kReads / 16; ++n) read(set[(q + 1) & 1], lds_dy + read_from, lds_v + read_from, (q + 1) & 3, n);
-            if ((i & 1) == 0) decode(row, (i & 7) >> 1);
+            if ((i & 1) == 0) decode(piece, (i & 7) >> 1);
             if ((i & 7) == 7) {
-                write_v(lds_v + write_to, row);
-                load_v(v_buffer(p.codes, p.code_pitch, ahead), v_buffer(p.scales, p.scale_pitch, ahead), row);
+                write_v(lds_v + write_to, piece);
+                if ((piece & 3) == 3) load_v(piece >> 2);
             }
             if ((i & 7) == 3) {
-                write_dy(lds_dy + write_to, row);
-                load_dy(dy_buffer(ahead), row);
+                write_dy(lds_dy + write_to, piece);
+                load_dy(piece);
             }
         };
         auto barrier = [&]() __attribute__((always_inline)) {
@@ -161,32 +169,7 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-
-        {
-            const __amdgpu_buffer_rsrc_t codes = v_buffer(p.codes, p.code_pitch, s_begin), scales = v_buffer(p.scales, p.scale_pitch, s_begin);
-            const __amdgpu_buffer_rsrc_t codes1 = v_buffer(p.codes, p.code_pitch, s_begin + 1), scales1 = v_buffer(p.scales, p.scale_pitch, s_begin + 1);
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                load_v(codes, scales, i);
-                load_dy(dy_buffer(s_begin), i);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) decode(i, q);
-                write_v(lds_v, i);
-                load_v(codes1, scales1, i);
-                write_dy(lds_dy, i);
-                load_dy(dy_buffer(s_begin + 1), i);
-            }
-        }
-        barrier();
-        // as if the last quarter of a step before the first
-        now = kWideBytes;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) between(s_begin - 1, 3, i);
-        for (int s = s_begin; s < s_fast; ++s) {
-            now ^= kWideBytes;
+        auto step = [&](auto now) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 if (q == 3) barrier();                       // the next step's tiles are written, this step's read
@@ -197,10 +180,33 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
                     for (int y = 0; y < 4; ++y) {
                         products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[y]),
                                                                                      products.acc[x][y], 0, 0, 0);
-                        between(s, q, 4 * x + y);
+                        between(now, q, 4 * x + y);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
+        };
+
+#pragma unroll
+        for (int i = 0; i < 8; ++i) load_dy(i);
+        load_v(0);
+        load_v(1);
+        advance();
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) decode(i, e);
+            write_v(lds_v, i);
+            if ((i & 3) == 3) load_v(i >> 2);
+            write_dy(lds_dy, i);
+            load_dy(i);
+        }
+        barrier();
+        // as if the last quarter of a step before the first
+#pragma unroll
+        for (int i = 0; i < 16; ++i) between(std::integral_constant<int, 1>{}, 3, i);
+        for (int s = s_begin; s < s_fast; s += 2) {
+            step(std::integral_constant<int, 0>{});
+            if (s + 1 < s_fast) step(std::integral_constant<int, 1>{});
         }
     }
     multiply_rest<__bf16, DW, kWideTile, kWideTile>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
