@@ -87,6 +87,34 @@ __device__ __forceinline__ void load_upto8(const T* p, int n, float (&v)[8]) {
     }
 }
 
+// Eight neighbouring elements as they lie in memory: what is on its way while something else is computed.
+template <class T>
+struct Raw8 {
+    uint32_t w[2 * sizeof(T)];
+};
+template <class T>
+__device__ __forceinline__ void load_raw(const T* p, int n, Raw8<T>& r) {
+    if (n >= 8) {
+        __builtin_memcpy(&r, p, sizeof(r));
+    } else {
+        T v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.0f;
+        __builtin_memcpy(&r, v, sizeof(r));
+    }
+}
+template <class T>
+__device__ __forceinline__ void values_of(const Raw8<T>& r, float (&v)[8]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if constexpr (sizeof(T) == 4) v[i] = __uint_as_float(r.w[i]);
+        else {
+            const uint16_t h = (uint16_t)(r.w[i >> 1] >> (16 * (i & 1)));
+            v[i] = (float)__builtin_bit_cast(T, h);
+        }
+    }
+}
+
 // Rounded to nearest even by the conversion instructions.
 __device__ __forceinline__ uint32_t pack2(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b}); }
 __device__ __forceinline__ uint32_t pack2(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, v2h{(_Float16)a, (_Float16)b}); }

@@ -15,10 +15,19 @@ struct NormParams {
     float eps, inv_K;
 };
 
+// The wavefront's sum in every lane: within rows of sixteen lanes by moves, between them by swaps, none through LDS.
 __device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-    for (int off = 32; off > 0; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
+    const auto moved = [](float x, auto control) __attribute__((always_inline)) {
+        return __uint_as_float((uint32_t)__builtin_amdgcn_mov_dpp((int)__float_as_uint(x), decltype(control)::value, 0xF, 0xF, true));
+    };
+    v += moved(v, std::integral_constant<int, 0xB1>{});      // lane ^ 1
+    v += moved(v, std::integral_constant<int, 0x4E>{});      // lane ^ 2
+    v += moved(v, std::integral_constant<int, 0x141>{});     // the other four of eight
+    v += moved(v, std::integral_constant<int, 0x140>{});     // the other eight of sixteen
+    const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = __uint_as_float(a[0]) + __uint_as_float(a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    return __uint_as_float(b[0]) + __uint_as_float(b[1]);
 }
 // Sum over the wavefronts that share a row.  Two buffers in turn: a wavefront may write the next sum while others still
 // read this one, but not the one after that before they have passed the barrier between.
@@ -35,80 +44,139 @@ __device__ __forceinline__ float row_sum(float v, float* shared, int& turn) {
     for (int i = 1; i < WAVES; ++i) s += at[i];
     return s;
 }
-__device__ __forceinline__ void load_upto8_f32(const float* p, int n, float (&v)[8]) {
-    if (n > 0) load_upto8(p, n, v);
+// A lane's eight values of a row in registers, loaded without a branch: from + 0..7, the last eight of the row where its own would reach past
+// the end.  WHOLE: rows of whole eights; else the first `skip` of them are the lane's before it's.
+struct Place {
+    int col, from, skip;
+    bool inside;
+};
+template <bool WHOLE>
+__device__ __forceinline__ Place place_of(int col, int K) {
+    Place p;
+    p.col = col;
+    p.inside = col < K;
+    p.from = col < K - 8 ? col : K - 8;
+    p.skip = WHOLE || !p.inside ? 0 : col - p.from;
+    return p;
+}
+// own(i): element i is the lane's
+template <bool WHOLE>
+__device__ __forceinline__ bool own(const Place& p, int i) { return p.inside && (WHOLE || i >= p.skip); }
+template <bool WHOLE, class T>
+__device__ __forceinline__ void store_own(T* row, const Place& p, const float (&v)[8]) {
+    if (!p.inside) return;
+    if (WHOLE || p.skip == 0) store8(row + p.from, v);
     else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        for (int i = 0; i < 8; ++i)
+            if (i >= p.skip) row[p.from + i] = (T)v[i];
     }
 }
 
-// WAVES wavefronts take a row, CHUNKS x 8 values a lane, which stay in registers from the load to the result: one pass over
-// memory, the mean first and the squares of what differs from it second.  CHUNKS 0: rows of any length, read three times.
-template <class T, int WAVES, int CHUNKS>
+// WAVES wavefronts take a row of at least eight, CHUNKS x 8 values a lane, which stay in registers from the load to the result: one
+// pass over memory, the mean first and the squares of what differs from it second.
+template <class T, int WAVES, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
                                                         float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
                                                         uint8_t* __restrict__ scales, const NormParams p) {
     __shared__ float shared[2 * WAVES];
-    constexpr int kPerBlock = kWaves / WAVES, kSpan = WAVES * 64 * 8;
+    constexpr int kPerBlock = kWaves / WAVES, kSpan = WAVES * 512;
     const int wave = threadIdx.x >> 6, t = threadIdx.x & (WAVES * 64 - 1), lane = threadIdx.x & 63;
     const int64_t row = (int64_t)blockIdx.x * kPerBlock + (WAVES == 1 ? wave : 0);
     if (row >= p.rows) return;                               // (whole workgroups where they share a row)
     int turn = 0;
     x += row * p.ldx;
     y += row * p.ldy;
-    const int chunks = CHUNKS ? CHUNKS : (int)((p.K + kSpan - 1) / kSpan);
-    constexpr int kHeld = CHUNKS ? CHUNKS : 1;
-    float v[kHeld][8];
-    float sum = 0.0f;
-    auto fetch = [&](int c) __attribute__((always_inline)) {
-        const int col = c * kSpan + 8 * t;
-        if (col < p.K) load_upto8(x + col, p.K - col, v[CHUNKS ? c : 0]);
-        else {
+    Raw8<T> raw[CHUNKS];
+    float v[CHUNKS][8], sum = 0.0f;
+    Place at[CHUNKS];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) v[CHUNKS ? c : 0][i] = 0.0f;
-        }
-    };
-    if constexpr (CHUNKS > 0) {                              // all of them on their way before the first is used
-#pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) fetch(c);
+    for (int c = 0; c < CHUNKS; ++c) {
+        at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
+        load_raw(x + at[c].from, 8, raw[c]);
     }
-#pragma unroll kHeld
-    for (int c = 0; c < chunks; ++c) {
-        if constexpr (CHUNKS == 0) fetch(c);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) sum += v[CHUNKS ? c : 0][i];
+    for (int c = 0; c < CHUNKS; ++c) {
+        values_of(raw[c], v[c]);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += own<WHOLE>(at[c], i) ? v[c][i] : 0.0f;
     }
     const float mean = row_sum<WAVES>(sum, shared, turn) * p.inv_K;
     float squares = 0.0f;
-#pragma unroll kHeld
-    for (int c = 0; c < chunks; ++c) {
-        if constexpr (CHUNKS == 0) fetch(c);
-        const int n = p.K - (c * kSpan + 8 * t);
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            const float d = v[CHUNKS ? c : 0][i] - mean;
-            squares += i < n ? d * d : 0.0f;
+            const float d = v[c][i] - mean;
+            squares += own<WHOLE>(at[c], i) ? d * d : 0.0f;
         }
-    }
     const float var = row_sum<WAVES>(squares, shared, turn) * p.inv_K;
     const float rstd = 1.0f / sqrtf(var + p.eps);
     if (t == 0 && mean_out) mean_out[row] = mean;
     if (t == 0 && rstd_out) rstd_out[row] = rstd;
-#pragma unroll kHeld
-    for (int c = 0; c < chunks; ++c) {
-        if constexpr (CHUNKS == 0) fetch(c);
-        const int col = c * kSpan + 8 * t, n = p.K - col;
-        float g[8], b[8], o[8];
-        load_upto8_f32(gamma + col, n, g);
-        if (beta) load_upto8_f32(beta + col, n, b);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (v[CHUNKS ? c : 0][i] - mean) * rstd * g[i] + (beta ? b[i] : 0.0f);
+    for (int c = 0; c < CHUNKS; ++c) {
+        float g[8], b[8], o[8];
+        load8(gamma + at[c].from, g);
+        if (beta) load8(beta + at[c].from, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = (v[c][i] - mean) * rstd * g[i] + (beta ? b[i] : 0.0f);
+        store_own<WHOLE>(y, at[c], o);
+        if (codes && at[c].col - 8 * lane < p.K) {           // the wavefront's 512 values begin inside the row
+            if (!WHOLE && at[c].skip) load_upto8(x + at[c].col, p.K - at[c].col, v[c]);
+            if (!at[c].inside) {
+#pragma unroll
+                for (int i = 0; i < 8; ++i) v[c][i] = 0.0f;
+            }
+            const uint32_t byte = scale8_of(block_top(v[c]));
+            const v2u w = codes8_of(v[c], byte);
+            if (at[c].col < p.K128) *reinterpret_cast<v2u*>(codes + row * p.code_pitch + at[c].col) = w;
+            if ((lane & 3) == 0) scales[row * p.scale_pitch + (at[c].col >> 5)] = (uint8_t)byte;
+        }
+    }
+}
+
+// Rows of any length, read three times.
+template <class T>
+__global__ __launch_bounds__(kThreads) void norm_long_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
+                                                             const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
+                                                             float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
+                                                             uint8_t* __restrict__ scales, const NormParams p) {
+    __shared__ float shared[2 * kWaves];
+    const int t = threadIdx.x, lane = t & 63;
+    const int64_t row = blockIdx.x;
+    int turn = 0;
+    x += row * p.ldx;
+    y += row * p.ldy;
+    float v[8], sum = 0.0f, squares = 0.0f;
+    for (int col = 8 * t; col < p.K; col += 8 * kThreads) {
+        load_upto8(x + col, p.K - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum += v[i];
+    }
+    const float mean = row_sum<kWaves>(sum, shared, turn) * p.inv_K;
+    for (int col = 8 * t; col < p.K; col += 8 * kThreads) {
+        load_upto8(x + col, p.K - col, v);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) squares += i < p.K - col ? (v[i] - mean) * (v[i] - mean) : 0.0f;
+    }
+    const float var = row_sum<kWaves>(squares, shared, turn) * p.inv_K;
+    const float rstd = 1.0f / sqrtf(var + p.eps);
+    if (t == 0 && mean_out) mean_out[row] = mean;
+    if (t == 0 && rstd_out) rstd_out[row] = rstd;
+    for (int col = 8 * t; col - 8 * lane < p.K; col += 8 * kThreads) {       // (whole wavefronts: a block is four lanes')
+        const int n = p.K - col;
+        float g[8], b[8], o[8];
+        load_upto8(x + col, n, v);
+        load_upto8(gamma + col, n, g);
+        if (beta) load_upto8(beta + col, n, b);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = (v[i] - mean) * rstd * g[i] + (beta ? b[i] : 0.0f);
         if (n > 0) store_upto8(y + col, n, o);
-        if (codes && col - 8 * lane < p.K) {                 // the wavefront's 512 values begin inside the row
-            const uint32_t byte = scale8_of(block_top(v[CHUNKS ? c : 0]));
-            const v2u w = codes8_of(v[CHUNKS ? c : 0], byte);
+        if (codes) {
+            const uint32_t byte = scale8_of(block_top(v));
+            const v2u w = codes8_of(v, byte);
             if (col < p.K128) *reinterpret_cast<v2u*>(codes + row * p.code_pitch + col) = w;
             if ((lane & 3) == 0) scales[row * p.scale_pitch + (col >> 5)] = (uint8_t)byte;
         }
@@ -123,7 +191,122 @@ struct NormGradParams {
     int32_t parts;                       // partial sums of the weights' gradients: rows part, part + parts, ...
 };
 
-// Row sums of d and d h (d = dy gamma, h = (X - mean) rstd), one wavefront a row.
+// dx, and the workgroup's share of the weights' gradients, in one pass: WAVES wavefronts take a row, CHUNKS x 8 values a lane, rows part,
+// part + parts, ..., the next row on its way while this one is summed and written.  What the workgroup's wavefronts added up is joined in
+// LDS in their order and leaves as one partial sum.
+template <class T, int WAVES, int CHUNKS, bool WHOLE>
+__global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
+                                                             const uint8_t* __restrict__ scales, const float* __restrict__ mean,
+                                                             const float* __restrict__ rstd, const float* __restrict__ gamma, T* __restrict__ dx,
+                                                             float* __restrict__ partial, const NormGradParams p) {
+    constexpr int kRows = kWaves / WAVES, kSpan = WAVES * 512;
+    __shared__ float sums[2][2][WAVES];
+    __shared__ float joined[kRows > 1 ? kRows * CHUNKS * 512 : 1];
+    const int wave = threadIdx.x >> 6, t = threadIdx.x & (WAVES * 64 - 1);
+    const int64_t first = (int64_t)blockIdx.x * kRows + (WAVES == 1 ? wave : 0), stride = (int64_t)p.parts * kRows;
+    float g[CHUNKS][8], dg[CHUNKS][8] = {}, db[CHUNKS][8] = {};
+    Place at[CHUNKS];
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
+        load8(gamma + at[c].from, g[c]);
+    }
+    struct Held {
+        Raw8<T> dy[CHUNKS];
+        v2u x[CHUNKS];
+        uint32_t scale[CHUNKS];
+        float mean, rstd;
+    };
+    auto fetch = [&](Held& h, int64_t row) __attribute__((always_inline)) {
+        row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            load_raw(dy + row * p.ldy + at[c].from, 8, h.dy[c]);
+            __builtin_memcpy(&h.x[c], codes + row * p.code_pitch + at[c].from, 8);
+            h.scale[c] = scales[row * p.scale_pitch + ((at[c].inside ? at[c].col : at[c].from) >> 5)];
+        }
+        h.mean = mean[row];
+        h.rstd = rstd[row];
+    };
+    Held held;
+    fetch(held, first);
+    int turn = 0;
+    for (int64_t row = first; row < p.rows; row += stride) {
+        float d[CHUNKS][8], h[CHUNKS][8], s1 = 0.0f, s2 = 0.0f;
+        const float mu = held.mean, r = held.rstd;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            values_of(held.dy[c], d[c]);
+            values8_of(held.x[c], held.scale[c], h[c]);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                h[c][i] = own<WHOLE>(at[c], i) ? (h[c][i] - mu) * r : 0.0f;
+                const float e = own<WHOLE>(at[c], i) ? d[c][i] * g[c][i] : 0.0f;
+                s1 += e;
+                s2 += e * h[c][i];
+            }
+        }
+        fetch(held, row + stride);
+        s1 = wave_sum(s1);
+        s2 = wave_sum(s2);
+        if constexpr (WAVES > 1) {
+            if ((threadIdx.x & 63) == 0) {
+                sums[turn][0][wave] = s1;
+                sums[turn][1][wave] = s2;
+            }
+            __syncthreads();
+            s1 = sums[turn][0][0];
+            s2 = sums[turn][1][0];
+#pragma unroll
+            for (int i = 1; i < WAVES; ++i) {
+                s1 += sums[turn][0][i];
+                s2 += sums[turn][1][i];
+            }
+            turn ^= 1;                                       // (the one after the next sum is written behind the next barrier)
+        }
+        s1 *= p.inv_K;
+        s2 *= p.inv_K;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                o[i] = r * (d[c][i] * g[c][i] - s1 - h[c][i] * s2);
+                dg[c][i] += d[c][i] * h[c][i];
+                db[c][i] += d[c][i];
+            }
+            store_own<WHOLE>(dx + row * p.ldx, at[c], o);
+        }
+    }
+    if (!partial) return;
+    float* to = partial + (int64_t)blockIdx.x * 2 * p.K;
+    if constexpr (kRows == 1) {
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            store_own<WHOLE>(to, at[c], dg[c]);
+            store_own<WHOLE>(to + p.K, at[c], db[c]);
+        }
+    } else {
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            if (which) __syncthreads();
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (own<WHOLE>(at[c], i)) joined[wave * CHUNKS * 512 + at[c].from + i] = which ? db[c][i] : dg[c][i];
+            __syncthreads();
+            for (int col = threadIdx.x; col < p.K; col += kThreads) {
+                float s = joined[col];
+#pragma unroll
+                for (int w = 1; w < kRows; ++w) s += joined[w * CHUNKS * 512 + col];
+                to[which * p.K + col] = s;
+            }
+        }
+    }
+}
+
+// Rows too long for registers, or too short: their sums of d and d h first, one wavefront a row ...
 template <class T>
 __global__ __launch_bounds__(kThreads) void norm_grad_rows_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                                   const uint8_t* __restrict__ scales, const float* __restrict__ mean,
@@ -152,7 +335,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_rows_kernel(const T* __res
     if (lane == 0) sums[row] = v2f{s1 * p.inv_K, s2 * p.inv_K};
 }
 
-// dx, and this workgroup's share of the weights' gradients: 2048 columns of rows part, part + parts, ...
+// ... then dx and the weights' shares, 2048 columns of rows part, part + parts, ... a workgroup.
 template <class T>
 __global__ __launch_bounds__(kThreads) void norm_grad_columns_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                                      const uint8_t* __restrict__ scales, const float* __restrict__ mean,
@@ -185,21 +368,36 @@ __global__ __launch_bounds__(kThreads) void norm_grad_columns_kernel(const T* __
     }
 }
 
-// The partial sums' sum, part after part.
-__global__ __launch_bounds__(kThreads) void norm_grad_join_kernel(const float* __restrict__ partial, float* __restrict__ dgamma,
-                                                                  float* __restrict__ dbeta, int K, int parts) {
-    const int c = blockIdx.x * kThreads + threadIdx.x;
-    if (c >= 2 * K) return;
-    float* out = c < K ? dgamma : dbeta;
-    if (!out) return;
+// The partial sums' sum: 32 columns a workgroup, every 32nd part a thread, joined in LDS.
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void norm_grad_join_kernel(const float* __restrict__ partial, float* __restrict__ dgamma,
+                                                                      float* __restrict__ dbeta, int K, int parts) {
+    __shared__ float shared[32][33];
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
     float s = 0.0f;
-    for (int i = 0; i < parts; ++i) s += partial[(int64_t)i * 2 * K + c];
-    out[c < K ? c : c - K] = s;
+    if (c < 2 * K) {
+#pragma unroll 4
+        for (int i = y; i < parts; i += 32) s += partial[(int64_t)i * 2 * K + c];
+    }
+    shared[y][x] = s;
+    __syncthreads();
+    if (y != 0 || c >= 2 * K) return;
+#pragma unroll
+    for (int i = 1; i < 32; ++i) s += shared[i][x];
+    float* out = c < K ? dgamma : dbeta;
+    if (out) out[c < K ? c : c - K] = s;
 }
 
-static int norm_parts(int64_t rows) { return (int)(rows < 256 ? rows : 256); }
+// Rows are held in registers up to this length, one wavefront a row up to the other.
+constexpr int kHeldK = 8192, kWaveK = 1024;
+static bool held_in_registers(int K) { return K >= 8 && K <= kHeldK; }
+// Workgroups: enough that what they ask for hides the memory's latency, and no more, since each leaves a partial sum of both gradients.
+static int norm_parts(int64_t rows, int K) {
+    const int64_t most = !held_in_registers(K) ? 256 : 512, needed = held_in_registers(K) && K <= kWaveK ? (rows + kWaves - 1) / kWaves : rows;
+    return (int)(needed < most ? needed : most);
+}
 static size_t norm_grad_bytes(int64_t rows, int K) {
-    return (size_t)(round_up(rows * 8, 256) + round_up((int64_t)norm_parts(rows) * 2 * K * 4, 256));
+    return (size_t)((held_in_registers(K) ? 0 : round_up(rows * 8, 256)) + round_up((int64_t)norm_parts(rows, K) * 2 * K * 4, 256));
 }
 
 }  // namespace mx
@@ -226,12 +424,17 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
                 static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, static_cast<uint8_t*>(codes),
                 static_cast<uint8_t*>(scales), p);
         };
-        if (K <= 512) launch(norm_kernel<T, 1, 1>, 4);
-        else if (K <= 1024) launch(norm_kernel<T, 1, 2>, 4);
-        else if (K <= 2048) launch(norm_kernel<T, 4, 1>, 1);
-        else if (K <= 4096) launch(norm_kernel<T, 4, 2>, 1);
-        else if (K <= 8192) launch(norm_kernel<T, 4, 4>, 1);
-        else launch(norm_kernel<T, 4, 0>, 1);
+        const auto held = [&](auto whole) {
+            constexpr bool W = decltype(whole)::value;
+            if (K <= 512) launch(norm_kernel<T, 1, 1, W>, 4);
+            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W>, 4);
+            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W>, 1);
+            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W>, 1);
+            else launch(norm_kernel<T, 4, 4, W>, 1);
+        };
+        if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1);
+        else if (K % 8 == 0) held(std::true_type{});
+        else held(std::false_type{});
     });
     return launch_status();
 }
@@ -246,9 +449,9 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
     if (!sizes_ok(rows, K) || !type_valid(type) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return SPARQ_EINVAL;
     if (!extent_ok(rows, K)) return SPARQ_EINVAL;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const unsigned join = (unsigned)((2ll * K + kThreads - 1) / kThreads);
+    const unsigned join = (unsigned)((2ll * K + 31) / 32);
     if (rows == 0) {
-        if (dgamma || dbeta) norm_grad_join_kernel<<<join, kThreads, 0, s>>>(nullptr, dgamma, dbeta, K, 0);
+        if (dgamma || dbeta) norm_grad_join_kernel<<<join, kJoinThreads, 0, s>>>(nullptr, dgamma, dbeta, K, 0);
         return launch_status();
     }
     if (!tensor_ok(dy, type, lddy, K) || !tensor_ok(dx, type, lddx, K) || !coded_ok(codes, scales)) return SPARQ_EINVAL;
@@ -258,16 +461,29 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
     if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
     if (workspace_bytes < norm_grad_bytes(rows, K)) return SPARQ_EWORKSPACE;
     v2f* sums = static_cast<v2f*>(workspace);
-    float* partial = dgamma || dbeta ? reinterpret_cast<float*>(static_cast<char*>(workspace) + round_up(rows * 8, 256)) : nullptr;
-    const NormGradParams p = {lddy, lddx, code_pitch(K, 8), scale_pitch(K), rows, K, (float)(1.0 / K), norm_parts(rows)};
+    float* partial = dgamma || dbeta ? reinterpret_cast<float*>(static_cast<char*>(workspace) + (held_in_registers(K) ? 0 : round_up(rows * 8, 256))) : nullptr;
+    const NormGradParams p = {lddy, lddx, code_pitch(K, 8), scale_pitch(K), rows, K, (float)(1.0 / K), norm_parts(rows, K)};
     const uint8_t *c = static_cast<const uint8_t*>(codes), *sc = static_cast<const uint8_t*>(scales);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        norm_grad_rows_kernel<T><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(
-            static_cast<const T*>(dy), c, sc, mean, rstd, gamma, sums, p);
-        norm_grad_columns_kernel<T><<<dim3((unsigned)((K + 8ll * kThreads - 1) / (8 * kThreads)), p.parts), kThreads, 0, s>>>(
-            static_cast<const T*>(dy), c, sc, mean, rstd, gamma, sums, static_cast<T*>(dx), partial, p);
+        const T* from = static_cast<const T*>(dy);
+        T* to = static_cast<T*>(dx);
+        const auto launch = [&](auto kernel) { kernel<<<p.parts, kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, to, partial, p); };
+        const auto held = [&](auto whole) {
+            constexpr bool W = decltype(whole)::value;
+            if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W>);
+            else if (K <= kWaveK) launch(norm_grad_kernel<T, 1, 2, W>);
+            else if (K <= 2048) launch(norm_grad_kernel<T, 4, 1, W>);
+            else if (K <= 4096) launch(norm_grad_kernel<T, 4, 2, W>);
+            else launch(norm_grad_kernel<T, 4, 4, W>);
+        };
+        if (held_in_registers(K)) K % 8 == 0 ? held(std::true_type{}) : held(std::false_type{});
+        else {
+            norm_grad_rows_kernel<T><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, sums, p);
+            norm_grad_columns_kernel<T><<<dim3((unsigned)((K + 8ll * kThreads - 1) / (8 * kThreads)), p.parts), kThreads, 0, s>>>(
+                from, c, sc, mean, rstd, gamma, sums, to, partial, p);
+        }
     });
-    if (partial) norm_grad_join_kernel<<<join, kThreads, 0, s>>>(partial, dgamma, dbeta, K, p.parts);
+    if (partial) norm_grad_join_kernel<<<join, kJoinThreads, 0, s>>>(partial, dgamma, dbeta, K, p.parts);
     return launch_status();
 }
