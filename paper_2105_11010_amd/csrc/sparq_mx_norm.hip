@@ -73,8 +73,17 @@ __device__ __forceinline__ void store_own(T* row, const Place& p, const float (&
     }
 }
 
+// The lane's own elements to the front, zeros behind them: a checkpoint's codes lie where the row's eights begin.
+__device__ __forceinline__ void first_own(const Place& p, float (&v)[8]) {
+#pragma unroll
+    for (int by = 4; by; by >>= 1)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = p.skip & by ? (i + by < 8 ? v[i + by] : 0.0f) : v[i];
+}
+
 // WAVES wavefronts take a row of at least eight, CHUNKS x 8 values a lane, which stay in registers from the load to the result: one
-// pass over memory, the mean first and the squares of what differs from it second.
+// pass over memory, the mean first and the squares of what differs from it second.  As many workgroups as have room go through the rows,
+// gamma and beta in registers and the next row on its way while this one is summed.
 template <class T, int WAVES, int CHUNKS, bool WHOLE>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
@@ -83,56 +92,68 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x,
     __shared__ float shared[2 * WAVES];
     constexpr int kPerBlock = kWaves / WAVES, kSpan = WAVES * 512;
     const int wave = threadIdx.x >> 6, t = threadIdx.x & (WAVES * 64 - 1), lane = threadIdx.x & 63;
-    const int64_t row = (int64_t)blockIdx.x * kPerBlock + (WAVES == 1 ? wave : 0);
-    if (row >= p.rows) return;                               // (whole workgroups where they share a row)
+    const int64_t first = (int64_t)blockIdx.x * kPerBlock + (WAVES == 1 ? wave : 0), stride = (int64_t)gridDim.x * kPerBlock;
+    if (first >= p.rows) return;                             // (whole workgroups where they share a row)
     int turn = 0;
-    x += row * p.ldx;
-    y += row * p.ldy;
     Raw8<T> raw[CHUNKS];
-    float v[CHUNKS][8], sum = 0.0f;
+    float g[CHUNKS][8], b[CHUNKS][8];
     Place at[CHUNKS];
+    auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+        row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) load_raw(x + row * p.ldx + at[c].from, 8, raw[c]);
+    };
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
+    fetch(first);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
-        at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
-        load_raw(x + at[c].from, 8, raw[c]);
-    }
+        load8(gamma + at[c].from, g[c]);
+        if (beta) load8(beta + at[c].from, b[c]);
+        else {
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        values_of(raw[c], v[c]);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) sum += own<WHOLE>(at[c], i) ? v[c][i] : 0.0f;
-    }
-    const float mean = row_sum<WAVES>(sum, shared, turn) * p.inv_K;
-    float squares = 0.0f;
-#pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const float d = v[c][i] - mean;
-            squares += own<WHOLE>(at[c], i) ? d * d : 0.0f;
+            for (int i = 0; i < 8; ++i) b[c][i] = 0.0f;
         }
-    const float var = row_sum<WAVES>(squares, shared, turn) * p.inv_K;
-    const float rstd = 1.0f / sqrtf(var + p.eps);
-    if (t == 0 && mean_out) mean_out[row] = mean;
-    if (t == 0 && rstd_out) rstd_out[row] = rstd;
+    }
+    for (int64_t row = first; row < p.rows; row += stride) {
+        float v[CHUNKS][8], sum = 0.0f;
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c) {
-        float g[8], b[8], o[8];
-        load8(gamma + at[c].from, g);
-        if (beta) load8(beta + at[c].from, b);
+        for (int c = 0; c < CHUNKS; ++c) {
+            values_of(raw[c], v[c]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (v[c][i] - mean) * rstd * g[i] + (beta ? b[i] : 0.0f);
-        store_own<WHOLE>(y, at[c], o);
-        if (codes && at[c].col - 8 * lane < p.K) {           // the wavefront's 512 values begin inside the row
-            if (!WHOLE && at[c].skip) load_upto8(x + at[c].col, p.K - at[c].col, v[c]);
-            if (!at[c].inside) {
+            for (int i = 0; i < 8; ++i) sum += own<WHOLE>(at[c], i) ? v[c][i] : 0.0f;
+        }
+        fetch(row + stride);
+        const float mean = row_sum<WAVES>(sum, shared, turn) * p.inv_K;
+        float squares = 0.0f;
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[c][i] = 0.0f;
+        for (int c = 0; c < CHUNKS; ++c)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const float d = v[c][i] - mean;
+                squares += own<WHOLE>(at[c], i) ? d * d : 0.0f;
             }
-            const uint32_t byte = scale8_of(block_top(v[c]));
-            const v2u w = codes8_of(v[c], byte);
-            if (at[c].col < p.K128) *reinterpret_cast<v2u*>(codes + row * p.code_pitch + at[c].col) = w;
-            if ((lane & 3) == 0) scales[row * p.scale_pitch + (at[c].col >> 5)] = (uint8_t)byte;
+        const float var = row_sum<WAVES>(squares, shared, turn) * p.inv_K;
+        const float rstd = 1.0f / sqrtf(var + p.eps);
+        if (t == 0 && mean_out) mean_out[row] = mean;
+        if (t == 0 && rstd_out) rstd_out[row] = rstd;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) {
+            float o[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (v[c][i] - mean) * rstd * g[c][i] + b[c][i];
+            store_own<WHOLE>(y + row * p.ldy, at[c], o);
+            if (codes && at[c].col - 8 * lane < p.K) {       // the wavefront's 512 values begin inside the row
+                if constexpr (!WHOLE) first_own(at[c], v[c]);
+                if (!at[c].inside) {
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) v[c][i] = 0.0f;
+                }
+                const uint32_t byte = scale8_of(block_top(v[c]));
+                const v2u w = codes8_of(v[c], byte);
+                if (at[c].col < p.K128) *reinterpret_cast<v2u*>(codes + row * p.code_pitch + at[c].col) = w;
+                if ((lane & 3) == 0) scales[row * p.scale_pitch + (at[c].col >> 5)] = (uint8_t)byte;
+            }
         }
     }
 }
@@ -419,20 +440,21 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const auto launch = [&](auto kernel, int per_block) {
-            kernel<<<(unsigned)((rows + per_block - 1) / per_block), kThreads, 0, s>>>(
+        const auto launch = [&](auto kernel, int per_block, int per_cu) {
+            const int64_t blocks = (rows + per_block - 1) / per_block, places = per_cu ? (int64_t)per_cu * device_cu_count() : blocks;
+            kernel<<<(unsigned)(blocks < places ? blocks : places), kThreads, 0, s>>>(
                 static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, static_cast<uint8_t*>(codes),
                 static_cast<uint8_t*>(scales), p);
         };
         const auto held = [&](auto whole) {
             constexpr bool W = decltype(whole)::value;
-            if (K <= 512) launch(norm_kernel<T, 1, 1, W>, 4);
-            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W>, 4);
-            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W>, 1);
-            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W>, 1);
-            else launch(norm_kernel<T, 4, 4, W>, 1);
+            if (K <= 512) launch(norm_kernel<T, 1, 1, W>, 4, 8);
+            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W>, 4, 5);
+            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W>, 1, 8);
+            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W>, 1, 5);
+            else launch(norm_kernel<T, 4, 4, W>, 1, 3);
         };
-        if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1);
+        if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1, 0);
         else if (K % 8 == 0) held(std::true_type{});
         else held(std::false_type{});
     });
