@@ -1,22 +1,26 @@
 // The product of 4-bit operands (include/sparq_mx.h).
+#include "sparq_mx_few.h"
 #include "sparq_mx_gemm_kernel.h"
 
 namespace sparq {
 namespace mx {
 
 struct GemmPlan {
-    int tile;                // 256 or 128: results a workgroup makes along either side
+    int tile;                // 256 or 128: results a workgroup makes along either side; 0: few rows, a kernel of their own
     int parts;               // of the reduction
     size_t bytes;            // of partial results
 };
 static GemmPlan gemm_plan(int64_t M, int N, int K) {
     GemmPlan p = {};
+    // Few rows: the kernel that reads the weights at memory's pace, while its rereading of A is no longer than that (us, it -> 128 x 128 tiles:
+    // 64 x 4096 x 4096 8.2 -> 11, 32 x 8192 x 8192 16 -> 18.5, 48 x 8192 x 8192 20.9 -> 18.6, 64 x 8192 x 8192 24.9 -> 18.6).
+    if (M <= 32 || (M <= kFewMost && M * N * K <= 1ll << 31)) return p;
     const auto tiles = [&](int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
     p.tile = tiles(256) >= 192 ? 256 : 128;
-    const int64_t n = tiles(p.tile), steps = (K + kCodeUnit - 1) / kCodeUnit;
-    int64_t parts = p.tile == 256 ? 1 : 512 / n;
-    if (parts > steps / 8) parts = steps / 8;
-    p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
+    // Few tiles of a long reduction are divided; shorter ones, or more of them, are over before the parts would be joined (us, whole -> in
+    // parts: 128 x 1024 x 8192 16.2 -> 13.6, 65 x 8192 x 8192 18.6 -> 16.8, 128 x 4096 x 4096 11.3 -> 14.6, 512 x 4096 x 4096 12 -> 23).
+    const int64_t n = tiles(p.tile), steps = (K + kCodeUnit - 1) / kCodeUnit, most = steps / 16;
+    p.parts = n <= 64 && steps >= 64 ? (int)(128 / n < most ? 128 / n : most) : 1;
     p.bytes = p.parts > 1 ? (size_t)round_up(p.parts * M * N * 4, 256) : 0;
     return p;
 }
@@ -41,6 +45,12 @@ static sparq_status launch_tile(const GemmParams& p, void* y, hipStream_t stream
 static sparq_status gemm(const void* a, const void* as, const void* w, const void* ws, const float* bias, void* y, int type, int64_t ldy,
                          int64_t M, int N, int K, const GemmPlan& plan, void* workspace, hipStream_t stream) {
     const int t = plan.tile;
+    if (t == 0) {
+        const FewParams f = {nullptr, static_cast<const uint8_t*>(a), static_cast<const uint8_t*>(as), static_cast<const uint8_t*>(w),
+                             static_cast<const uint8_t*>(ws), bias, 0, ldy, code_pitch(K, 4), scale_pitch(K), (int)M, N, K,
+                             (K + kScaleUnit - 1) / kScaleUnit, (K + kCodeUnit - 1) / kCodeUnit - 1};
+        return launch_few_rows(f, 0, y, type, stream);
+    }
     const int64_t tiles_m = (M + t - 1) / t, tiles_n = (N + t - 1) / t;
     if (tiles_m > INT32_MAX || tiles_m * tiles_n > INT32_MAX) return SPARQ_EUNSUPPORTED;
     const bool parted = plan.parts > 1;
@@ -98,10 +108,17 @@ extern "C" sparq_status sparq_mx_gemm(const void* a_codes, const void* a_scales,
     return gemm(a_codes, a_scales, w_codes, w_scales, bias, y, type, ldy, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
 }
 
-static size_t coded_bytes(int64_t M, int K) { return (size_t)(round_up(M * code_pitch(K, 4), 256) + round_up(M * scale_pitch(K), 256)); }
+// Whether the product quantises its rows itself: what that saves is a launch, about 3 us, and what it costs is every workgroup doing it
+// again (us, itself -> before it: 8 x 4096 x 4096 6.1 -> 6.9, 16 x 4096 x 4096 8.1 -> 7.1, 1 x 8192 x 8192 9.4 -> 10.8, 8 x 8192 x 8192
+// 15.2 -> 12.5).
+static bool quantised_on_the_way(int64_t M, int N, int K) { return M <= kFewRows && M * N * K <= 1 << 27; }
+static size_t coded_bytes(int64_t M, int N, int K) {
+    if (quantised_on_the_way(M, N, K)) return 0;
+    return (size_t)(round_up(M * code_pitch(K, 4), 256) + round_up(M * scale_pitch(K), 256));
+}
 
 extern "C" size_t sparq_mx_linear_workspace_bytes(int64_t M, int32_t N, int32_t K) {
-    return gemm_sizes_ok(M, N, K) && M > 0 ? coded_bytes(M, K) + gemm_plan(M, N, K).bytes : 0;
+    return gemm_sizes_ok(M, N, K) && M > 0 ? coded_bytes(M, N, K) + gemm_plan(M, N, K).bytes : 0;
 }
 
 extern "C" sparq_status sparq_mx_linear(const void* x, int32_t x_type, int64_t ldx, const void* w_codes, const void* w_scales,
@@ -112,11 +129,16 @@ extern "C" sparq_status sparq_mx_linear(const void* x, int32_t x_type, int64_t l
     if (!coded_ok(w_codes, w_scales) || !aligned(bias, 4)) return SPARQ_EINVAL;
     if (!tensor_ok(x, x_type, ldx, K) || !extent_ok(M, ldx) || !tensor_ok(y, y_type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K))
         return SPARQ_EINVAL;
-    if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
-    const GemmPlan plan = gemm_plan(M, N, K);
-    const size_t coded = coded_bytes(M, K);
-    if (workspace_bytes < coded + plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    if (quantised_on_the_way(M, N, K)) {
+        const FewParams f = {x, nullptr, nullptr, static_cast<const uint8_t*>(w_codes), static_cast<const uint8_t*>(w_scales), bias, ldx, ldy,
+                             code_pitch(K, 4), scale_pitch(K), (int)M, N, K, (K + kScaleUnit - 1) / kScaleUnit, (K + kCodeUnit - 1) / kCodeUnit - 1};
+        return launch_few_rows(f, x_type, y, y_type, s);
+    }
+    const GemmPlan plan = gemm_plan(M, N, K);
+    const size_t coded = coded_bytes(M, N, K);
+    if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
+    if (workspace_bytes < coded + plan.bytes) return SPARQ_EWORKSPACE;
     uint8_t *codes = static_cast<uint8_t*>(workspace), *scales = codes + round_up(M * code_pitch(K, 4), 256);
     const sparq_status q = launch_quantize(x, x_type, ldx, M, K, codes, scales, nullptr, nullptr, s);
     if (q != SPARQ_OK) return q;

@@ -8,22 +8,33 @@ constexpr int kThreads = 256;
 
 // out = the parts' sum, part after part; four values a thread.
 template <class O>
-__global__ __launch_bounds__(kThreads) void join_kernel(const float* __restrict__ partial, const float* __restrict__ bias, O* __restrict__ out, int64_t J, int K, int64_t ldo, int parts) {
+__global__ __launch_bounds__(kThreads) void join_kernel(const float* __restrict__ partial, const float* __restrict__ bias, O* __restrict__ out,
+                                                        int64_t J, int K, int64_t ldo, int parts) {
     const int k = (blockIdx.x * kThreads + threadIdx.x) * 4;
     if (k >= K) return;
     const int n = K - k < 4 ? K - k : 4;
-    for (int64_t j = blockIdx.y; j < J; j += gridDim.y) {
-        float s[4] = {};
-        for (int i = 0; i < parts; ++i) {
-            const float* at = partial + (i * J + j) * K + k;
+    const bool words = K % 4 == 0;                           // (rows of partial results are K apart)
+    float b[4] = {};
+    if (bias) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (e < n) s[e] += at[e];
+        for (int e = 0; e < 4; ++e)
+            if (e < n) b[e] = bias[k + e];
+    }
+    for (int64_t j = blockIdx.y; j < J; j += gridDim.y) {
+        v4f s = {};
+        const float* at = partial + j * K + k;
+        for (int i = 0; i < parts; ++i, at += J * K) {
+            if (words) s += *reinterpret_cast<const v4f*>(at);
+            else {
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (e < n) s[e] += at[e];
+            }
         }
         O* to = out + j * ldo + k;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
-            if (e < n) to[e] = (O)(s[e] + (bias ? bias[k + e] : 0.0f));
+            if (e < n) to[e] = (O)(s[e] + b[e]);
     }
 }
 
