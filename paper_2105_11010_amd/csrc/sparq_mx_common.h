@@ -245,6 +245,8 @@ sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows,
 // Implemented in sparq_mx_join.hip: out[j][k] = the sum over the parts of partial [parts][J][K], part after part, + bias[k]
 // (NULL: none), rounded to the type.
 sparq_status launch_join(const float* partial, const float* bias, void* out, int type, int64_t J, int K, int64_t ldo, int parts, hipStream_t stream);
+// ... and of partial [parts][columns]: the columns before `split` into first, the others into second (NULL: not wanted).
+sparq_status launch_join_columns(const float* partial, float* first, float* second, int split, int columns, int parts, hipStream_t stream);
 
 typedef __attribute__((address_space(3))) void* LdsPtr;
 // The wait instruction's operand for at most n loads and stores on their way; for that and no access to LDS.

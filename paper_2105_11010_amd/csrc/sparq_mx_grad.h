@@ -40,7 +40,7 @@ sparq_status launch_grad_types(const GradParams& p, int parts, int tile, void* o
     sparq_status s = SPARQ_OK;
     with_type(out_type, [&](auto o) {
         typedef decltype(o) O;
-        static std::atomic<bool> allowed[2][kMaxDevices];
+        static std::atomic<bool> allowed[3][kMaxDevices];
         if constexpr (std::is_same_v<T, __bf16>) {
             if (tile == kWideTile) {
                 s = launch_grad_kernel<O>(grad_wide_kernel<O, DW>, kWideLds, allowed[0], p, parts, out, stream);
@@ -49,7 +49,8 @@ sparq_status launch_grad_types(const GradParams& p, int parts, int tile, void* o
         }
         constexpr int lds_bytes = 2 * (kParts<T> + 1) * 128 * kGradStep * 2;
         static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
-        s = launch_grad_kernel<O>(grad_kernel<T, O, DW, 128, 128>, lds_bytes, allowed[1], p, parts, out, stream);
+        s = tile == 64 ? launch_grad_kernel<O>(grad_kernel<T, O, DW, 64, 64>, lds_bytes / 2, allowed[2], p, parts, out, stream)
+                       : launch_grad_kernel<O>(grad_kernel<T, O, DW, 128, 128>, lds_bytes, allowed[1], p, parts, out, stream);
     });
     return s;
 }

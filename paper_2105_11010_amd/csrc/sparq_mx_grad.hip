@@ -4,36 +4,44 @@
 namespace sparq {
 namespace mx {
 
-constexpr int kThreads = 256;
-
-// Sums of dy's columns over a slab of its rows: a workgroup takes 256 columns, eight a thread, and eight rows at a time.
+// Sums of dy's columns over a slab of its rows: a workgroup takes 64 columns, eight a lane, and 128 rows at a time.
+constexpr int kSumThreads = 1024, kSumColumns = 64, kSumRows = kSumThreads / (kSumColumns / 8);
 template <class T>
-__global__ __launch_bounds__(kThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
-    __shared__ float shared[8][256 + 8];
-    const int t = threadIdx.x, c = (blockIdx.x * 32 + (t & 31)) * 8;
+__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
+    __shared__ float shared[kSumRows][kSumColumns + 4];
+    const int t = threadIdx.x, x = t % (kSumColumns / 8), r0 = t / (kSumColumns / 8), c = blockIdx.x * kSumColumns + 8 * x;
     const int64_t begin = blockIdx.y * slab, end = begin + slab < rows ? begin + slab : rows;
     float s[8] = {};
     if (c < n)
-        for (int64_t r = begin + (t >> 5); r < end; r += 8) {
-            float v[8];
-            load_upto8(dy + r * ld + c, n - c, v);
+        for (int64_t r = begin + r0; r < end; r += 4 * kSumRows) {
+            float v[4][8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) s[i] += v[i];
+            for (int u = 0; u < 4; ++u) load_upto8(dy + (r + u * kSumRows) * ld + c, r + u * kSumRows < end ? n - c : 0, v[u]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; ++i) s[i] += v[u][i];
         }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) shared[t >> 5][(t & 31) * 8 + i] = s[i];
+    for (int i = 0; i < 8; ++i) shared[r0][8 * x + i] = s[i];
     __syncthreads();
-    const int col = blockIdx.x * 256 + t;
-    if (col >= n) return;
-    float total = shared[0][t];
+    // 16 threads a column, eight rows each, then one
+    const int col = t & 63, part = t >> 6;
+    float total = 0.0f;
 #pragma unroll
-    for (int i = 1; i < 8; ++i) total += shared[i][t];
-    sum[(int64_t)blockIdx.y * n + col] = total;
+    for (int i = 0; i < kSumRows / 16; ++i) total += shared[part * (kSumRows / 16) + i][col];
+    __syncthreads();
+    shared[part][col] = total;
+    __syncthreads();
+    if (part != 0 || blockIdx.x * kSumColumns + col >= n) return;
+#pragma unroll
+    for (int i = 1; i < 16; ++i) total += shared[i][col];
+    sum[(int64_t)blockIdx.y * n + blockIdx.x * kSumColumns + col] = total;
 }
 
 // ---- plan ----------------------------------------------------------------------------
 struct GradPlan {
-    int tile;                // 256 or 128: results a workgroup makes along either side
+    int tile;                // 256, 128 or 64: results a workgroup makes along either side
     int parts;               // of the reduction
     int slabs;               // of rows for the column sums
     size_t partial_bytes, bytes;
@@ -41,12 +49,14 @@ struct GradPlan {
 static GradPlan grad_plan(bool wide, int64_t J, int64_t R, int K, bool dw) {
     GradPlan p = {};
     const auto tiles = [&](int t) { return ((J + t - 1) / t) * ((K + t - 1) / t); };
-    p.tile = wide && tiles(256) >= 192 ? 256 : 128;
-    const int64_t n = tiles(p.tile), steps = (R + kGradStep - 1) / kGradStep;
-    int64_t parts = p.tile == 256 ? 1 : 512 / n;
-    if (parts > steps / 4) parts = steps / 4;
+    // Few tiles of a long reduction are divided; shorter ones are over before the parts would be joined.  Tiles are as large as still leaves
+    // work for every CU: a larger one's steps cost less per result.
+    const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / 16 > 1 ? steps / 16 : 1;
+    p.tile = wide && tiles(256) >= 192 ? 256 : tiles(128) * most >= 192 ? 128 : 64;
+    const int64_t n = tiles(p.tile), places = p.tile == 256 || n >= 192 ? 1 : (p.tile == 128 ? 512 : 1024) / n, parts = places < most ? places : most;
     p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
-    p.slabs = !dw ? 0 : (int)(R < 64 ? 1 : R / 64 < 64 ? R / 64 : 64);
+    const int64_t columns = (J + 63) / 64, slabs = R / 512 < 1024 / columns ? R / 512 : 1024 / columns;
+    p.slabs = !dw ? 0 : slabs < 1 ? 1 : (int)slabs;
     p.partial_bytes = p.parts > 1 ? (size_t)round_up(p.parts * J * K * 4, 256) : 0;
     p.bytes = p.partial_bytes + (p.slabs > 1 ? (size_t)round_up((int64_t)p.slabs * J * 4, 256) : 0);
     return p;
@@ -130,11 +140,11 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
         float* sums = plan.slabs > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes) : db;
         with_type(dy_type, [&](auto t) {
             typedef decltype(t) T;
-            column_sum_kernel<T><<<dim3((N + 255) / 256, plan.slabs), kThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
+            column_sum_kernel<T><<<dim3((N + kSumColumns - 1) / kSumColumns, plan.slabs), kSumThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
                                                                                         (M + plan.slabs - 1) / plan.slabs, sums);
         });
         if (plan.slabs > 1) {
-            const sparq_status joined = launch_join(sums, nullptr, db, SPARQ_MX_F32, 1, N, N, plan.slabs, s);
+            const sparq_status joined = launch_join_columns(sums, db, nullptr, N, N, plan.slabs, s);
             if (joined != SPARQ_OK) return joined;
         }
     }

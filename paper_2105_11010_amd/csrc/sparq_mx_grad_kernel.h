@@ -44,6 +44,7 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return pack2(a
 
 // C neighbouring elements
 template <int BYTES> struct Word;
+template <> struct Word<1> { typedef uint8_t Type; };
 template <> struct Word<2> { typedef uint16_t Type; };
 template <> struct Word<4> { typedef uint32_t Type; };
 template <> struct Word<8> { typedef v2u Type; };
@@ -200,7 +201,7 @@ struct CodedTile {
             for (int i = 0; i < 8; ++i) {
                 uint32_t w;
                 if constexpr (N == 8) w = raw[i][q >> 1];
-                else w = raw[i];
+                else w = (uint32_t)raw[i];
                 const float s = unit8_of(scale[i]);
                 v[i][0] = (float)(int8_t)(w >> (16 * (q & 1))) * s;
                 v[i][1] = (float)(int8_t)(w >> (16 * (q & 1) + 8)) * s;
@@ -256,8 +257,9 @@ template <class Dy, class Coded, int TJ, int TK>
 __device__ __forceinline__ void convert(const Dy& dy, const Coded& coded, v4u* tile, int q) {
     constexpr int kDyParts = TJ / 32, kCodedParts = TK / 64;
 #pragma unroll
-    for (int i = 0; i < kDyParts / 4; ++i) dy.store(tile, q * (kDyParts / 4) + i);
-    if (kCodedParts >= 4 || (q & 1) == 0) coded.store(tile + Dy::P * TJ * 8, kCodedParts >= 4 ? q : q >> 1);
+    for (int i = q * kDyParts / 4; i < (q + 1) * kDyParts / 4; ++i) dy.store(tile, i);
+#pragma unroll
+    for (int i = q * kCodedParts / 4; i < (q + 1) * kCodedParts / 4; ++i) coded.store(tile + Dy::P * TJ * 8, i);
 }
 // Steps that are not whole, or whose loads would not be: checked loads, one step after the other.
 template <class T, bool DW, int TJ, int TK>
@@ -279,7 +281,7 @@ __device__ __forceinline__ void multiply_rest(Products<kParts<T>, TJ, TK>& produ
 }
 
 template <class T, class O, bool DW, int TJ, int TK>
-__global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ out, const GradParams p) {
+__global__ __launch_bounds__(kGradThreads) void grad_kernel(O* __restrict__ out, const GradParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
     constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
@@ -327,7 +329,7 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_kernel(O* __restrict__ o
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, FK, FJ, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + products.wj, p.J, k0 + products.wk, p.K, none,
+    store_results<O, FK, FJ, FK == 1 ? 64 : 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + products.wj, p.J, k0 + products.wk, p.K, none,
                                   reinterpret_cast<uint8_t*>(lds) + (threadIdx.x >> 6) * 4096);
 #endif
 }

@@ -389,26 +389,6 @@ __global__ __launch_bounds__(kThreads) void norm_grad_columns_kernel(const T* __
     }
 }
 
-// The partial sums' sum: 32 columns a workgroup, every 32nd part a thread, joined in LDS.
-constexpr int kJoinThreads = 1024;
-__global__ __launch_bounds__(kJoinThreads) void norm_grad_join_kernel(const float* __restrict__ partial, float* __restrict__ dgamma,
-                                                                      float* __restrict__ dbeta, int K, int parts) {
-    __shared__ float shared[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
-    float s = 0.0f;
-    if (c < 2 * K) {
-#pragma unroll 4
-        for (int i = y; i < parts; i += 32) s += partial[(int64_t)i * 2 * K + c];
-    }
-    shared[y][x] = s;
-    __syncthreads();
-    if (y != 0 || c >= 2 * K) return;
-#pragma unroll
-    for (int i = 1; i < 32; ++i) s += shared[i][x];
-    float* out = c < K ? dgamma : dbeta;
-    if (out) out[c < K ? c : c - K] = s;
-}
-
 // Rows are held in registers up to this length, one wavefront a row up to the other.
 constexpr int kHeldK = 8192, kWaveK = 1024;
 static bool held_in_registers(int K) { return K >= 8 && K <= kHeldK; }
@@ -471,10 +451,8 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
     if (!sizes_ok(rows, K) || !type_valid(type) || !aligned(dgamma, 4) || !aligned(dbeta, 4)) return SPARQ_EINVAL;
     if (!extent_ok(rows, K)) return SPARQ_EINVAL;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const unsigned join = (unsigned)((2ll * K + 31) / 32);
     if (rows == 0) {
-        if (dgamma || dbeta) norm_grad_join_kernel<<<join, kJoinThreads, 0, s>>>(nullptr, dgamma, dbeta, K, 0);
-        return launch_status();
+        return dgamma || dbeta ? launch_join_columns(nullptr, dgamma, dbeta, K, 2 * K, 0, s) : SPARQ_OK;
     }
     if (!tensor_ok(dy, type, lddy, K) || !tensor_ok(dx, type, lddx, K) || !coded_ok(codes, scales)) return SPARQ_EINVAL;
     if (!mean || !rstd || !gamma || !aligned(mean, 4) || !aligned(rstd, 4) || !aligned(gamma, 4)) return SPARQ_EINVAL;
@@ -506,6 +484,6 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
                 from, c, sc, mean, rstd, gamma, sums, to, partial, p);
         }
     });
-    if (partial) norm_grad_join_kernel<<<join, kJoinThreads, 0, s>>>(partial, dgamma, dbeta, K, p.parts);
+    if (partial) return launch_join_columns(partial, dgamma, dbeta, K, 2 * K, p.parts, s);
     return launch_status();
 }
