@@ -42,6 +42,7 @@ __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const T* __rest
 // ---- plan ----------------------------------------------------------------------------
 struct GradPlan {
     int tile;                // 256, 128 or 64: results a workgroup makes along either side
+    bool wide;               // on grad_wide_kernel (bf16; 256 or 128)
     int parts;               // of the reduction
     int slabs;               // of rows for the column sums
     size_t partial_bytes, bytes;
@@ -53,6 +54,7 @@ static GradPlan grad_plan(bool wide, int64_t J, int64_t R, int K, bool dw) {
     // work for every CU: a larger one's steps cost less per result.
     const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / 16 > 1 ? steps / 16 : 1;
     p.tile = wide && tiles(256) >= 192 ? 256 : tiles(128) * most >= 192 ? 128 : 64;
+    p.wide = wide && p.tile != 64;
     const int64_t n = tiles(p.tile), places = p.tile == 256 || n >= 192 ? 1 : (p.tile == 128 ? 512 : 1024) / n, parts = places < most ? places : most;
     p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
     const int64_t columns = (J + 63) / 64, slabs = R / 512 < 1024 / columns ? R / 512 : 1024 / columns;
@@ -92,7 +94,7 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     const bool parted = plan.parts > 1;
     p.ldo = parted ? K : ldo;
     p.part_stride = parted ? J * K : 0;
-    const sparq_status s = launch_grad(p, plan.parts, t, dy_type, bits == 8, parted ? workspace : out, parted ? SPARQ_MX_F32 : out_type, stream);
+    const sparq_status s = launch_grad(p, plan.parts, t, plan.wide, dy_type, bits == 8, parted ? workspace : out, parted ? SPARQ_MX_F32 : out_type, stream);
     if (s != SPARQ_OK || !parted) return s;
     return launch_join(static_cast<const float*>(workspace), nullptr, out, out_type, J, K, ldo, plan.parts, stream);
 }

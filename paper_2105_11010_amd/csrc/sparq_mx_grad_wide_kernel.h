@@ -1,9 +1,9 @@
-// The gradients of large layers in bf16: 256 x 256 results a workgroup.
+// The gradients in bf16: 256 x 256 results a workgroup, or 128 x 128 where those would leave CUs without.
 // out[j][k] = sum_r dy(j, r) V[r][k] as in sparq_mx_grad_kernel.h.  V's rows are decoded as they lie, eight values of a row a thread, and dy's are
 // copied; the matrix instruction's operands, eight neighbouring r of one column, come out of LDS by reads that turn 4 x 16 values (V, and dy
 // where r is its row).  Sixteen lanes read four rows, 32 bytes each, at a time: a row's 16-byte units are permuted by the row so that four
 // neighbouring rows lie in different quarters of the banks.
-// A step is 64 r, four quarters of sixteen matrix instructions; one wavefront a SIMD has nobody else to fill the time an
+// A step is 64 r, four quarters of sixteen (or four) matrix instructions; one wavefront a SIMD has nobody else to fill the time an
 // instruction runs, so what goes between them is laid out here: the next quarter's reads, and of V and of dy two rows each, written to the
 // next step's tiles, and the request for their successors.  One barrier a step, before the last quarter: by then the step's tiles have been
 // read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, 392 us where
@@ -16,9 +16,7 @@
 namespace sparq {
 namespace mx {
 
-constexpr int kWideTile = 256;
-constexpr int kWideBytes = kGradStep * kWideTile * 2;        // of one side's tile
-constexpr int kWideLds = 4 * kWideBytes;
+template <int TILE> inline constexpr int kWideBytes = kGradStep * TILE * 2;       // of one side's tile
 
 // A call this kernel is for: whole words of dy, rows whose distances fit the loads' 32-bit offsets, and no run of eight columns (DW) that the
 // last column cuts.
@@ -27,43 +25,48 @@ inline bool grad_wide_fits(const void* dy, int64_t lddy, int64_t J, int64_t code
     return aligned(dy, 4) && lddy % 2 == 0 && lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J % 8 == 0);
 }
 
-template <class O, bool DW>
-__global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
+template <class O, bool DW, int TILE>
+__global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
+    constexpr int kF = TILE / 64, kSlots = kF * kF;          // 32 x 32 results along a side; matrix instructions a quarter
+    constexpr int kUnits = TILE / 32, kRuns = TILE / 128, kRow = TILE * 2;      // of dy and of V a thread; bytes of a tile's row
+    constexpr int kBytes = kWideBytes<TILE>;
     typedef short v4s __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
-    uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * kWideBytes;
+    uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * kBytes;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
     uint32_t tj, tk;
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
-    const int64_t j0 = (int64_t)tj * kWideTile;
-    const int k0 = (int)tk * kWideTile;
+    const int64_t j0 = (int64_t)tj * TILE;
+    const int k0 = (int)tk * TILE;
     const int s_begin = (int)blockIdx.y * p.steps_per_part, s_all = (int)((p.R + kGradStep - 1) / kGradStep), s_whole = (int)(p.R / kGradStep);
     const int s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = s_whole < s_end ? s_whole : s_end;
-    Products<1, kWideTile, kWideTile> products;
+    Products<1, TILE, TILE> products;
     const int wj = products.wj, wk = products.wk;
 
     if (s_begin < s_fast) {
-        // ---- dy: a thread has eight 16-byte units: of rows 8 i + t / 32 (DW) or of rows 32 i + t / 8, 64 r each
-        v4u kept[8];
-        uint32_t dy_at[DW ? 1 : 8];
+        // ---- dy: a thread has kUnits 16-byte units: of every eighth or 16th row (DW) or of rows 32 i + t / 8, 64 r each
+        constexpr int kAcross = TILE / 8, kRowsAtOnce = kGradThreads / kAcross;
+        v4u kept[kUnits];
+        uint32_t dy_at[DW ? 1 : kUnits];
         if constexpr (DW) {
-            int64_t j = j0 + 8 * (t & 31);
+            int64_t j = j0 + 8 * (t % kAcross);
             j = j < p.J ? j : p.J - 8;                       // (columns past the last one make results that are not stored)
-            dy_at[0] = (uint32_t)(((t >> 5) * p.lddy + (j - j0)) * 2);
+            dy_at[0] = (uint32_t)((t / kAcross * p.lddy + (j - j0)) * 2);
         } else {
             const int64_t last = p.J - 1 - j0;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < kUnits; ++i) {
                 const int row = 32 * i + (t >> 3), from = row < last ? row : (int)last;
                 dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * 2);
             }
         }
-        // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32
+        // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32, or one of row 4 (lane / 4) + wave
         constexpr int kWords = DW ? 8 : 4;
-        uint32_t raw[2][kWords], scale[2];
-        const int v_row = 4 * (lane >> 3) + wave;
-        int k = k0 + 32 * (lane & 7);
+        uint32_t raw[kRuns][kWords], scale[kRuns];
+        constexpr int kBlocks = TILE / 32;
+        const int v_row = 4 * (lane / kBlocks) + wave;
+        int k = k0 + 32 * (lane % kBlocks);
         k = k < p.K128 ? k : p.K128 - 32;
         const uint32_t v_at = (uint32_t)(v_row * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)(v_row * p.scale_pitch + (k >> 5));
 
@@ -81,7 +84,7 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
         };
         const auto buffer = [](const uint8_t* from) __attribute__((always_inline)) { return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000); };
         auto load_dy = [&](int i) __attribute__((always_inline)) {
-            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], DW ? (int)(8 * i * p.lddy * 2) : 0, 0);
+            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], DW ? (int)(kRowsAtOnce * i * p.lddy * 2) : 0, 0);
         };
         auto load_v = [&](int run) __attribute__((always_inline)) {
 #pragma unroll
@@ -92,15 +95,15 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
             }
             scale[run] = __builtin_amdgcn_raw_buffer_load_b8(buffer(scales_from), scale_at, (int)(32 * run * p.scale_pitch), 0);
         };
-        // A tile's row of 512 bytes is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
+        // A tile's row is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
         const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
-            return row * 512 + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
+            return row * kRow + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
         };
         auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
-            if constexpr (DW) *reinterpret_cast<v4u*>(tile + permuted(8 * i + (t >> 5), t & 31)) = kept[i];
+            if constexpr (DW) *reinterpret_cast<v4u*>(tile + permuted(kRowsAtOnce * i + t / kAcross, t % kAcross)) = kept[i];
             else *reinterpret_cast<v4u*>(tile + 16 * unit_at(32 * i + (t >> 3), t & 7)) = kept[i];
         };
-        // values 2 e and 2 e + 1 of the eight of piece 0..7 (two runs of four)
+        // values 2 e and 2 e + 1 of the eight of a piece, four of which are a run
         v4u decoded;
         float unit;
         auto decode = [&](int piece, int e) __attribute__((always_inline)) {
@@ -114,26 +117,26 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
             }
         };
         auto write_v = [&](uint8_t* tile, int piece) __attribute__((always_inline)) {
-            *reinterpret_cast<v4u*>(tile + permuted(v_row + 32 * (piece >> 2), 4 * (lane & 7) + (piece & 3))) = decoded;
+            *reinterpret_cast<v4u*>(tile + permuted(v_row + 32 * (piece >> 2), 4 * (lane % kBlocks) + (piece & 3))) = decoded;
         };
         // ---- operands: eight neighbouring r of one row or column
         struct Operands {
-            v4u v[4], dy[4];
+            v4u v[kF], dy[kF];
         };
         Operands set[2];
         // A lane's half of operand f: r = 16 q + 8 g + 4 h + (lane / 4) % 4, columns first + 32 f + 16 ((lane / 16) % 2) + 4 (lane % 4) and on.
         auto read_turned = [&](v4u& to, const uint8_t* tile, int first, int f, int q, int h) __attribute__((always_inline)) {
             typedef __attribute__((address_space(3))) v4s* P;
             const int row = 8 * g + 4 * h + ((lane >> 2) & 3), chunk = first / 8 + 4 * f + 2 * ((lane >> 4) & 1) + ((lane >> 1) & 1);
-            const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(tile + permuted(row, chunk) + ((lane & 1) << 3) + q * 16 * 512));
+            const v4s r = __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(tile + permuted(row, chunk) + ((lane & 1) << 3) + q * 16 * kRow));
             const v2u w = __builtin_bit_cast(v2u, r);
             to[2 * h] = w[0];
             to[2 * h + 1] = w[1];
         };
-        constexpr int kReads = DW ? 16 : 12;
+        constexpr int kReads = kF * (DW ? 4 : 3);
         // read n of a quarter's kReads, in the order the products need them: the first fragment of V, all of dy, the rest of V
         auto read = [&](Operands& o, const uint8_t* dy_tile, const uint8_t* v_tile, int q, int n) __attribute__((always_inline)) {
-            constexpr int kDy = DW ? 8 : 4;
+            constexpr int kDy = DW ? 2 * kF : kF;
             if (n < 2) read_turned(o.v[0], v_tile, wk, 0, q, n);
             else if (n < 2 + kDy) {
                 n -= 2;
@@ -148,19 +151,22 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
         // What is issued after matrix instruction i of quarter q of a step whose tiles are the first or second of each side.  Between two
         // barriers, quarters 3, 0, 1, 2, the tiles of the step after the later one's are written and those after them asked for.
         auto between = [&](auto now_, int q, int i) __attribute__((always_inline)) {
-            constexpr int now = decltype(now_)::value * kWideBytes;
-            const int part = (q + 1) & 3, piece = 2 * part + (i >> 3);
+            constexpr int now = decltype(now_)::value * kBytes, kPieces = kRuns, kParts = 8 * kPieces;      // pieces a quarter, eight parts each
+            const int part = (q + 1) & 3;
             if (q == 3 && i == 0) advance();
-            const int read_from = q == 3 ? now ^ kWideBytes : now, write_to = q == 3 ? now : now ^ kWideBytes;
-            for (int n = i * kReads / 16; n < (i + 1) * kReads / 16; ++n) read(set[(q + 1) & 1], lds_dy + read_from, lds_v + read_from, (q + 1) & 3, n);
-            if ((i & 1) == 0) decode(piece, (i & 7) >> 1);
-            if ((i & 7) == 7) {
-                write_v(lds_v + write_to, piece);
-                if ((piece & 3) == 3) load_v(piece >> 2);
-            }
-            if ((i & 7) == 3) {
-                write_dy(lds_dy + write_to, piece);
-                load_dy(piece);
+            const int read_from = q == 3 ? now ^ kBytes : now, write_to = q == 3 ? now : now ^ kBytes;
+            for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from, lds_v + read_from, (q + 1) & 3, n);
+            for (int u = i * kParts / kSlots; u < (i + 1) * kParts / kSlots; ++u) {
+                const int piece = part * kPieces + u / 8;
+                if (u % 2 == 0) decode(piece, u % 8 / 2);
+                if (u % 8 == 7) {
+                    write_v(lds_v + write_to, piece);
+                    if ((piece & 3) == 3) load_v(piece >> 2);
+                }
+                if (u % 8 == 3) {
+                    write_dy(lds_dy + write_to, piece);
+                    load_dy(piece);
+                }
             }
         };
         auto barrier = [&]() __attribute__((always_inline)) {
@@ -175,24 +181,25 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
                 if (q == 3) barrier();                       // the next step's tiles are written, this step's read
                 const Operands& o = set[q & 1];
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < kF; ++x)
 #pragma unroll
-                    for (int y = 0; y < 4; ++y) {
+                    for (int y = 0; y < kF; ++y) {
                         products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[y]),
                                                                                      products.acc[x][y], 0, 0, 0);
-                        between(now, q, 4 * x + y);
+                        between(now, q, kF * x + y);
                         __builtin_amdgcn_sched_barrier(0);
                     }
             }
         };
 
 #pragma unroll
-        for (int i = 0; i < 8; ++i) load_dy(i);
-        load_v(0);
-        load_v(1);
-        advance();
+        for (int i = 0; i < kUnits; ++i) load_dy(i);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
+        for (int i = 0; i < kRuns; ++i) load_v(i);
+        advance();
+        static_assert(kUnits == 4 * kRuns, "a unit of dy to a piece of V");
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) decode(i, e);
             write_v(lds_v, i);
@@ -203,17 +210,17 @@ __global__ __launch_bounds__(kGradThreads, 1) void grad_wide_kernel(O* __restric
         barrier();
         // as if the last quarter of a step before the first
 #pragma unroll
-        for (int i = 0; i < 16; ++i) between(std::integral_constant<int, 1>{}, 3, i);
+        for (int i = 0; i < kSlots; ++i) between(std::integral_constant<int, 1>{}, 3, i);
         for (int s = s_begin; s < s_fast; s += 2) {
             step(std::integral_constant<int, 0>{});
             if (s + 1 < s_fast) step(std::integral_constant<int, 1>{});
         }
     }
-    multiply_rest<__bf16, DW, kWideTile, kWideTile>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
+    multiply_rest<__bf16, DW, TILE, TILE>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, 4, 4, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
+    store_results<O, kF, kF, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
 #endif
 }
 

@@ -212,7 +212,7 @@ def test_product_of_what_is_not_finite(sq, M, N, K):
 
 # ---- the product's gradients ---------------------------------------------------------------------------------------------
 GRAD = [(1, 1, 1), (3, 5, 33), (17, 64, 128), (64, 33, 100), (40, 129, 257), (130, 96, 640), (257, 300, 130), (515, 70, 200), (96, 1030, 64), (1300, 40, 72),
-        (256, 512, 512)]
+        (256, 512, 512), (2100, 70, 96), (70, 2100, 96)]
 
 
 @pytest.mark.parametrize("M,N,K", GRAD)
@@ -237,7 +237,7 @@ def test_product_gradients(sq, M, N, K, t, o, pad, at):
     guard(ws, view)
 
 
-@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400)])
+@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000)])
 @pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2)])
 def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at):
     """dx [J][K] over R outputs, dw [J][K] over R rows."""
