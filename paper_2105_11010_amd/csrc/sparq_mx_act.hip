@@ -23,11 +23,20 @@ __device__ __forceinline__ float sigmoid(float v) {
     if constexpr (PRECISE) return 1.0f / (1.0f + expf(-v));
     else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
 }
+// The normal distribution's integral and exp(-v^2 / 2), for 16-bit results: erfc by Abramowitz and Stegun's formula 7.1.26, a
+// polynomial in 1 / (1 + 0.3275911 |v| / sqrt 2) times that exponential, whose error is 1.5e-7 (half of it in the integral).
+__device__ __forceinline__ float normal_integral(float v, float& density) {
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.231641888f * __builtin_fabsf(v));
+    density = __builtin_amdgcn_exp2f(v * v * -0.721347520f);
+    const float tail = 0.5f * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))) * density;
+    return v < 0.0f ? tail : 1.0f - tail;
+}
 template <int F, bool PRECISE>
 __device__ __forceinline__ float function(float v) {
+    float density;
     if constexpr (F == SPARQ_MX_SILU) return v * sigmoid<PRECISE>(v);
     else if constexpr (PRECISE) return 0.5f * v * erfcf(v * -0.707106781f);
-    else return 0.5f * v * (1.0f + erff(v * 0.707106781f));
+    else return v * normal_integral(v, density);
 }
 template <int F, bool PRECISE>
 __device__ __forceinline__ void function_and_slope(float v, float& value, float& slope) {
@@ -36,15 +45,16 @@ __device__ __forceinline__ void function_and_slope(float v, float& value, float&
         value = v * s;
         slope = s + value * (1.0f - s);
     } else {
-        const float c = PRECISE ? 0.5f * erfcf(v * -0.707106781f) : 0.5f + 0.5f * erff(v * 0.707106781f);
-        const float d = 0.398942280f * (PRECISE ? expf(-0.5f * v * v) : __builtin_amdgcn_exp2f(v * v * -0.721347520f));
+        float density;
+        const float c = PRECISE ? 0.5f * erfcf(v * -0.707106781f) : normal_integral(v, density);
+        if (PRECISE) density = expf(-0.5f * v * v);
         value = v * c;
-        slope = c + v * d;
+        slope = c + v * (0.398942280f * density);
     }
 }
 
 // A wavefront takes 512 values of a row, a lane eight, as the quantiser does.  Bound by memory.
-template <class T, int F, bool UP, bool KEEP>
+template <class T, int F, bool UP, bool KEEP, bool NT>
 __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gate, const T* __restrict__ up, T* __restrict__ y,
                                                        uint8_t* __restrict__ gate_codes, uint8_t* __restrict__ gate_scales,
                                                        uint8_t* __restrict__ up_codes, uint8_t* __restrict__ up_scales, const ActParams p) {
@@ -54,11 +64,11 @@ __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gat
     const uint32_t row = fastdiv(item, p.div_chunks);
     const int col = (int)(item - row * p.chunks) * kScaleUnit + 8 * lane, n = p.K - col;
     float g[8], u[8], o[8];
-    load_upto8(gate + row * p.ldg + col, n, g);
-    if constexpr (UP) load_upto8(up + row * p.ldu + col, n, u);
+    load_upto8<NT>(gate + row * p.ldg + col, n, g);
+    if constexpr (UP) load_upto8<NT>(up + row * p.ldu + col, n, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = function<F, sizeof(T) == 4>(g[i]) * (UP ? u[i] : 1.0f);
-    if (n > 0) store_upto8(y + row * p.ldy + col, n, o);
+    if (n > 0) store_upto8<NT>(y + row * p.ldy + col, n, o);
     if constexpr (KEEP) {
         const int64_t codes_at = row * p.code_pitch + col, scale_at = row * p.scale_pitch + (col >> 5);
         auto keep = [&](const float (&v)[8], uint8_t* codes, uint8_t* scales) __attribute__((always_inline)) {
@@ -73,7 +83,7 @@ __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gat
     }
 }
 
-template <class T, int F, bool UP>
+template <class T, int F, bool UP, bool NT>
 __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ gate_codes,
                                                             const uint8_t* __restrict__ gate_scales, const uint8_t* __restrict__ up_codes,
                                                             const uint8_t* __restrict__ up_scales, T* __restrict__ dgate,
@@ -86,7 +96,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict_
     if (n <= 0) return;
     const int64_t codes_at = row * p.code_pitch + col, scale_at = row * p.scale_pitch + (col >> 5);
     float d[8], g[8], u[8], dg[8], du[8];
-    load_upto8(dy + row * p.ldy + col, n, d);
+    load_upto8<NT>(dy + row * p.ldy + col, n, d);
     values8_of(*reinterpret_cast<const v2u*>(gate_codes + codes_at), gate_scales[scale_at], g);
     if constexpr (UP) values8_of(*reinterpret_cast<const v2u*>(up_codes + codes_at), up_scales[scale_at], u);
 #pragma unroll
@@ -96,8 +106,8 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict_
         dg[i] = (UP ? d[i] * u[i] : d[i]) * slope;
         du[i] = d[i] * value;
     }
-    store_upto8(dgate + row * p.ldg + col, n, dg);
-    if constexpr (UP) store_upto8(dup + row * p.ldu + col, n, du);
+    store_upto8<NT>(dgate + row * p.ldg + col, n, dg);
+    if constexpr (UP) store_upto8<NT>(dup + row * p.ldu + col, n, du);
 }
 
 static bool act_params(int64_t rows, int K, int64_t ldg, int64_t ldu, int64_t ldy, ActParams* p) {
@@ -137,8 +147,11 @@ extern "C" sparq_status sparq_mx_act(int32_t function, const void* gate, int64_t
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
-            if (up) keep ? launch(act_kernel<T, F, true, true>) : launch(act_kernel<T, F, true, false>);
-            else keep ? launch(act_kernel<T, F, false, true>) : launch(act_kernel<T, F, false, false>);
+            with_flag(streamed<T>(rows * K * ((up ? 3 : 2) * (int64_t)sizeof(T) + (gate_codes ? 1 : 0) + (up_codes ? 1 : 0))), [&](auto nt) {
+                constexpr bool NT = decltype(nt)::value;
+                if (up) keep ? launch(act_kernel<T, F, true, true, NT>) : launch(act_kernel<T, F, true, false, NT>);
+                else keep ? launch(act_kernel<T, F, false, true, NT>) : launch(act_kernel<T, F, false, false, NT>);
+            });
         };
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});
         else of(std::integral_constant<int, SPARQ_MX_GELU>{});
@@ -168,7 +181,10 @@ extern "C" sparq_status sparq_mx_act_grad(int32_t function, const void* dy, int6
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
-            up ? launch(act_grad_kernel<T, F, true>) : launch(act_grad_kernel<T, F, false>);
+            with_flag(streamed<T>(rows * K * ((up ? 3 : 2) * (int64_t)sizeof(T) + (up ? 2 : 1))), [&](auto nt) {
+                constexpr bool NT = decltype(nt)::value;
+                up ? launch(act_grad_kernel<T, F, true, NT>) : launch(act_grad_kernel<T, F, false, NT>);
+            });
         };
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});
         else of(std::integral_constant<int, SPARQ_MX_GELU>{});

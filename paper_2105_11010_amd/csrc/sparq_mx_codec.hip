@@ -17,7 +17,7 @@ struct CodecParams {
 // A wavefront takes 512 values of one row, a lane eight of them, so that a block is four neighbouring lanes: the block's
 // largest magnitude is two exchanges inside a quad, loads are 16 bytes a lane (fp32: twice), codes leave as 4 and 8 bytes a
 // lane and the 16 scales as one byte of every fourth lane.  Bound by memory.
-template <class T, bool F4, bool I8>
+template <class T, bool F4, bool I8, bool NT>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict__ x, uint8_t* __restrict__ codes4,
                                                             uint8_t* __restrict__ scales4, uint8_t* __restrict__ codes8,
                                                             uint8_t* __restrict__ scales8, const CodecParams p) {
@@ -27,7 +27,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict_
     const uint32_t row = fastdiv(item, p.div_chunks);
     const int col = (int)(item - row * p.chunks) * kScaleUnit + 8 * lane;
     float v[8];
-    load_upto8(x + row * p.ld + col, p.K - col, v);
+    load_upto8<NT>(x + row * p.ld + col, p.K - col, v);
     const uint32_t top = block_top(v);
     const int64_t scale_at = row * p.scale_pitch + (col >> 5);
     if constexpr (F4) {
@@ -43,20 +43,40 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict_
     }
 }
 
-template <class T, int BITS>
+template <class T, int BITS, bool NT>
 __global__ __launch_bounds__(kThreads) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                               T* __restrict__ y, const CodecParams p) {
     const int lane = threadIdx.x & 63;
     const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= p.items) return;
     const uint32_t row = fastdiv(item, p.div_chunks);
+    if constexpr (sizeof(T) == 4) {
+        // 32 bytes a lane would be two stores that each leave half of every line: four values of either half of the 512 instead.
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int col = (int)(item - row * p.chunks) * kScaleUnit + 256 * h + 4 * lane, n = p.K - col;
+            if (n <= 0) return;
+            const uint32_t byte = scales[row * p.scale_pitch + (col >> 5)];
+            float v[8];
+            if constexpr (BITS == 4) values4_of(*reinterpret_cast<const uint16_t*>(codes + row * p.code4_pitch + (col >> 1)), byte, v);
+            else values8_of(v2u{*reinterpret_cast<const uint32_t*>(codes + row * p.code8_pitch + col), 0}, byte, v);
+            T* to = y + row * p.ld + col;
+            if (n >= 4) word_to<NT>(to, v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+            else {
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+                    if (i < n) to[i] = v[i];
+            }
+        }
+        return;
+    }
     const int col = (int)(item - row * p.chunks) * kScaleUnit + 8 * lane;
     if (col >= p.K) return;
     const uint32_t byte = scales[row * p.scale_pitch + (col >> 5)];
     float v[8];
     if constexpr (BITS == 4) values4_of(*reinterpret_cast<const uint32_t*>(codes + row * p.code4_pitch + (col >> 1)), byte, v);
     else values8_of(*reinterpret_cast<const v2u*>(codes + row * p.code8_pitch + col), byte, v);
-    store_upto8(y + row * p.ld + col, p.K - col, v);
+    store_upto8<NT>(y + row * p.ld + col, p.K - col, v);
 }
 
 // false: more rows than a launch counts
@@ -75,9 +95,12 @@ sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows,
     const uint32_t grid = (p.items + kWaves - 1) / kWaves;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const auto kernel = codes4 && codes8 ? quantize_kernel<T, true, true> : codes4 ? quantize_kernel<T, true, false> : quantize_kernel<T, false, true>;
-        kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(x), static_cast<uint8_t*>(codes4), static_cast<uint8_t*>(scales4),
-                                              static_cast<uint8_t*>(codes8), static_cast<uint8_t*>(scales8), p);
+        with_flag(streamed<T>(rows * (K * (int64_t)sizeof(T) + (codes4 ? p.code4_pitch : 0) + (codes8 ? p.code8_pitch : 0))), [&](auto nt) {
+            constexpr bool NT = decltype(nt)::value;
+            const auto kernel = codes4 && codes8 ? quantize_kernel<T, true, true, NT> : codes4 ? quantize_kernel<T, true, false, NT> : quantize_kernel<T, false, true, NT>;
+            kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(x), static_cast<uint8_t*>(codes4), static_cast<uint8_t*>(scales4),
+                                                  static_cast<uint8_t*>(codes8), static_cast<uint8_t*>(scales8), p);
+        });
     });
     return launch_status();
 }
@@ -113,8 +136,11 @@ extern "C" sparq_status sparq_mx_dequantize(const void* codes, const void* scale
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const auto kernel = bits == 4 ? dequantize_kernel<T, 4> : dequantize_kernel<T, 8>;
-        kernel<<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<T*>(y), p);
+        with_flag(rows * (K * (int64_t)sizeof(T) + code_pitch(K, bits)) >= kStreamedBytes, [&](auto nt) {
+            constexpr bool NT = decltype(nt)::value;
+            const auto kernel = bits == 4 ? dequantize_kernel<T, 4, NT> : dequantize_kernel<T, 8, NT>;
+            kernel<<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<T*>(y), p);
+        });
     });
     return launch_status();
 }

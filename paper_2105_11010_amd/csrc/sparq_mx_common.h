@@ -1,6 +1,8 @@
 // What the kernels of the microscaled formats share: element types, rows of codes and scales, both quantisers in
 // registers, and the argument checks of their entry points.
 #pragma once
+#include <type_traits>
+
 #include "../../include/sparq_mx.h"
 #include "sparq_common.h"
 #include "sparq_fastdiv.h"
@@ -39,6 +41,17 @@ inline bool sizes_ok(int64_t rows, int64_t K) { return rows >= 0 && K >= 1 && K 
 // rows * pitch bytes and rows * ld elements stay inside 64 bits
 inline bool extent_ok(int64_t rows, int64_t ld) { return rows == 0 || ld <= (INT64_MAX / 8) / rows; }
 
+// A call that moves this many bytes streams them past the caches (us, kept -> streamed: 16384 x 8192 bf16 from 4-bit codes 72 -> 47, the gated
+// activation of 8192 x 8192 94 -> 83; 16384 x 4096 bf16 to 4-bit codes, 174 MB, 27 -> 31, and what follows a smaller call finds it there).
+// Not fp32 tensors, whose lanes' halves of 32 bytes go one after the other (16384 x 4096 from 4-bit codes 70 -> 104).
+template <class T>
+inline bool streamed(int64_t bytes) { return sizeof(T) == 2 && bytes >= kStreamedBytes; }
+template <class F>
+inline void with_flag(bool flag, F&& f) {
+    if (flag) f(std::true_type{});
+    else f(std::false_type{});
+}
+
 template <class F>
 inline void with_type(int type, F&& f) {
     if (type == SPARQ_MX_F32) f(float{});
@@ -51,24 +64,40 @@ inline void with_type(int type, F&& f) {
 typedef v4u v4u_at4 __attribute__((aligned(4)));
 typedef v4u v4u_at2 __attribute__((aligned(2)));
 
+// NT: non-temporal, for what is streamed once and is larger than the last-level cache (streamed below).
+template <bool NT, class T>
+__device__ __forceinline__ v4u word_at(const T* p) {
+    typedef std::conditional_t<sizeof(T) == 4, const v4u_at4, const v4u_at2> V;
+    if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<V*>(p));
+    else return *reinterpret_cast<V*>(p);
+}
+template <bool NT, class T>
+__device__ __forceinline__ void word_to(T* p, v4u w) {
+    typedef std::conditional_t<sizeof(T) == 4, v4u_at4, v4u_at2> V;
+    if constexpr (NT) __builtin_nontemporal_store(w, reinterpret_cast<V*>(p));
+    else *reinterpret_cast<V*>(p) = w;
+}
+template <bool NT = false>
 __device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-    const v4u a = *reinterpret_cast<const v4u_at4*>(p), b = *reinterpret_cast<const v4u_at4*>(p + 4);
+    const v4u a = word_at<NT>(p), b = word_at<NT>(p + 4);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[i] = __uint_as_float(a[i]);
         v[4 + i] = __uint_as_float(b[i]);
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void load8(const __bf16* p, float (&v)[8]) {
-    const v4u a = *reinterpret_cast<const v4u_at2*>(p);
+    const v4u a = word_at<NT>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         v[2 * i] = __uint_as_float(a[i] << 16);
         v[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
     }
 }
+template <bool NT = false>
 __device__ __forceinline__ void load8(const _Float16* p, float (&v)[8]) {
-    const v4u a = *reinterpret_cast<const v4u_at2*>(p);
+    const v4u a = word_at<NT>(p);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const uint32_t w = a[i];                     // (a copy: the bits of a vector's element cannot be taken in place)
@@ -78,9 +107,9 @@ __device__ __forceinline__ void load8(const _Float16* p, float (&v)[8]) {
     }
 }
 // ... of which the first n are there
-template <class T>
+template <bool NT = false, class T>
 __device__ __forceinline__ void load_upto8(const T* p, int n, float (&v)[8]) {
-    if (n >= 8) load8(p, v);
+    if (n >= 8) load8<NT>(p, v);
     else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
@@ -92,15 +121,13 @@ template <class T>
 struct Raw8 {
     uint32_t w[2 * sizeof(T)];
 };
-template <class T>
-__device__ __forceinline__ void load_raw(const T* p, int n, Raw8<T>& r) {
-    if (n >= 8) {
-        __builtin_memcpy(&r, p, sizeof(r));
-    } else {
-        T v[8];
+template <bool NT, class T>
+__device__ __forceinline__ void load_raw(const T* p, Raw8<T>& r) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : (T)0.0f;
-        __builtin_memcpy(&r, v, sizeof(r));
+    for (int h = 0; h < (int)sizeof(T) / 2; ++h) {
+        const v4u w = word_at<NT>(p + 4 * h);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[4 * h + i] = w[i];
     }
 }
 template <class T>
@@ -118,13 +145,14 @@ __device__ __forceinline__ void values_of(const Raw8<T>& r, float (&v)[8]) {
 // Rounded to nearest even by the conversion instructions.
 __device__ __forceinline__ uint32_t pack2(float a, float b, __bf16) { return __builtin_bit_cast(uint32_t, v2bf{(__bf16)a, (__bf16)b}); }
 __device__ __forceinline__ uint32_t pack2(float a, float b, _Float16) { return __builtin_bit_cast(uint32_t, v2h{(_Float16)a, (_Float16)b}); }
-template <class T>
+template <bool NT = false, class T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
     v4u a;
 #pragma unroll
     for (int i = 0; i < 4; ++i) a[i] = pack2(v[2 * i], v[2 * i + 1], T{});
-    *reinterpret_cast<v4u_at2*>(p) = a;
+    word_to<NT>(p, a);
 }
+template <bool NT = false>
 __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
     v4u a, b;
 #pragma unroll
@@ -132,12 +160,12 @@ __device__ __forceinline__ void store8(float* p, const float (&v)[8]) {
         a[i] = __float_as_uint(v[i]);
         b[i] = __float_as_uint(v[4 + i]);
     }
-    *reinterpret_cast<v4u_at4*>(p) = a;
-    *reinterpret_cast<v4u_at4*>(p + 4) = b;
+    word_to<NT>(p, a);
+    word_to<NT>(p + 4, b);
 }
-template <class T>
+template <bool NT = false, class T>
 __device__ __forceinline__ void store_upto8(T* p, int n, const float (&v)[8]) {
-    if (n >= 8) store8(p, v);
+    if (n >= 8) store8<NT>(p, v);
     else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)

@@ -62,10 +62,10 @@ __device__ __forceinline__ Place place_of(int col, int K) {
 // own(i): element i is the lane's
 template <bool WHOLE>
 __device__ __forceinline__ bool own(const Place& p, int i) { return p.inside && (WHOLE || i >= p.skip); }
-template <bool WHOLE, class T>
+template <bool WHOLE, bool NT = false, class T>
 __device__ __forceinline__ void store_own(T* row, const Place& p, const float (&v)[8]) {
     if (!p.inside) return;
-    if (WHOLE || p.skip == 0) store8(row + p.from, v);
+    if (WHOLE || p.skip == 0) store8<NT>(row + p.from, v);
     else {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
@@ -84,7 +84,7 @@ __device__ __forceinline__ void first_own(const Place& p, float (&v)[8]) {
 // WAVES wavefronts take a row of at least eight, CHUNKS x 8 values a lane, which stay in registers from the load to the result: one
 // pass over memory, the mean first and the squares of what differs from it second.  As many workgroups as have room go through the rows,
 // gamma and beta in registers and the next row on its way while this one is summed.
-template <class T, int WAVES, int CHUNKS, bool WHOLE>
+template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
                                                         float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
@@ -101,7 +101,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x,
     auto fetch = [&](int64_t row) __attribute__((always_inline)) {
         row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) load_raw(x + row * p.ldx + at[c].from, 8, raw[c]);
+        for (int c = 0; c < CHUNKS; ++c) load_raw<NT>(x + row * p.ldx + at[c].from, raw[c]);
     };
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
@@ -142,7 +142,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x,
             float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = (v[c][i] - mean) * rstd * g[c][i] + b[c][i];
-            store_own<WHOLE>(y + row * p.ldy, at[c], o);
+            store_own<WHOLE, NT>(y + row * p.ldy, at[c], o);
             if (codes && at[c].col - 8 * lane < p.K) {       // the wavefront's 512 values begin inside the row
                 if constexpr (!WHOLE) first_own(at[c], v[c]);
                 if (!at[c].inside) {
@@ -215,7 +215,7 @@ struct NormGradParams {
 // dx, and the workgroup's share of the weights' gradients, in one pass: WAVES wavefronts take a row, CHUNKS x 8 values a lane, rows part,
 // part + parts, ..., the next row on its way while this one is summed and written.  What the workgroup's wavefronts added up is joined in
 // LDS in their order and leaves as one partial sum.
-template <class T, int WAVES, int CHUNKS, bool WHOLE>
+template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, const float* __restrict__ gamma, T* __restrict__ dx,
@@ -242,7 +242,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict
         row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            load_raw(dy + row * p.ldy + at[c].from, 8, h.dy[c]);
+            load_raw<NT>(dy + row * p.ldy + at[c].from, h.dy[c]);
             __builtin_memcpy(&h.x[c], codes + row * p.code_pitch + at[c].from, 8);
             h.scale[c] = scales[row * p.scale_pitch + ((at[c].inside ? at[c].col : at[c].from) >> 5)];
         }
@@ -296,7 +296,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict
                 dg[c][i] += d[c][i] * h[c][i];
                 db[c][i] += d[c][i];
             }
-            store_own<WHOLE>(dx + row * p.ldx, at[c], o);
+            store_own<WHOLE, NT>(dx + row * p.ldx, at[c], o);
         }
     }
     if (!partial) return;
@@ -426,17 +426,17 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
                 static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, static_cast<uint8_t*>(codes),
                 static_cast<uint8_t*>(scales), p);
         };
-        const auto held = [&](auto whole) {
-            constexpr bool W = decltype(whole)::value;
-            if (K <= 512) launch(norm_kernel<T, 1, 1, W>, 4, 8);
-            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W>, 4, 5);
-            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W>, 1, 8);
-            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W>, 1, 5);
-            else launch(norm_kernel<T, 4, 4, W>, 1, 3);
+        const auto held = [&](auto whole, auto nt) {
+            constexpr bool W = decltype(whole)::value, NT = decltype(nt)::value;
+            if (K <= 512) launch(norm_kernel<T, 1, 1, W, NT>, 4, 8);
+            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W, NT>, 4, 5);
+            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W, NT>, 1, 8);
+            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W, NT>, 1, 5);
+            else launch(norm_kernel<T, 4, 4, W, NT>, 1, 3);
         };
         if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1, 0);
-        else if (K % 8 == 0) held(std::true_type{});
-        else held(std::false_type{});
+        else if (K % 8 == 0) with_flag(streamed<T>(rows * K * (2 * (int64_t)sizeof(T) + (codes ? 1 : 0))), [&](auto nt) { held(std::true_type{}, nt); });
+        else held(std::false_type{}, std::false_type{});
     });
     return launch_status();
 }
@@ -469,16 +469,18 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
         const T* from = static_cast<const T*>(dy);
         T* to = static_cast<T*>(dx);
         const auto launch = [&](auto kernel) { kernel<<<p.parts, kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, to, partial, p); };
-        const auto held = [&](auto whole) {
-            constexpr bool W = decltype(whole)::value;
-            if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W>);
-            else if (K <= kWaveK) launch(norm_grad_kernel<T, 1, 2, W>);
-            else if (K <= 2048) launch(norm_grad_kernel<T, 4, 1, W>);
-            else if (K <= 4096) launch(norm_grad_kernel<T, 4, 2, W>);
-            else launch(norm_grad_kernel<T, 4, 4, W>);
+        const auto held = [&](auto whole, auto nt) {
+            constexpr bool W = decltype(whole)::value, NT = decltype(nt)::value;
+            if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W, NT>);
+            else if (K <= kWaveK) launch(norm_grad_kernel<T, 1, 2, W, NT>);
+            else if (K <= 2048) launch(norm_grad_kernel<T, 4, 1, W, NT>);
+            else if (K <= 4096) launch(norm_grad_kernel<T, 4, 2, W, NT>);
+            else launch(norm_grad_kernel<T, 4, 4, W, NT>);
         };
-        if (held_in_registers(K)) K % 8 == 0 ? held(std::true_type{}) : held(std::false_type{});
-        else {
+        if (held_in_registers(K)) {
+            if (K % 8 == 0) with_flag(streamed<T>(rows * K * (2 * (int64_t)sizeof(T) + 1)), [&](auto nt) { held(std::true_type{}, nt); });
+            else held(std::false_type{}, std::false_type{});
+        } else {
             norm_grad_rows_kernel<T><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, sums, p);
             norm_grad_columns_kernel<T><<<dim3((unsigned)((K + 8ll * kThreads - 1) / (8 * kThreads)), p.parts), kThreads, 0, s>>>(
                 from, c, sc, mean, rstd, gamma, sums, to, partial, p);
