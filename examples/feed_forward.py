@@ -5,7 +5,7 @@
 Products run on 4-bit operands; what the backward pass reads again -- the norm's input, the layers' inputs, the gate and what it
 gates -- is kept in 8 bits.  Weights are fp32 between the steps and quantised once per step (when served: once).
 
-    python examples/feed_forward.py [--tokens 4096] [--width 1024] [--hidden 4096] [--steps 20]
+    python examples/feed_forward.py [--tokens 4096] [--width 1024] [--hidden 4096] [--steps 16]
 """
 import argparse
 import os
@@ -124,7 +124,7 @@ def train_and_serve(tokens, width, hidden, steps, rate=0.2):
 
 def main():
     p = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
-    for name, default in (("tokens", 4096), ("width", 1024), ("hidden", 4096), ("steps", 20)):
+    for name, default in (("tokens", 4096), ("width", 1024), ("hidden", 4096), ("steps", 16)):
         p.add_argument("--" + name, type=int, default=default)
     a = p.parse_args()
     losses, apart = train_and_serve(a.tokens, a.width, a.hidden, a.steps)

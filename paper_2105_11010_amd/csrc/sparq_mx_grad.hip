@@ -68,8 +68,8 @@ static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
     const size_t a = grad_plan(false, J, R, K, dw).bytes, b = grad_plan(true, J, R, K, dw).bytes;
     return a > b ? a : b;
 }
-static bool wide_fits(const void* dy, int dy_type, int64_t lddy, int64_t J, int64_t R, int K, bool dw) {
-    return dy_type == SPARQ_MX_BF16 && R < (1ll << 36) && (dw ? grad_wide_fits<true>(dy, lddy, J, code_pitch(K, 8)) : grad_wide_fits<false>(dy, lddy, J, code_pitch(K, 4)));
+static bool wide_fits(int dy_type, int64_t lddy, int64_t J, int64_t R, int K, bool dw) {
+    return dy_type == SPARQ_MX_BF16 && R < (1ll << 36) && (dw ? grad_wide_fits<true>(lddy, J, code_pitch(K, 8)) : grad_wide_fits<false>(lddy, J, code_pitch(K, 4)));
 }
 
 static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
@@ -121,7 +121,7 @@ extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int6
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
     if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan(wide_fits(dy, dy_type, lddy, M, N, K, false), M, N, K, false);
+    const GradPlan plan = grad_plan(wide_fits(dy_type, lddy, M, N, K, false), M, N, K, false);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
@@ -134,7 +134,7 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (!tensor_ok(dw, dw_type, lddw, K) || !extent_ok(N, lddw) || !aligned(db, 4)) return SPARQ_EINVAL;
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K)))
         return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan(wide_fits(dy, dy_type, lddy, N, M, K, true), N, M, K, true);
+    const GradPlan plan = grad_plan(wide_fits(dy_type, lddy, N, M, K, true), N, M, K, true);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);

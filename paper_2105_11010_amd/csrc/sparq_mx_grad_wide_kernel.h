@@ -18,11 +18,10 @@ namespace mx {
 
 template <int TILE> inline constexpr int kWideBytes = kGradStep * TILE * 2;       // of one side's tile
 
-// A call this kernel is for: whole words of dy, rows whose distances fit the loads' 32-bit offsets, and no run of eight columns (DW) that the
-// last column cuts.
+// A call this kernel is for: rows whose distances fit the loads' 32-bit offsets, and at least eight columns (DW).
 template <bool DW>
-inline bool grad_wide_fits(const void* dy, int64_t lddy, int64_t J, int64_t code_pitch) {
-    return aligned(dy, 4) && lddy % 2 == 0 && lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J % 8 == 0);
+inline bool grad_wide_fits(int64_t lddy, int64_t J, int64_t code_pitch) {
+    return lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J >= 8);
 }
 
 template <class O, bool DW, int TILE>
@@ -39,8 +38,10 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
     const int64_t j0 = (int64_t)tj * TILE;
     const int k0 = (int)tk * TILE;
-    const int s_begin = (int)blockIdx.y * p.steps_per_part, s_all = (int)((p.R + kGradStep - 1) / kGradStep), s_whole = (int)(p.R / kGradStep);
+    const int s_begin = (int)blockIdx.y * p.steps_per_part, s_all = (int)((p.R + kGradStep - 1) / kGradStep), s_whole = (int)((DW && p.J % 8 ? p.R - 1 : p.R) / kGradStep);
     const int s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = s_whole < s_end ? s_whole : s_end;
+    // (Steps before s_whole are loaded without checks.  A run of eight columns that the last column cuts reads on into the next row, so the
+    // last row is not among them then.)
     Products<1, TILE, TILE> products;
     const int wj = products.wj, wk = products.wk;
 
@@ -51,7 +52,7 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
         uint32_t dy_at[DW ? 1 : kUnits];
         if constexpr (DW) {
             int64_t j = j0 + 8 * (t % kAcross);
-            j = j < p.J ? j : p.J - 8;                       // (columns past the last one make results that are not stored)
+            j = j < p.J ? j : j0;                            // (columns past the last one make results that are not stored)
             dy_at[0] = (uint32_t)((t / kAcross * p.lddy + (j - j0)) * 2);
         } else {
             const int64_t last = p.J - 1 - j0;

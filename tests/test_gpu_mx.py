@@ -237,8 +237,8 @@ def test_product_gradients(sq, M, N, K, t, o, pad, at):
     guard(ws, view)
 
 
-@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000)])
-@pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2)])
+@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000), (4099, 257, 3201), (2049, 129, 1730), (261, 3300, 3000)])
+@pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2), ("f16", 4, 1)])
 def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at):
     """dx [J][K] over R outputs, dw [J][K] over R rows."""
     g = rng(13, J, R, K)
