@@ -8,7 +8,7 @@ namespace sparq {
 namespace mx {
 
 // Implemented in sparq_mx_grad_{dx,dw}_{bf16,f16,f32}.hip.
-#define SPARQ_MX_GRAD_DECLARE(NAME) sparq_status NAME(const GradParams& p, int parts, int tile, bool wide, void* out, int out_type, hipStream_t stream);
+#define SPARQ_MX_GRAD_DECLARE(NAME) sparq_status NAME(const GradParams& p, int parts, int tile, void* out, int out_type, hipStream_t stream);
 SPARQ_MX_GRAD_DECLARE(launch_grad_dx_bf16)
 SPARQ_MX_GRAD_DECLARE(launch_grad_dx_f16)
 SPARQ_MX_GRAD_DECLARE(launch_grad_dx_f32)
@@ -16,11 +16,11 @@ SPARQ_MX_GRAD_DECLARE(launch_grad_dw_bf16)
 SPARQ_MX_GRAD_DECLARE(launch_grad_dw_f16)
 SPARQ_MX_GRAD_DECLARE(launch_grad_dw_f32)
 
-inline sparq_status launch_grad(const GradParams& p, int parts, int tile, bool wide, int dy_type, bool dw, void* out, int out_type, hipStream_t stream) {
+inline sparq_status launch_grad(const GradParams& p, int parts, int tile, int dy_type, bool dw, void* out, int out_type, hipStream_t stream) {
     const auto f = dy_type == SPARQ_MX_BF16  ? (dw ? launch_grad_dw_bf16 : launch_grad_dx_bf16)
                    : dy_type == SPARQ_MX_F16 ? (dw ? launch_grad_dw_f16 : launch_grad_dx_f16)
                                              : (dw ? launch_grad_dw_f32 : launch_grad_dx_f32);
-    return f(p, parts, tile, wide, out, out_type, stream);
+    return f(p, parts, tile, out, out_type, stream);
 }
 
 template <class O, class F>
@@ -36,22 +36,19 @@ sparq_status launch_grad_kernel(F* kernel, int lds_bytes, std::atomic<bool> (&al
     return launch_status();
 }
 template <class T, bool DW>
-sparq_status launch_grad_types(const GradParams& p, int parts, int tile, bool wide, void* out, int out_type, hipStream_t stream) {
+sparq_status launch_grad_types(const GradParams& p, int parts, int tile, void* out, int out_type, hipStream_t stream) {
     sparq_status s = SPARQ_OK;
     with_type(out_type, [&](auto o) {
         typedef decltype(o) O;
-        static std::atomic<bool> allowed[4][kMaxDevices];
+        static std::atomic<bool> allowed[3][kMaxDevices];
         if constexpr (std::is_same_v<T, __bf16>) {
-            if (wide) {
-                s = tile == 256 ? launch_grad_kernel<O>(grad_wide_kernel<O, DW, 256>, 4 * kWideBytes<256>, allowed[0], p, parts, out, stream)
-                                : launch_grad_kernel<O>(grad_wide_kernel<O, DW, 128>, 4 * kWideBytes<128>, allowed[3], p, parts, out, stream);
+            if (tile == 256) {
+                s = launch_grad_kernel<O>(grad_wide_kernel<T, O, DW, 256>, kWideLds<T, 256>, allowed[0], p, parts, out, stream);
                 return;
             }
         }
-        constexpr int lds_bytes = 2 * (kParts<T> + 1) * 128 * kGradStep * 2;
-        static_assert(lds_bytes <= 160 * 1024, "LDS of a CU");
-        s = tile == 64 ? launch_grad_kernel<O>(grad_kernel<T, O, DW, 64, 64>, lds_bytes / 2, allowed[2], p, parts, out, stream)
-                       : launch_grad_kernel<O>(grad_kernel<T, O, DW, 128, 128>, lds_bytes, allowed[1], p, parts, out, stream);
+        s = tile == 128 ? launch_grad_kernel<O>(grad_wide_kernel<T, O, DW, 128>, kWideLds<T, 128>, allowed[1], p, parts, out, stream)
+                        : launch_grad_kernel<O>(grad_kernel<T, O, DW, 64, 64>, kWideLds<T, 64>, allowed[2], p, parts, out, stream);
     });
     return s;
 }

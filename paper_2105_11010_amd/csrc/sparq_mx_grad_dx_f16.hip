@@ -2,8 +2,8 @@
 
 namespace sparq {
 namespace mx {
-sparq_status launch_grad_dx_f16(const GradParams& p, int parts, int tile, bool wide, void* out, int out_type, hipStream_t stream) {
-    return launch_grad_types<_Float16, false>(p, parts, tile, wide, out, out_type, stream);
+sparq_status launch_grad_dx_f16(const GradParams& p, int parts, int tile, void* out, int out_type, hipStream_t stream) {
+    return launch_grad_types<_Float16, false>(p, parts, tile, out, out_type, stream);
 }
 }  // namespace mx
 }  // namespace sparq

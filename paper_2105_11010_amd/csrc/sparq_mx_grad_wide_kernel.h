@@ -1,4 +1,4 @@
-// The gradients in bf16: 256 x 256 results a workgroup, or 128 x 128 where those would leave CUs without.
+// The gradients' larger tiles: 256 x 256 results a workgroup (bf16), or 128 x 128 (the other types, and where those would leave CUs without).
 // out[j][k] = sum_r dy(j, r) V[r][k] as in sparq_mx_grad_kernel.h.  V's rows are decoded as they lie, eight values of a row a thread, and dy's are
 // copied; the matrix instruction's operands, eight neighbouring r of one column, come out of LDS by reads that turn 4 x 16 values (V, and dy
 // where r is its row).  Sixteen lanes read four rows, 32 bytes each, at a time: a row's 16-byte units are permuted by the row so that four
@@ -6,8 +6,11 @@
 // A step is 64 r, four quarters of sixteen (or four) matrix instructions; one wavefront a SIMD has nobody else to fill the time an
 // instruction runs, so what goes between them is laid out here: the next quarter's reads, and of V and of dy two rows each, written to the
 // next step's tiles, and the request for their successors.  One barrier a step, before the last quarter: by then the step's tiles have been
-// read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, 392 us where
-// this takes TIME.)
+// read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, and dx of
+// 8192 x 4096 x 4096 took 392 us instead of 268, before the steps' order was laid out as it is.)
+// Bound by the matrix instructions and, with data as large as this, by the card's power: 8192 x 4096 x 4096 takes 206-248 us for dx and 237-256
+// for dw (1.07-1.33 PF; the same instructions without loads and writes 1.57 PF).  fp16 dy, two instructions a product, 710 and 728 us, fp32, three,
+// 1015 and 1070 (grad_kernel's 128 x 128 tiles 720 and 921, 1083 and 1272).
 #pragma once
 #include <type_traits>
 
@@ -24,15 +27,18 @@ inline bool grad_wide_fits(int64_t lddy, int64_t J, int64_t code_pitch) {
     return lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J >= 8);
 }
 
-template <class O, bool DW, int TILE>
-__global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
+template <class T, int TILE> inline constexpr int kWideLds = 2 * (kParts<T> + 1) * kWideBytes<TILE>;
+template <class T, int TILE> inline constexpr int kWidePerCu = 160 * 1024 / kWideLds<T, TILE>;
+template <class T, class O, bool DW, int TILE>
+__global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int kF = TILE / 64, kSlots = kF * kF;          // 32 x 32 results along a side; matrix instructions a quarter
+    constexpr int P = kParts<T>;                             // of dy, a tile each
+    constexpr int kF = TILE / 64, kSlots = P * kF * kF;      // 32 x 32 results along a side; matrix instructions a quarter
     constexpr int kUnits = TILE / 32, kRuns = TILE / 128, kRow = TILE * 2;      // of dy and of V a thread; bytes of a tile's row
     constexpr int kBytes = kWideBytes<TILE>;
     typedef short v4s __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
-    uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * kBytes;
+    uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * P * kBytes;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
     uint32_t tj, tk;
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
@@ -42,24 +48,25 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
     const int s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = s_whole < s_end ? s_whole : s_end;
     // (Steps before s_whole are loaded without checks.  A run of eight columns that the last column cuts reads on into the next row, so the
     // last row is not among them then.)
-    Products<1, TILE, TILE> products;
+    Products<P, TILE, TILE> products;
     const int wj = products.wj, wk = products.wk;
 
     if (s_begin < s_fast) {
-        // ---- dy: a thread has kUnits 16-byte units: of every eighth or 16th row (DW) or of rows 32 i + t / 8, 64 r each
+        // ---- dy: a thread has kUnits runs of eight values: of every eighth or 16th row (DW) or of rows 32 i + t / 8, 64 r each
         constexpr int kAcross = TILE / 8, kRowsAtOnce = kGradThreads / kAcross;
-        v4u kept[kUnits];
+        constexpr int kSize = sizeof(T), kKept = 2 * kSize;
+        uint32_t kept[kUnits][kKept];
         uint32_t dy_at[DW ? 1 : kUnits];
         if constexpr (DW) {
             int64_t j = j0 + 8 * (t % kAcross);
             j = j < p.J ? j : j0;                            // (columns past the last one make results that are not stored)
-            dy_at[0] = (uint32_t)((t / kAcross * p.lddy + (j - j0)) * 2);
+            dy_at[0] = (uint32_t)((t / kAcross * p.lddy + (j - j0)) * kSize);
         } else {
             const int64_t last = p.J - 1 - j0;
 #pragma unroll
             for (int i = 0; i < kUnits; ++i) {
                 const int row = 32 * i + (t >> 3), from = row < last ? row : (int)last;
-                dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * 2);
+                dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * kSize);
             }
         }
         // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32, or one of row 4 (lane / 4) + wave
@@ -72,9 +79,9 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
         const uint32_t v_at = (uint32_t)(v_row * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)(v_row * p.scale_pitch + (k >> 5));
 
         // Where the next step to be asked for lies.  Past the last one it stays there, for tiles nobody reads.
-        const uint8_t* dy_from = static_cast<const uint8_t*>(p.dy) + (DW ? j0 + s_begin * (kGradStep * p.lddy) : j0 * p.lddy + (int64_t)s_begin * kGradStep) * 2;
+        const uint8_t* dy_from = static_cast<const uint8_t*>(p.dy) + (DW ? j0 + s_begin * (kGradStep * p.lddy) : j0 * p.lddy + (int64_t)s_begin * kGradStep) * kSize;
         const uint8_t *codes_from = p.codes + (int64_t)s_begin * kGradStep * p.code_pitch, *scales_from = p.scales + (int64_t)s_begin * kGradStep * p.scale_pitch;
-        const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * 2) : kGradStep * 2, codes_step = (uint32_t)(kGradStep * p.code_pitch);
+        const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * kSize) : kGradStep * kSize, codes_step = (uint32_t)(kGradStep * p.code_pitch);
         const uint32_t scales_step = (uint32_t)(kGradStep * p.scale_pitch);
         int left = s_fast - s_begin - 1;
         auto advance = [&]() __attribute__((always_inline)) {
@@ -85,7 +92,12 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
         };
         const auto buffer = [](const uint8_t* from) __attribute__((always_inline)) { return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000); };
         auto load_dy = [&](int i) __attribute__((always_inline)) {
-            kept[i] = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], DW ? (int)(kRowsAtOnce * i * p.lddy * 2) : 0, 0);
+#pragma unroll
+            for (int h = 0; h < kKept / 4; ++h) {
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], (DW ? (int)(kRowsAtOnce * i * p.lddy * kSize) : 0) + 16 * h, 0);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) kept[i][4 * h + e] = w[e];
+            }
         };
         auto load_v = [&](int run) __attribute__((always_inline)) {
 #pragma unroll
@@ -101,8 +113,17 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
             return row * kRow + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
         };
         auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
-            if constexpr (DW) *reinterpret_cast<v4u*>(tile + permuted(kRowsAtOnce * i + t / kAcross, t % kAcross)) = kept[i];
-            else *reinterpret_cast<v4u*>(tile + 16 * unit_at(32 * i + (t >> 3), t & 7)) = kept[i];
+            uint8_t* const to = tile + (DW ? permuted(kRowsAtOnce * i + t / kAcross, t % kAcross) : 16 * unit_at(32 * i + (t >> 3), t & 7));
+            if constexpr (P == 1) *reinterpret_cast<v4u*>(to) = v4u{kept[i][0], kept[i][1], kept[i][2], kept[i][3]};
+            else {
+                float part[8][P];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) split<P>(element<T>(kept[i][kSize == 4 ? e : e / 2], e % 2), part[e]);
+#pragma unroll
+                for (int n = 0; n < P; ++n)
+                    *reinterpret_cast<v4u*>(to + n * kBytes) = v4u{pack_bf16(part[0][n], part[1][n]), pack_bf16(part[2][n], part[3][n]),
+                                                                   pack_bf16(part[4][n], part[5][n]), pack_bf16(part[6][n], part[7][n])};
+            }
         };
         // values 2 e and 2 e + 1 of the eight of a piece, four of which are a run
         v4u decoded;
@@ -122,7 +143,7 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
         };
         // ---- operands: eight neighbouring r of one row or column
         struct Operands {
-            v4u v[kF], dy[kF];
+            v4u v[kF], dy[P][kF];
         };
         Operands set[2];
         // A lane's half of operand f: r = 16 q + 8 g + 4 h + (lane / 4) % 4, columns first + 32 f + 16 ((lane / 16) % 2) + 4 (lane % 4) and on.
@@ -134,15 +155,15 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
             to[2 * h] = w[0];
             to[2 * h + 1] = w[1];
         };
-        constexpr int kReads = kF * (DW ? 4 : 3);
+        constexpr int kReads = kF * (2 + P * (DW ? 2 : 1));
         // read n of a quarter's kReads, in the order the products need them: the first fragment of V, all of dy, the rest of V
         auto read = [&](Operands& o, const uint8_t* dy_tile, const uint8_t* v_tile, int q, int n) __attribute__((always_inline)) {
-            constexpr int kDy = DW ? 2 * kF : kF;
+            constexpr int kEach = DW ? 2 * kF : kF, kDy = P * kEach;
             if (n < 2) read_turned(o.v[0], v_tile, wk, 0, q, n);
             else if (n < 2 + kDy) {
-                n -= 2;
-                if constexpr (DW) read_turned(o.dy[n >> 1], dy_tile, wj, n >> 1, q, n & 1);
-                else o.dy[n] = *reinterpret_cast<const v4u*>(dy_tile + 16 * unit_at(wj + 32 * n + c, 2 * q + g));
+                const int part = (n - 2) / kEach, f = (n - 2) % kEach;
+                if constexpr (DW) read_turned(o.dy[part][f >> 1], dy_tile + part * kBytes, wj, f >> 1, q, f & 1);
+                else o.dy[part][f] = *reinterpret_cast<const v4u*>(dy_tile + part * kBytes + 16 * unit_at(wj + 32 * f + c, 2 * q + g));
             } else {
                 n -= kDy;
                 read_turned(o.v[n >> 1], v_tile, wk, n >> 1, q, n & 1);
@@ -152,20 +173,20 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
         // What is issued after matrix instruction i of quarter q of a step whose tiles are the first or second of each side.  Between two
         // barriers, quarters 3, 0, 1, 2, the tiles of the step after the later one's are written and those after them asked for.
         auto between = [&](auto now_, int q, int i) __attribute__((always_inline)) {
-            constexpr int now = decltype(now_)::value * kBytes, kPieces = kRuns, kParts = 8 * kPieces;      // pieces a quarter, eight parts each
+            constexpr int now = decltype(now_)::value, kPieces = kRuns, kParts = 8 * kPieces;      // pieces a quarter, eight parts each
             const int part = (q + 1) & 3;
             if (q == 3 && i == 0) advance();
-            const int read_from = q == 3 ? now ^ kBytes : now, write_to = q == 3 ? now : now ^ kBytes;
-            for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from, lds_v + read_from, (q + 1) & 3, n);
+            const int read_from = q == 3 ? now ^ 1 : now, write_to = q == 3 ? now : now ^ 1;
+            for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from * P * kBytes, lds_v + read_from * kBytes, (q + 1) & 3, n);
             for (int u = i * kParts / kSlots; u < (i + 1) * kParts / kSlots; ++u) {
                 const int piece = part * kPieces + u / 8;
                 if (u % 2 == 0) decode(piece, u % 8 / 2);
                 if (u % 8 == 7) {
-                    write_v(lds_v + write_to, piece);
+                    write_v(lds_v + write_to * kBytes, piece);
                     if ((piece & 3) == 3) load_v(piece >> 2);
                 }
                 if (u % 8 == 3) {
-                    write_dy(lds_dy + write_to, piece);
+                    write_dy(lds_dy + write_to * P * kBytes, piece);
                     load_dy(piece);
                 }
             }
@@ -184,12 +205,14 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
 #pragma unroll
                 for (int x = 0; x < kF; ++x)
 #pragma unroll
-                    for (int y = 0; y < kF; ++y) {
-                        products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[y]),
-                                                                                     products.acc[x][y], 0, 0, 0);
-                        between(now, q, kF * x + y);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }
+                    for (int n = 0; n < P; ++n)
+#pragma unroll
+                        for (int y = 0; y < kF; ++y) {
+                            products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[n][y]),
+                                                                                         products.acc[x][y], 0, 0, 0);
+                            between(now, q, (x * P + n) * kF + y);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }
             }
         };
 
@@ -217,7 +240,7 @@ __global__ __launch_bounds__(kGradThreads, TILE == 256 ? 1 : 2) void grad_wide_k
             if (s + 1 < s_fast) step(std::integral_constant<int, 1>{});
         }
     }
-    multiply_rest<__bf16, DW, TILE, TILE>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
+    multiply_rest<T, DW, TILE, TILE>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);

@@ -190,6 +190,13 @@ def test_product_in_large_tiles(sq, M, N, K, t, bias):
     test_product(sq, M, N, K, t, bias, 0, 0)
 
 
+# few results of a long reduction, which is divided; few rows whose weights are too many for x to be quantised on the way; most of the few rows
+@pytest.mark.parametrize("M,N,K", [(70, 100, 8300), (130, 65, 9000), (16, 3000, 3000), (64, 515, 2056), (49, 2000, 1100)])
+@pytest.mark.parametrize("t,bias,pad,at", [("bf16", True, 0, 0), ("f32", False, 3, 1)])
+def test_product_of_other_shapes(sq, M, N, K, t, bias, pad, at):
+    test_product(sq, M, N, K, t, bias, pad, at)
+
+
 @pytest.mark.parametrize("M,N,K", [(1, 40, 300), (40, 70, 300), (300, 300, 700)])
 def test_product_of_what_is_not_finite(sq, M, N, K):
     """A NaN or an infinity makes its row (of x) or column (of w) NaN and nothing else."""
@@ -239,21 +246,28 @@ def test_product_gradients(sq, M, N, K, t, o, pad, at):
 
 @pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000), (4099, 257, 3201), (2049, 129, 1730), (261, 3300, 3000)])
 @pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2), ("f16", 4, 1)])
-def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at):
+def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t="bf16"):
     """dx [J][K] over R outputs, dw [J][K] over R rows."""
     g = rng(13, J, R, K)
-    V, d = values(g, R, K, "bf16"), values(g, J, R, "bf16", 0.1)
+    V, d = values(g, R, K, "bf16"), values(g, J, R, t, 0.1)
+    parts = {"bf16": 1, "f16": 2, "f32": 3}[t]
     for bits in (4, 8):
         ref = R_quantised(V, bits)
         out = Result(J, K, o, pad, at)
         if bits == 4:
             ws, view = workspace(sq.sparq_mx_linear_dx_workspace_bytes(J, R, K))
-            sq.sparq_mx_linear_dx(matrix(d, "bf16", pad, at), *stored(sq, V, 4), out.view, workspace=view)
+            sq.sparq_mx_linear_dx(matrix(d, t, pad, at), *stored(sq, V, 4), out.view, workspace=view)
         else:
             ws, view = workspace(sq.sparq_mx_linear_dw_workspace_bytes(R, J, K))
-            sq.sparq_mx_linear_dw(matrix(d.T, "bf16", pad, at), *stored(sq, V, 8), out.view, workspace=view)
-        close(out.get(), d @ ref, 2 * (R + 2) * u * (np.abs(d) @ np.abs(ref)), o)
+            sq.sparq_mx_linear_dw(matrix(d.T, t, pad, at), *stored(sq, V, 8), out.view, workspace=view)
+        close(out.get(), d @ ref, 2 * (parts * R + 2) * u * (np.abs(d) @ np.abs(ref)), o)
         guard(ws, view)
+
+
+@pytest.mark.parametrize("J,R,K", [(2056, 205, 1700), (2049, 129, 1730), (264, 3300, 3000), (261, 3299, 3000), (2048, 64, 1664)])
+@pytest.mark.parametrize("t,o,pad,at", [("f16", "f32", 0, 0), ("f32", "f32", 0, 0), ("f16", "f16", 5, 1), ("f32", "bf16", 3, 2)])
+def test_product_gradients_of_wider_types(sq, J, R, K, t, o, pad, at):
+    test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t)
 
 
 def test_product_gradients_are_the_differences(sq):
@@ -549,6 +563,44 @@ def test_rows_more_than_32_bits_apart(sq):
     for d, y in zip(dw, (far_y, near_y)):
         sq.sparq_mx_linear_dw(y, a[0].t, a[1].t, d, workspace=ws)
     assert torch.equal(*dw)
+
+
+def test_a_large_call_is_its_pieces(sq):
+    """Calls of more bytes than the caches hold, to the bit what calls for a few rows at a time give."""
+    M, K, piece = 17001, 8200, 3001
+    g = torch.Generator(DEV).manual_seed(5)
+    new = lambda: torch.randn(M, K, generator=g, device=DEV, dtype=torch.float32).to(torch.bfloat16)      # noqa: E731
+    x, up, dy = new(), new(), new()
+    gamma, beta = torch.rand(K, generator=g, device=DEV) + 0.5, torch.rand(K, generator=g, device=DEV)
+    coded = lambda bits: (torch.zeros(M, sq.sparq_mx_code_bytes(K, bits), dtype=torch.uint8, device=DEV),      # noqa: E731
+                          torch.zeros(M, sq.sparq_mx_scale_bytes(K), dtype=torch.uint8, device=DEV))
+    like = lambda: torch.full_like(x, 7.0)      # noqa: E731
+    results = []
+    for rows in (M, piece):
+        c4, c8, cu, cn = coded(4), coded(8), coded(8), coded(8)
+        back4, back8, y, dgate, dup, n, dx = (like() for _ in range(7))
+        mean, rstd = torch.zeros(M, device=DEV), torch.zeros(M, device=DEV)
+        dg, db = torch.zeros(K, device=DEV), torch.zeros(K, device=DEV)
+        ws = torch.empty(sq.sparq_mx_norm_grad_workspace_bytes(rows, K), dtype=torch.uint8, device=DEV)
+        for r in range(0, M, rows):
+            p = slice(r, min(M, r + rows))
+            at = lambda *ts: [t[p] for t in ts]      # noqa: E731
+            sq.sparq_mx_quantize(x[p], *at(*c4, *c8))
+            sq.sparq_mx_dequantize(*at(*c4), 4, back4[p])
+            sq.sparq_mx_dequantize(*at(*c8), 8, back8[p])
+            sq.sparq_mx_act("gelu", x[p], y[p], up=up[p], up_codes=cu[0][p], up_scales=cu[1][p])
+            sq.sparq_mx_act_grad("gelu", dy[p], *at(*c8), dgate[p], up_codes=cu[0][p], up_scales=cu[1][p], dup=dup[p])
+            sq.sparq_mx_norm(x[p], gamma, beta, 1e-5, n[p], mean=mean[p], rstd=rstd[p], codes=cn[0][p], scales=cn[1][p])
+            sq.sparq_mx_norm_grad(dy[p], *at(*cn), mean[p], rstd[p], gamma, dx[p], dgamma=dg, dbeta=db, workspace=ws)
+        torch.cuda.synchronize()
+        results.append([*c4, *c8, *cu, *cn, back4, back8, y, dgate, dup, n, dx, mean, rstd])
+        if rows == M:
+            h = back8.double().sub_(mean.double()[:, None]).mul_(rstd.double()[:, None])
+            wrong = lambda got, terms: float(((got.double() - terms.sum(0)).abs() / terms.abs().sum(0)).max())      # noqa: E731
+            assert wrong(dg, dy.double() * h) <= (M + 10) * u and wrong(db, dy.double()) <= (M + 2) * u
+            del h
+    for i, (a, b) in enumerate(zip(*results)):
+        assert torch.equal(a, b), i
 
 
 def test_binding_refuses_wrong_shapes(sq):
