@@ -48,7 +48,7 @@ sparq_status launch_grad_types(const GradParams& p, int parts, int tile, void* o
             }
         }
         s = tile == 128 ? launch_grad_kernel<O>(grad_wide_kernel<T, O, DW, 128>, kWideLds<T, 128>, allowed[1], p, parts, out, stream)
-                        : launch_grad_kernel<O>(grad_kernel<T, O, DW, 64, 64>, kWideLds<T, 64>, allowed[2], p, parts, out, stream);
+                        : launch_grad_kernel<O>(grad_wide_kernel<T, O, DW, 64>, kWideLds<T, 64>, allowed[2], p, parts, out, stream);
     });
     return s;
 }

@@ -41,18 +41,18 @@ __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const T* __rest
 
 // ---- plan ----------------------------------------------------------------------------
 struct GradPlan {
-    int tile;                // 256 (bf16) or 128, on grad_wide_kernel, or 64, on grad_kernel: results a workgroup makes along either side
+    int tile;                // 256 (bf16), 128 or 64: results a workgroup makes along either side
     int parts;               // of the reduction
     int slabs;               // of rows for the column sums
     size_t partial_bytes, bytes;
 };
-static GradPlan grad_plan(bool wide, bool bf16, int64_t J, int64_t R, int K, bool dw) {
+static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
     GradPlan p = {};
     const auto tiles = [&](int t) { return ((J + t - 1) / t) * ((K + t - 1) / t); };
     // Few tiles of a long reduction are divided; shorter ones are over before the parts would be joined.  Tiles are as large as still leaves
     // work for every CU: a larger one's steps cost less per result.
     const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / 16 > 1 ? steps / 16 : 1;
-    p.tile = !wide ? 64 : bf16 && tiles(256) >= 192 ? 256 : tiles(128) * most >= 192 ? 128 : 64;
+    p.tile = bf16 && tiles(256) >= 192 ? 256 : tiles(128) * most >= 192 ? 128 : 64;
     const int64_t n = tiles(p.tile), places = p.tile == 256 || n >= 192 ? 1 : (p.tile == 128 ? 512 : 1024) / n, parts = places < most ? places : most;
     p.parts = (int)(parts < 1 ? 1 : parts > 64 ? 64 : parts);
     const int64_t columns = (J + 63) / 64, slabs = R / 512 < 1024 / columns ? R / 512 : 1024 / columns;
@@ -61,14 +61,17 @@ static GradPlan grad_plan(bool wide, bool bf16, int64_t J, int64_t R, int K, boo
     p.bytes = p.partial_bytes + (p.slabs > 1 ? (size_t)round_up((int64_t)p.slabs * J * 4, 256) : 0);
     return p;
 }
-// The workspace does not depend on dy's type and place: the largest.
+// The workspace does not depend on dy's type: the larger.
 static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
-    const size_t a = grad_plan(false, false, J, R, K, dw).bytes, b = grad_plan(true, true, J, R, K, dw).bytes;
+    const size_t a = grad_plan(false, J, R, K, dw).bytes, b = grad_plan(true, J, R, K, dw).bytes;
     return a > b ? a : b;
 }
-static GradPlan grad_plan_of(int dy_type, int64_t lddy, int64_t J, int64_t R, int K, bool dw) {
-    const bool wide = R < (1ll << 36) && (dw ? grad_wide_fits<true>(lddy, J, code_pitch(K, 8)) : grad_wide_fits<false>(lddy, J, code_pitch(K, 4)));
-    return grad_plan(wide, dy_type == SPARQ_MX_BF16, J, R, K, dw);
+// Steps that are read without checks, in runs of eight: none if rows' distances do not fit the loads' 32-bit offsets.  A run that dw's last
+// column cuts reads on into the next rows (one, unless rows are shorter than a run): the last rows, which it would leave, are not among them.
+static int64_t whole_steps(int64_t lddy, int64_t J, int64_t R, int64_t pitch, bool dw) {
+    if (lddy >= 1 << 21 || pitch >= 1 << 24 || R >= 1ll << 36) return 0;
+    const int64_t over = dw ? round_up(J, 8) - J : 0, rows = R - (over + lddy - 1) / lddy;
+    return rows > 0 ? rows / kGradStep : 0;
 }
 
 static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
@@ -85,6 +88,7 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     p.R = R;
     p.K = K;
     p.K128 = (int)round_up(K, kCodeUnit);
+    p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);
     const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
     if (tiles_j * tiles_k >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
     p.tiles_j = (int)tiles_j;
@@ -120,7 +124,7 @@ extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int6
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
     if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan_of(dy_type, lddy, M, N, K, false);
+    const GradPlan plan = grad_plan(dy_type == SPARQ_MX_BF16, M, N, K, false);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
@@ -133,7 +137,7 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (!tensor_ok(dw, dw_type, lddw, K) || !extent_ok(N, lddw) || !aligned(db, 4)) return SPARQ_EINVAL;
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K)))
         return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan_of(dy_type, lddy, N, M, K, true);
+    const GradPlan plan = grad_plan(dy_type == SPARQ_MX_BF16, N, M, K, true);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);

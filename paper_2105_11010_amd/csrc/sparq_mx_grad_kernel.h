@@ -3,9 +3,9 @@
 // V's codes and scales go through registers into bf16 (their values are bf16 exactly: at most eight significand bits and a
 // power of two) and, turned so that the reduction index is the fast one, into LDS; dy goes the same way, as one bf16 part
 // (bf16), two (fp16) or three (fp32) whose sum is the value.
-// A workgroup of four wavefronts makes TJ x TK results in steps of 64 products, a wavefront a quarter of them.  Two tiles in LDS
-// and two sets of registers: while the matrix instructions work on step s, step s + 1 is converted and written to the other tile
-// and step s + 2 is on its way from memory; one barrier a step.
+// A workgroup of four wavefronts makes TJ x TK results in steps of 64 products, a wavefront a quarter of them.  What is here takes steps of
+// any kind, one after the other, with checked loads: the last step of a reduction, and calls whose rows lie too far apart for
+// sparq_mx_grad_wide_kernel.h, which takes the others.
 #pragma once
 #include "sparq_mx_store.h"
 
@@ -21,6 +21,7 @@ struct GradParams {
     int32_t K, K128, blocks;             // row length, the same in whole units of codes, bytes of a row of scales
     int32_t tiles_j, tiles_k;
     int32_t steps_per_part;              // steps of 64 products
+    int64_t s_whole;                     // steps before this one are read without checks
 };
 
 constexpr int kGradThreads = 256;
@@ -64,18 +65,14 @@ __device__ __forceinline__ float element(uint32_t w, int half) {
 }
 // COUNT neighbouring elements as they lie in memory, of which the first n are there
 template <class T, int COUNT>
-__device__ __forceinline__ void fetch(uint32_t (&w)[COUNT * sizeof(T) / 4], const T* at, bool whole, int64_t n) {
-    constexpr int W = COUNT * sizeof(T) / 4;
-    if (whole) __builtin_memcpy(w, at, sizeof(w));
-    else {
+__device__ __forceinline__ void fetch(uint32_t (&w)[COUNT * sizeof(T) / 4], const T* at, int64_t n) {
 #pragma unroll
-        for (int i = 0; i < W; ++i) {
-            if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, at[i]) : 0u;
-            else {
-                const uint32_t lo = 2 * i < n ? __builtin_bit_cast(uint16_t, at[2 * i]) : 0u;
-                const uint32_t hi = 2 * i + 1 < n ? __builtin_bit_cast(uint16_t, at[2 * i + 1]) : 0u;
-                w[i] = lo | hi << 16;
-            }
+    for (int i = 0; i < COUNT * (int)sizeof(T) / 4; ++i) {
+        if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, at[i]) : 0u;
+        else {
+            const uint32_t lo = 2 * i < n ? __builtin_bit_cast(uint16_t, at[2 * i]) : 0u;
+            const uint32_t hi = 2 * i + 1 < n ? __builtin_bit_cast(uint16_t, at[2 * i + 1]) : 0u;
+            w[i] = lo | hi << 16;
         }
     }
 }
@@ -87,42 +84,31 @@ struct DyTile {
     static constexpr int kRuns = TURN ? 8 : N, kLength = TURN ? N : 8, kPer = 4 / sizeof(T);        // elements a word
     uint32_t v[kRuns][kLength / kPer];
 
-    int row;                                                 // of the tile, of the thread's first column (TURN) or run
-
-    // WHOLE: the step lies inside dy.  TURN: a thread whose columns would reach past the last one takes the last N instead, some of
-    // them beside a neighbour who writes the same; rows of the tile past the last column are then left as they are: the
-    // results they make are not stored.
-    template <bool WHOLE>
     __device__ __forceinline__ void load(const GradParams& p, int64_t j0, int64_t r0) {
         const T* dy = static_cast<const T*>(p.dy);
         const int t = threadIdx.x;
         if constexpr (TURN) {
-            int64_t j = j0 + (t & 31) * N;
-            if (WHOLE) j = j < p.J - N ? j : p.J - N;
-            row = (int)(j - j0);
-            const int64_t r = r0 + (t >> 5) * 8;
+            const int64_t j = j0 + (t & 31) * N, r = r0 + (t >> 5) * 8;
             const T* at = dy + r * p.lddy + j;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                fetch<T, N>(v[i], at, WHOLE, r + i < p.R ? p.J - j : 0);
+                fetch<T, N>(v[i], at, r + i < p.R ? p.J - j : 0);
                 at += p.lddy;
             }
         } else {
             const int64_t r = r0 + (t & 7) * 8;
-            row = t >> 3;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
-                int64_t j = j0 + row + 32 * i;
-                j = j < p.J ? j : p.J - 1;                   // (rows past the last one: as above)
-                fetch<T, 8>(v[i], dy + j * p.lddy + r, WHOLE, p.R - r);
+                int64_t j = j0 + (t >> 3) + 32 * i;
+                j = j < p.J ? j : p.J - 1;                   // (rows past the last one make results that are not stored)
+                fetch<T, 8>(v[i], dy + j * p.lddy + r, p.R - r);
             }
         }
     }
     // column or run c into the parts' tiles
     __device__ __forceinline__ void store(v4u* lds, int c) const {
         const int t = threadIdx.x;
-        const int at_row = TURN ? row + c : row + 32 * c, chunk = TURN ? t >> 5 : t & 7;
-        if (TURN && at_row < 0) return;
+        const int at_row = TURN ? (t & 31) * N + c : (t >> 3) + 32 * c, chunk = TURN ? t >> 5 : t & 7;
         const int at = unit_at(at_row, chunk);
         if constexpr (P == 1) {
             v4u w;
@@ -153,30 +139,19 @@ struct CodedTile {
     Raw raw[8];
     uint32_t scale[8];
 
-    template <bool WHOLE>
     __device__ __forceinline__ void load(const GradParams& p, int k0, int64_t r0) {
         const int t = threadIdx.x;
         int k = k0 + (t & 31) * N;
         k = k < p.K128 ? k : p.K128 - N;                     // (columns past the last one make results that are not stored)
         const int64_t r = r0 + (t >> 5) * 8;
         const uint8_t *at = p.codes + r * p.code_pitch + k * BITS / 8, *sc = p.scales + r * p.scale_pitch + (k >> 5);
-        if constexpr (WHOLE) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                raw[i] = *reinterpret_cast<const Raw*>(at);
-                scale[i] = *sc;
-                at += p.code_pitch;
-                sc += p.scale_pitch;
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                raw[i] = Raw{};
-                scale[i] = 127;
-                if (r + i < p.R) {
-                    raw[i] = *reinterpret_cast<const Raw*>(at + i * p.code_pitch);
-                    scale[i] = sc[i * p.scale_pitch];
-                }
+        for (int i = 0; i < 8; ++i) {
+            raw[i] = Raw{};
+            scale[i] = 127;
+            if (r + i < p.R) {
+                raw[i] = *reinterpret_cast<const Raw*>(at + i * p.code_pitch);
+                scale[i] = sc[i * p.scale_pitch];
             }
         }
     }
@@ -252,15 +227,6 @@ struct Products {
                 for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[i][y], acc[x][y], 0, 0, 0);
     }
 };
-// quarter q of a step into a tile
-template <class Dy, class Coded, int TJ, int TK>
-__device__ __forceinline__ void convert(const Dy& dy, const Coded& coded, v4u* tile, int q) {
-    constexpr int kDyParts = TJ / 32, kCodedParts = TK / 64;
-#pragma unroll
-    for (int i = q * kDyParts / 4; i < (q + 1) * kDyParts / 4; ++i) dy.store(tile, i);
-#pragma unroll
-    for (int i = q * kCodedParts / 4; i < (q + 1) * kCodedParts / 4; ++i) coded.store(tile + Dy::P * TJ * 8, i);
-}
 // Steps that are not whole, or whose loads would not be: checked loads, one step after the other.
 template <class T, bool DW, int TJ, int TK>
 __device__ __forceinline__ void multiply_rest(Products<kParts<T>, TJ, TK>& products, const GradParams& p, v4u* lds, int64_t j0, int k0, int64_t s, int64_t s_end) {
@@ -269,69 +235,17 @@ __device__ __forceinline__ void multiply_rest(Products<kParts<T>, TJ, TK>& produ
     for (; s < s_end; ++s) {
         Dy dy;
         Coded coded;
-        dy.template load<false>(p, j0, s * kGradStep);
-        coded.template load<false>(p, k0, s * kGradStep);
+        dy.load(p, j0, s * kGradStep);
+        coded.load(p, k0, s * kGradStep);
         __syncthreads();
 #pragma unroll
-        for (int q = 0; q < 4; ++q) convert<Dy, Coded, TJ, TK>(dy, coded, lds, q);
+        for (int i = 0; i < TJ / 32; ++i) dy.store(lds, i);
+#pragma unroll
+        for (int i = 0; i < TK / 64; ++i) coded.store(lds + Dy::P * TJ * 8, i);
         __syncthreads();
 #pragma unroll
         for (int q = 0; q < 4; ++q) products.multiply(lds, q);
     }
-}
-
-template <class T, class O, bool DW, int TJ, int TK>
-__global__ __launch_bounds__(kGradThreads) void grad_kernel(O* __restrict__ out, const GradParams p) {
-#if defined(__HIP_DEVICE_COMPILE__)
-    constexpr int P = kParts<T>, BITS = DW ? 8 : 4, FJ = TJ / 64, FK = TK / 64;
-    constexpr int kUnits = (P * TJ + TK) * 8;                // 16-byte units of a tile
-    extern __shared__ v4u lds[];
-    uint32_t tj, tk;
-    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
-    const int64_t j0 = (int64_t)tj * TJ;
-    const int k0 = (int)tk * TK;
-    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
-    const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all;
-    // steps before this one are whole
-    const int64_t whole = DW && p.J < TJ / 32 ? 0 : p.R / kGradStep, s_fast = whole < s_end ? whole : s_end;
-    typedef DyTile<T, TJ, DW> Dy;
-    typedef CodedTile<BITS, TK> Coded;
-    Products<P, TJ, TK> products;
-
-    if (s_begin < s_fast) {
-        Dy dy[2];
-        Coded coded[2];
-        auto load = [&](int64_t s, int set) __attribute__((always_inline)) {
-            s = s < s_fast ? s : s_fast - 1;                 // (past the end: the last step again, into registers nobody reads)
-            dy[set].template load<true>(p, j0, s * kGradStep);
-            coded[set].template load<true>(p, k0, s * kGradStep);
-        };
-        auto step = [&](int64_t s, int set) __attribute__((always_inline)) {
-            load(s + 2, set);
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                products.multiply(lds + set * kUnits, q);
-                convert<Dy, Coded, TJ, TK>(dy[set ^ 1], coded[set ^ 1], lds + (set ^ 1) * kUnits, q);
-            }
-            __syncthreads();
-        };
-        load(s_begin, 0);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) convert<Dy, Coded, TJ, TK>(dy[0], coded[0], lds, q);
-        load(s_begin + 1, 1);
-        __syncthreads();
-        for (int64_t s = s_begin; s < s_fast; s += 2) {
-            step(s, 0);
-            if (s + 1 < s_fast) step(s + 1, 1);
-        }
-    }
-    multiply_rest<T, DW, TJ, TK>(products, p, lds, j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
-
-    __syncthreads();
-    const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, FK, FJ, FK == 1 ? 64 : 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + products.wj, p.J, k0 + products.wk, p.K, none,
-                                  reinterpret_cast<uint8_t*>(lds) + (threadIdx.x >> 6) * 4096);
-#endif
 }
 
 }  // namespace mx

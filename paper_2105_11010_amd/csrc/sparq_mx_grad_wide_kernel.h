@@ -1,16 +1,16 @@
-// The gradients' larger tiles: 256 x 256 results a workgroup (bf16), or 128 x 128 (the other types, and where those would leave CUs without).
+// The gradients' kernel: 256 x 256 results a workgroup (bf16), 128 x 128 (the other types), or 64 x 64, the largest that leaves no CUs without.
 // out[j][k] = sum_r dy(j, r) V[r][k] as in sparq_mx_grad_kernel.h.  V's rows are decoded as they lie, eight values of a row a thread, and dy's are
 // copied; the matrix instruction's operands, eight neighbouring r of one column, come out of LDS by reads that turn 4 x 16 values (V, and dy
 // where r is its row).  Sixteen lanes read four rows, 32 bytes each, at a time: a row's 16-byte units are permuted by the row so that four
 // neighbouring rows lie in different quarters of the banks.
-// A step is 64 r, four quarters of sixteen (or four) matrix instructions; one wavefront a SIMD has nobody else to fill the time an
+// A step is 64 r, four quarters of sixteen (256 x 256), four or one matrix instructions; one wavefront a SIMD has nobody else to fill the time an
 // instruction runs, so what goes between them is laid out here: the next quarter's reads, and of V and of dy two rows each, written to the
 // next step's tiles, and the request for their successors.  One barrier a step, before the last quarter: by then the step's tiles have been
 // read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, and dx of
 // 8192 x 4096 x 4096 took 392 us instead of 268, before the steps' order was laid out as it is.)
 // Bound by the matrix instructions and, with data as large as this, by the card's power: 8192 x 4096 x 4096 takes 206-248 us for dx and 237-256
 // for dw (1.07-1.33 PF; the same instructions without loads and writes 1.57 PF).  fp16 dy, two instructions a product, 710 and 728 us, fp32, three,
-// 1015 and 1070 (grad_kernel's 128 x 128 tiles 720 and 921, 1083 and 1272).
+// 1015 and 1070.  A small layer is bound by the steps' latency: 515 x 771 x 577 7.7 and 8.4 us in 64 x 64 tiles, 12 or 13 steps.
 #pragma once
 #include <type_traits>
 
@@ -21,20 +21,17 @@ namespace mx {
 
 template <int TILE> inline constexpr int kWideBytes = kGradStep * TILE * 2;       // of one side's tile
 
-// A call this kernel is for: rows whose distances fit the loads' 32-bit offsets, and at least eight columns (DW).
-template <bool DW>
-inline bool grad_wide_fits(int64_t lddy, int64_t J, int64_t code_pitch) {
-    return lddy < (1 << 21) && code_pitch < (1 << 24) && (!DW || J >= 8);
-}
-
 template <class T, int TILE> inline constexpr int kWideLds = 2 * (kParts<T> + 1) * kWideBytes<TILE>;
-template <class T, int TILE> inline constexpr int kWidePerCu = 160 * 1024 / kWideLds<T, TILE>;
+template <class T, int TILE> inline constexpr int kWidePerCu = kWideLds<T, TILE> < 40 * 1024 ? 4 : 160 * 1024 / kWideLds<T, TILE>;
 template <class T, class O, bool DW, int TILE>
 __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr int P = kParts<T>;                             // of dy, a tile each
     constexpr int kF = TILE / 64, kSlots = P * kF * kF;      // 32 x 32 results along a side; matrix instructions a quarter
-    constexpr int kUnits = TILE / 32, kRuns = TILE / 128, kRow = TILE * 2;      // of dy and of V a thread; bytes of a tile's row
+    constexpr int kRow = TILE * 2;                           // bytes of a tile's row
+    constexpr int kRun = TILE == 64 ? 16 : 32, kRuns = TILE * kGradStep / kGradThreads / kRun;      // a thread's runs of V's values
+    constexpr int kUnits = TILE / 32;                        // and of eight values of dy, as many as V's pieces of eight
+    constexpr int kPieces = kRun / 8;                        // a run
     constexpr int kBytes = kWideBytes<TILE>;
     typedef short v4s __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
@@ -44,10 +41,8 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
     const int64_t j0 = (int64_t)tj * TILE;
     const int k0 = (int)tk * TILE;
-    const int s_begin = (int)blockIdx.y * p.steps_per_part, s_all = (int)((p.R + kGradStep - 1) / kGradStep), s_whole = (int)((DW && p.J % 8 ? p.R - 1 : p.R) / kGradStep);
-    const int s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = s_whole < s_end ? s_whole : s_end;
-    // (Steps before s_whole are loaded without checks.  A run of eight columns that the last column cuts reads on into the next row, so the
-    // last row is not among them then.)
+    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
+    const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = p.s_whole < s_end ? p.s_whole : s_end;
     Products<P, TILE, TILE> products;
     const int wj = products.wj, wk = products.wk;
 
@@ -69,21 +64,22 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
                 dy_at[i] = (uint32_t)((from * p.lddy + 8 * (t & 7)) * kSize);
             }
         }
-        // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32, or one of row 4 (lane / 4) + wave
-        constexpr int kWords = DW ? 8 : 4;
+        // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32; or one of row 4 (lane / 4) + wave;
+        // or one of 16 values of row lane / 4 + 16 wave
+        constexpr int kWords = kRun / (DW ? 4 : 8);
         uint32_t raw[kRuns][kWords], scale[kRuns];
-        constexpr int kBlocks = TILE / 32;
-        const int v_row = 4 * (lane / kBlocks) + wave;
-        int k = k0 + 32 * (lane % kBlocks);
-        k = k < p.K128 ? k : p.K128 - 32;
+        constexpr int kAlong = TILE / kRun;
+        const int v_row = TILE == 64 ? lane / kAlong + 16 * wave : 4 * (lane / kAlong) + wave;
+        int k = k0 + kRun * (lane % kAlong);
+        k = k < p.K128 ? k : p.K128 - kRun;
         const uint32_t v_at = (uint32_t)(v_row * p.code_pitch + (DW ? k : k / 2)), scale_at = (uint32_t)(v_row * p.scale_pitch + (k >> 5));
 
         // Where the next step to be asked for lies.  Past the last one it stays there, for tiles nobody reads.
-        const uint8_t* dy_from = static_cast<const uint8_t*>(p.dy) + (DW ? j0 + s_begin * (kGradStep * p.lddy) : j0 * p.lddy + (int64_t)s_begin * kGradStep) * kSize;
-        const uint8_t *codes_from = p.codes + (int64_t)s_begin * kGradStep * p.code_pitch, *scales_from = p.scales + (int64_t)s_begin * kGradStep * p.scale_pitch;
+        const uint8_t* dy_from = static_cast<const uint8_t*>(p.dy) + (DW ? j0 + s_begin * (kGradStep * p.lddy) : j0 * p.lddy + s_begin * kGradStep) * kSize;
+        const uint8_t *codes_from = p.codes + s_begin * kGradStep * p.code_pitch, *scales_from = p.scales + s_begin * kGradStep * p.scale_pitch;
         const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * kSize) : kGradStep * kSize, codes_step = (uint32_t)(kGradStep * p.code_pitch);
         const uint32_t scales_step = (uint32_t)(kGradStep * p.scale_pitch);
-        int left = s_fast - s_begin - 1;
+        int left = (int)(s_fast - s_begin) - 1;
         auto advance = [&]() __attribute__((always_inline)) {
             dy_from += left > 0 ? dy_step : 0;
             codes_from += left > 0 ? codes_step : 0;
@@ -100,6 +96,11 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             }
         };
         auto load_v = [&](int run) __attribute__((always_inline)) {
+            if constexpr (kWords == 2) {
+                const v2u w = __builtin_amdgcn_raw_buffer_load_b64(buffer(codes_from), v_at, 0, 0);
+                raw[run][0] = w[0];
+                raw[run][1] = w[1];
+            }
 #pragma unroll
             for (int h = 0; h < kWords / 4; ++h) {
                 const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(codes_from), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
@@ -110,7 +111,8 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         };
         // A tile's row is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
         const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
-            return row * kRow + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
+            if constexpr (TILE == 64) return row * kRow + ((chunk ^ (row & 2 ? 5 : 0)) << 4);
+            else return row * kRow + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
         };
         auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
             uint8_t* const to = tile + (DW ? permuted(kRowsAtOnce * i + t / kAcross, t % kAcross) : 16 * unit_at(32 * i + (t >> 3), t & 7));
@@ -125,11 +127,11 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
                                                                    pack_bf16(part[4][n], part[5][n]), pack_bf16(part[6][n], part[7][n])};
             }
         };
-        // values 2 e and 2 e + 1 of the eight of a piece, four of which are a run
+        // values 2 e and 2 e + 1 of the eight of a piece
         v4u decoded;
         float unit;
         auto decode = [&](int piece, int e) __attribute__((always_inline)) {
-            const int run = piece >> 2, at = piece & 3;
+            const int run = piece / kPieces, at = piece % kPieces;
             if (at == 0 && e == 0) unit = DW ? unit8_of(scale[run]) : scale_operand(scale[run]);
             if constexpr (DW) {
                 const uint32_t w = raw[run][2 * at + (e >> 1)] >> (16 * (e & 1));
@@ -139,7 +141,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             }
         };
         auto write_v = [&](uint8_t* tile, int piece) __attribute__((always_inline)) {
-            *reinterpret_cast<v4u*>(tile + permuted(v_row + 32 * (piece >> 2), 4 * (lane % kBlocks) + (piece & 3))) = decoded;
+            *reinterpret_cast<v4u*>(tile + permuted(v_row + 32 * (piece / kPieces), kPieces * (lane % kAlong) + piece % kPieces)) = decoded;
         };
         // ---- operands: eight neighbouring r of one row or column
         struct Operands {
@@ -173,17 +175,17 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // What is issued after matrix instruction i of quarter q of a step whose tiles are the first or second of each side.  Between two
         // barriers, quarters 3, 0, 1, 2, the tiles of the step after the later one's are written and those after them asked for.
         auto between = [&](auto now_, int q, int i) __attribute__((always_inline)) {
-            constexpr int now = decltype(now_)::value, kPieces = kRuns, kParts = 8 * kPieces;      // pieces a quarter, eight parts each
-            const int part = (q + 1) & 3;
+            constexpr int now = decltype(now_)::value;
+            const int part = (q + 1) & 3, first = part * kUnits / 4, parts = 8 * ((part + 1) * kUnits / 4 - first);      // pieces this quarter, eight parts each
             if (q == 3 && i == 0) advance();
             const int read_from = q == 3 ? now ^ 1 : now, write_to = q == 3 ? now : now ^ 1;
             for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from * P * kBytes, lds_v + read_from * kBytes, (q + 1) & 3, n);
-            for (int u = i * kParts / kSlots; u < (i + 1) * kParts / kSlots; ++u) {
-                const int piece = part * kPieces + u / 8;
+            for (int u = i * parts / kSlots; u < (i + 1) * parts / kSlots; ++u) {
+                const int piece = first + u / 8;
                 if (u % 2 == 0) decode(piece, u % 8 / 2);
                 if (u % 8 == 7) {
                     write_v(lds_v + write_to * kBytes, piece);
-                    if ((piece & 3) == 3) load_v(piece >> 2);
+                    if (piece % kPieces == kPieces - 1) load_v(piece / kPieces);
                 }
                 if (u % 8 == 3) {
                     write_dy(lds_dy + write_to * P * kBytes, piece);
@@ -221,13 +223,13 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 #pragma unroll
         for (int i = 0; i < kRuns; ++i) load_v(i);
         advance();
-        static_assert(kUnits == 4 * kRuns, "a unit of dy to a piece of V");
+        static_assert(kUnits == kPieces * kRuns, "a unit of dy to a piece of V");
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) decode(i, e);
             write_v(lds_v, i);
-            if ((i & 3) == 3) load_v(i >> 2);
+            if (i % kPieces == kPieces - 1) load_v(i / kPieces);
             write_dy(lds_dy, i);
             load_dy(i);
         }
@@ -235,7 +237,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // as if the last quarter of a step before the first
 #pragma unroll
         for (int i = 0; i < kSlots; ++i) between(std::integral_constant<int, 1>{}, 3, i);
-        for (int s = s_begin; s < s_fast; s += 2) {
+        for (int64_t s = s_begin; s < s_fast; s += 2) {
             step(std::integral_constant<int, 0>{});
             if (s + 1 < s_fast) step(std::integral_constant<int, 1>{});
         }
@@ -244,7 +246,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, kF, kF, 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
+    store_results<O, kF, kF, kF == 1 ? 64 : 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
 #endif
 }
 
