@@ -32,7 +32,9 @@ sparq_status launch_grad_kernel(F* kernel, int lds_bytes, std::atomic<bool> (&al
             return SPARQ_ELAUNCH;
         allowed[slot].store(true, std::memory_order_relaxed);
     }
-    kernel<<<dim3((unsigned)(p.tiles_j * (int64_t)p.tiles_k), parts), kGradThreads, lds_bytes, stream>>>(static_cast<O*>(out), p);
+    constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
+    const int64_t sums = p.column_sums ? (p.J + kColumns - 1) / kColumns : 0;
+    kernel<<<dim3((unsigned)(p.tiles_j * (int64_t)p.tiles_k + sums), parts), kGradThreads, lds_bytes, stream>>>(static_cast<O*>(out), p);
     return launch_status();
 }
 template <class T, bool DW>

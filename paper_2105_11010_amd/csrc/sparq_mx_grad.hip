@@ -4,46 +4,21 @@
 namespace sparq {
 namespace mx {
 
-// Sums of dy's columns over a slab of its rows: a workgroup takes 64 columns, eight a lane, and 128 rows at a time.
-constexpr int kSumThreads = 1024, kSumColumns = 64, kSumRows = kSumThreads / (kSumColumns / 8);
+// Sums of dy's columns over a slab of its rows, a grid row a slab.
+constexpr int kSumThreads = 1024;
 template <class T>
 __global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
-    __shared__ float shared[kSumRows][kSumColumns + 4];
-    const int t = threadIdx.x, x = t % (kSumColumns / 8), r0 = t / (kSumColumns / 8), c = blockIdx.x * kSumColumns + 8 * x;
+    typedef ColumnSums<T, kSumThreads> Sums;
+    __shared__ float shared[Sums::kFloats];
     const int64_t begin = blockIdx.y * slab, end = begin + slab < rows ? begin + slab : rows;
-    float s[8] = {};
-    if (c < n)
-        for (int64_t r = begin + r0; r < end; r += 4 * kSumRows) {
-            float v[4][8];
-#pragma unroll
-            for (int u = 0; u < 4; ++u) load_upto8(dy + (r + u * kSumRows) * ld + c, r + u * kSumRows < end ? n - c : 0, v[u]);
-#pragma unroll
-            for (int u = 0; u < 4; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; ++i) s[i] += v[u][i];
-        }
-#pragma unroll
-    for (int i = 0; i < 8; ++i) shared[r0][8 * x + i] = s[i];
-    __syncthreads();
-    // 16 threads a column, eight rows each, then one
-    const int col = t & 63, part = t >> 6;
-    float total = 0.0f;
-#pragma unroll
-    for (int i = 0; i < kSumRows / 16; ++i) total += shared[part * (kSumRows / 16) + i][col];
-    __syncthreads();
-    shared[part][col] = total;
-    __syncthreads();
-    if (part != 0 || blockIdx.x * kSumColumns + col >= n) return;
-#pragma unroll
-    for (int i = 1; i < 16; ++i) total += shared[i][col];
-    sum[(int64_t)blockIdx.y * n + blockIdx.x * kSumColumns + col] = total;
+    Sums::run(dy, ld, begin, end, n, blockIdx.x * Sums::kColumns, sum + (int64_t)blockIdx.y * n, shared);
 }
 
 // ---- plan ----------------------------------------------------------------------------
 struct GradPlan {
     int tile;                // 256 (bf16), 128 or 64: results a workgroup makes along either side
     int parts;               // of the reduction
-    int slabs;               // of rows for the column sums
+    int slabs;               // of rows for the column sums; one: by the product's launch itself
     size_t partial_bytes, bytes;
 };
 static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
@@ -75,7 +50,7 @@ static int64_t whole_steps(int64_t lddy, int64_t J, int64_t R, int64_t pitch, bo
 }
 
 static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
-                         int64_t ldo, int64_t J, int64_t R, int K, const GradPlan& plan, void* workspace, hipStream_t stream) {
+                         int64_t ldo, float* column_sums, int64_t J, int64_t R, int K, const GradPlan& plan, void* workspace, hipStream_t stream) {
     const int t = plan.tile;
     GradParams p = {};
     p.dy = dy;
@@ -88,9 +63,10 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     p.R = R;
     p.K = K;
     p.K128 = (int)round_up(K, kCodeUnit);
+    p.column_sums = column_sums;
     p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);
     const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
-    if (tiles_j * tiles_k >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    if (tiles_j * tiles_k + J >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
     p.tiles_j = (int)tiles_j;
     p.tiles_k = (int)tiles_k;
     p.steps_per_part = (int)((steps + plan.parts - 1) / plan.parts);
@@ -127,7 +103,7 @@ extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int6
     const GradPlan plan = grad_plan(dy_type == SPARQ_MX_BF16, M, N, K, false);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
-    return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
+    return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, nullptr, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
 }
 
 extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int64_t lddy, const void* x_codes, const void* x_scales,
@@ -141,17 +117,15 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (db) {
-        float* sums = plan.slabs > 1 ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes) : db;
+    if (db && plan.slabs > 1) {
+        float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes);
         with_type(dy_type, [&](auto t) {
             typedef decltype(t) T;
-            column_sum_kernel<T><<<dim3((N + kSumColumns - 1) / kSumColumns, plan.slabs), kSumThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
+            column_sum_kernel<T><<<dim3((N + 63) / 64, plan.slabs), kSumThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
                                                                                         (M + plan.slabs - 1) / plan.slabs, sums);
         });
-        if (plan.slabs > 1) {
-            const sparq_status joined = launch_join_columns(sums, db, nullptr, N, N, plan.slabs, s);
-            if (joined != SPARQ_OK) return joined;
-        }
+        const sparq_status joined = launch_join_columns(sums, db, nullptr, N, N, plan.slabs, s);
+        if (joined != SPARQ_OK) return joined;
     }
-    return grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, N, M, K, plan, workspace, s);
+    return grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, plan.slabs > 1 ? nullptr : db, N, M, K, plan, workspace, s);
 }

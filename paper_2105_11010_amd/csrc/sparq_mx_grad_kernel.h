@@ -21,6 +21,7 @@ struct GradParams {
     int32_t K, K128, blocks;             // row length, the same in whole units of codes, bytes of a row of scales
     int32_t tiles_j, tiles_k;
     int32_t steps_per_part;              // steps of 64 products
+    float* column_sums;                  // of dy [R][J], by workgroups past the tiles' (dw), or null
     int64_t s_whole;                     // steps before this one are read without checks
 };
 
@@ -227,6 +228,42 @@ struct Products {
                 for (int y = 0; y < FJ; ++y) acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[x], b[i][y], acc[x][y], 0, 0, 0);
     }
 };
+// Sums of dy's columns, rows begin to end: a workgroup takes kColumns of them, eight a lane, and kRows rows at a time.
+template <class T, int THREADS>
+struct ColumnSums {
+    static constexpr int kColumns = THREADS == 1024 ? 64 : 32, kLanes = kColumns / 8, kRows = THREADS / kLanes, kSlices = THREADS / kColumns;
+    static constexpr int kPitch = kColumns + 4, kFloats = kRows * kPitch;
+    static __device__ __forceinline__ void run(const T* __restrict__ dy, int64_t ld, int64_t begin, int64_t end, int n, int first, float* __restrict__ sum, float* shared) {
+        const int t = threadIdx.x, x = t % kLanes, r0 = t / kLanes, c = first + 8 * x;
+        float s[8] = {};
+        if (c < n)
+            for (int64_t r = begin + r0; r < end; r += 4 * kRows) {
+                float v[4][8];
+#pragma unroll
+                for (int u = 0; u < 4; ++u) load_upto8(dy + (r + u * kRows) * ld + c, r + u * kRows < end ? n - c : 0, v[u]);
+#pragma unroll
+                for (int u = 0; u < 4; ++u)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) s[i] += v[u][i];
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) shared[r0 * kPitch + 8 * x + i] = s[i];
+        __syncthreads();
+        // kSlices threads a column, eight rows each, then one
+        const int col = t % kColumns, part = t / kColumns;
+        float total = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kRows / kSlices; ++i) total += shared[(part * (kRows / kSlices) + i) * kPitch + col];
+        __syncthreads();
+        shared[part * kPitch + col] = total;
+        __syncthreads();
+        if (part != 0 || first + col >= n) return;
+#pragma unroll
+        for (int i = 1; i < kSlices; ++i) total += shared[i * kPitch + col];
+        sum[first + col] = total;
+    }
+};
+
 // Steps that are not whole, or whose loads would not be: checked loads, one step after the other.
 template <class T, bool DW, int TJ, int TK>
 __device__ __forceinline__ void multiply_rest(Products<kParts<T>, TJ, TK>& products, const GradParams& p, v4u* lds, int64_t j0, int k0, int64_t s, int64_t s_end) {

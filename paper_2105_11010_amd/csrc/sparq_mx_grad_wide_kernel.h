@@ -37,6 +37,16 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
     uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * P * kBytes;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
+    if constexpr (DW) {
+        const uint32_t tiles = (uint32_t)p.tiles_j * (uint32_t)p.tiles_k;
+        if (blockIdx.x >= tiles) {
+            typedef ColumnSums<T, kGradThreads> Sums;
+            static_assert(Sums::kFloats * 4 <= kWideLds<T, TILE>);
+            if (blockIdx.y == 0)
+                Sums::run(static_cast<const T*>(p.dy), p.lddy, 0, p.R, (int)p.J, (int)(blockIdx.x - tiles) * Sums::kColumns, p.column_sums, reinterpret_cast<float*>(lds8));
+            return;
+        }
+    }
     uint32_t tj, tk;
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
     const int64_t j0 = (int64_t)tj * TILE;
