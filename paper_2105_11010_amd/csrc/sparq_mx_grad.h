@@ -33,7 +33,7 @@ sparq_status launch_grad_kernel(F* kernel, int lds_bytes, std::atomic<bool> (&al
         allowed[slot].store(true, std::memory_order_relaxed);
     }
     constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
-    const int64_t sums = p.column_sums ? (p.J + kColumns - 1) / kColumns : 0;
+    const int64_t sums = p.slabs * ((p.J + kColumns - 1) / kColumns);
     kernel<<<dim3((unsigned)(p.tiles_j * (int64_t)p.tiles_k + sums), parts), kGradThreads, lds_bytes, stream>>>(static_cast<O*>(out), p);
     return launch_status();
 }

@@ -4,21 +4,21 @@
 namespace sparq {
 namespace mx {
 
-// Sums of dy's columns over a slab of its rows, a grid row a slab.
+// Sums of dy's columns, a grid row a slab of its rows, for gradients as large as to keep memory busy on their own.
 constexpr int kSumThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const T* __restrict__ dy, int64_t ld, int64_t rows, int n, int64_t slab, float* __restrict__ sum) {
+__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const GradParams p) {
     typedef ColumnSums<T, kSumThreads> Sums;
     __shared__ float shared[Sums::kFloats];
-    const int64_t begin = blockIdx.y * slab, end = begin + slab < rows ? begin + slab : rows;
-    Sums::run(dy, ld, begin, end, n, blockIdx.x * Sums::kColumns, sum + (int64_t)blockIdx.y * n, shared);
+    const int64_t begin = blockIdx.y * p.slab, end = begin + p.slab < p.R ? begin + p.slab : p.R;
+    Sums::run(static_cast<const T*>(p.dy), p.lddy, begin, end, (int)p.J, blockIdx.x * Sums::kColumns, p.column_sums + blockIdx.y * p.J, shared);
 }
 
 // ---- plan ----------------------------------------------------------------------------
 struct GradPlan {
     int tile;                // 256 (bf16), 128 or 64: results a workgroup makes along either side
     int parts;               // of the reduction
-    int slabs;               // of rows for the column sums; one: by the product's launch itself
+    int slabs;               // of rows for the column sums
     size_t partial_bytes, bytes;
 };
 static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
@@ -64,9 +64,20 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     p.K = K;
     p.K128 = (int)round_up(K, kCodeUnit);
     p.column_sums = column_sums;
+    p.slab = plan.slabs > 1 ? (R + plan.slabs - 1) / plan.slabs : R;
+    p.slabs = column_sums ? plan.slabs : 0;
+    // The column sums: by workgroups of the product's launch, which saves a launch, unless dy is so large that these would come last and
+    // last longer than it (us with either, in the launch -> in one before: 515 x 771 x 577 8.4 -> 13.4, 2048^3 36.9 -> 40.8, 4096 x 512 x 512
+    // 16.8 -> 20.3; 8192 x 1024 x 1024 45.6 -> 42.5, 4096^3 150 -> 141, 8192 x 4096 x 4096 283 -> 272).
+    if (column_sums && J * R > 1 << 22) {
+        with_type(dy_type, [&](auto t) { column_sum_kernel<decltype(t)><<<dim3((unsigned)((J + 63) / 64), p.slabs), kSumThreads, 0, stream>>>(p); });
+        p.slabs = 0;
+        const sparq_status s = launch_status();
+        if (s != SPARQ_OK) return s;
+    }
     p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);
     const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
-    if (tiles_j * tiles_k + J >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
+    if (tiles_j * tiles_k + p.slabs * J >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
     p.tiles_j = (int)tiles_j;
     p.tiles_k = (int)tiles_k;
     p.steps_per_part = (int)((steps + plan.parts - 1) / plan.parts);
@@ -117,15 +128,8 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    if (db && plan.slabs > 1) {
-        float* sums = reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes);
-        with_type(dy_type, [&](auto t) {
-            typedef decltype(t) T;
-            column_sum_kernel<T><<<dim3((N + 63) / 64, plan.slabs), kSumThreads, 0, s>>>(static_cast<const T*>(dy), lddy, M, N,
-                                                                                        (M + plan.slabs - 1) / plan.slabs, sums);
-        });
-        const sparq_status joined = launch_join_columns(sums, db, nullptr, N, N, plan.slabs, s);
-        if (joined != SPARQ_OK) return joined;
-    }
-    return grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, plan.slabs > 1 ? nullptr : db, N, M, K, plan, workspace, s);
+    const bool slabs = db && plan.slabs > 1;
+    float* const sums = slabs ? reinterpret_cast<float*>(static_cast<char*>(workspace) + plan.partial_bytes) : db;
+    const sparq_status done = grad(dy, dy_type, lddy, x_codes, x_scales, 8, dw, dw_type, lddw, sums, N, M, K, plan, workspace, s);
+    return done != SPARQ_OK || !slabs ? done : launch_join_columns(sums, db, nullptr, N, N, plan.slabs, s);
 }

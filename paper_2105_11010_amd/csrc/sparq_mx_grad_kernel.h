@@ -21,7 +21,9 @@ struct GradParams {
     int32_t K, K128, blocks;             // row length, the same in whole units of codes, bytes of a row of scales
     int32_t tiles_j, tiles_k;
     int32_t steps_per_part;              // steps of 64 products
-    float* column_sums;                  // of dy [R][J], by workgroups past the tiles' (dw), or null
+    float* column_sums;                  // [slabs][J], of dy [R][J] (dw), by workgroups past the tiles', or by a launch before
+    int64_t slab;                        // rows of one
+    int32_t slabs;
     int64_t s_whole;                     // steps before this one are read without checks
 };
 

@@ -42,8 +42,11 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         if (blockIdx.x >= tiles) {
             typedef ColumnSums<T, kGradThreads> Sums;
             static_assert(Sums::kFloats * 4 <= kWideLds<T, TILE>);
+            const uint32_t n = blockIdx.x - tiles, across = (uint32_t)((p.J + Sums::kColumns - 1) / Sums::kColumns), slab = n / across;
+            const int64_t begin = slab * p.slab, end = begin + p.slab < p.R ? begin + p.slab : p.R;
             if (blockIdx.y == 0)
-                Sums::run(static_cast<const T*>(p.dy), p.lddy, 0, p.R, (int)p.J, (int)(blockIdx.x - tiles) * Sums::kColumns, p.column_sums, reinterpret_cast<float*>(lds8));
+                Sums::run(static_cast<const T*>(p.dy), p.lddy, begin, end, (int)p.J, (int)(n % across) * Sums::kColumns, p.column_sums + slab * p.J,
+                          reinterpret_cast<float*>(lds8));
             return;
         }
     }

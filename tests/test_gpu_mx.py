@@ -270,8 +270,8 @@ def test_product_gradients_of_wider_types(sq, J, R, K, t, o, pad, at):
     test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t)
 
 
-# fewer columns of dy than a read takes, whose reads run on into the next rows; small layers of many rows
-@pytest.mark.parametrize("M,N,K", [(700, 1, 300), (577, 2, 128), (640, 5, 64), (131, 7, 100), (900, 9, 130), (1000, 200, 333)])
+# fewer columns of dy than a read takes, whose reads run on into the next rows; bias gradients of a few rows, of slabs, and of many elements
+@pytest.mark.parametrize("M,N,K", [(700, 1, 300), (577, 2, 128), (640, 5, 64), (131, 7, 100), (900, 9, 130), (1000, 200, 333), (2100, 2100, 64), (1040, 4101, 33)])
 @pytest.mark.parametrize("t,o,pad,at", [("bf16", "f32", 0, 0), ("f16", "f16", 1, 0), ("f32", "f32", 0, 0)])
 def test_product_gradients_of_few_columns(sq, M, N, K, t, o, pad, at):
     test_product_gradients(sq, M, N, K, t, o, pad, at)
