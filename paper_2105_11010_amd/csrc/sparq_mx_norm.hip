@@ -212,6 +212,55 @@ struct NormGradParams {
     int32_t parts;                       // partial sums of the weights' gradients: rows part, part + parts, ...
 };
 
+// The weights' gradients of 32 columns, eight a lane and 64 rows at a time: what reads dy and the codes once more.
+struct ColumnGradients {
+    static constexpr int kColumns = 32, kLanes = kColumns / 8, kRows = kThreads / kLanes, kSlices = kThreads / kColumns, kPitch = kColumns + 4;
+    static constexpr int kFloats = kRows * kPitch;
+    template <class T>
+    static __device__ __forceinline__ void run(const T* __restrict__ dy, const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
+                                               const float* __restrict__ mean, const float* __restrict__ rstd, float* __restrict__ dgamma,
+                                               float* __restrict__ dbeta, const NormGradParams& p, int first, float* shared) {
+        const int t = threadIdx.x, x = t % kLanes, r0 = t / kLanes, col = first + 8 * x, n = p.K - col;
+        float g[8] = {}, b[8] = {};
+        if (n > 0) {
+#pragma unroll 2
+            for (int64_t row = r0; row < p.rows; row += kRows) {
+                float d[8], h[8];
+                load_upto8(dy + row * p.ldy + col, n, d);
+                values8_of(*reinterpret_cast<const v2u*>(codes + row * p.code_pitch + col), scales[row * p.scale_pitch + (col >> 5)], h);
+                const float mu = mean[row], r = rstd[row];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    g[i] += d[i] * ((h[i] - mu) * r);
+                    b[i] += d[i];
+                }
+            }
+        }
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            float* const to = which ? dbeta : dgamma;
+            if (!to) continue;
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) shared[r0 * kPitch + 8 * x + i] = which ? b[i] : g[i];
+            __syncthreads();
+            // kSlices threads a column, then one
+            const int c = t % kColumns, slice = t / kColumns;
+            float total = 0.0f;
+#pragma unroll
+            for (int i = 0; i < kRows / kSlices; ++i) total += shared[(slice * (kRows / kSlices) + i) * kPitch + c];
+            __syncthreads();
+            shared[slice * kPitch + c] = total;
+            __syncthreads();
+            if (slice == 0 && first + c < p.K) {
+#pragma unroll
+                for (int i = 1; i < kSlices; ++i) total += shared[i * kPitch + c];
+                to[first + c] = total;
+            }
+        }
+    }
+};
+
 // dx, and the workgroup's share of the weights' gradients, in one pass: WAVES wavefronts take a row, CHUNKS x 8 values a lane, rows part,
 // part + parts, ..., the next row on its way while this one is summed and written.  What the workgroup's wavefronts added up is joined in
 // LDS in their order and leaves as one partial sum.
@@ -219,7 +268,13 @@ template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, const float* __restrict__ gamma, T* __restrict__ dx,
-                                                             float* __restrict__ partial, const NormGradParams p) {
+                                                             float* __restrict__ partial, float* __restrict__ dgamma, float* __restrict__ dbeta,
+                                                             const NormGradParams p) {
+    __shared__ float columns[ColumnGradients::kFloats];
+    if ((int)blockIdx.x >= p.parts) {
+        ColumnGradients::run(dy, codes, scales, mean, rstd, dgamma, dbeta, p, (int)(blockIdx.x - p.parts) * ColumnGradients::kColumns, columns);
+        return;
+    }
     constexpr int kRows = kWaves / WAVES, kSpan = WAVES * 512;
     __shared__ float sums[2][2][WAVES];
     __shared__ float joined[kRows > 1 ? kRows * CHUNKS * 512 : 1];
@@ -392,6 +447,10 @@ __global__ __launch_bounds__(kThreads) void norm_grad_columns_kernel(const T* __
 // Rows are held in registers up to this length, one wavefront a row up to the other.
 constexpr int kHeldK = 8192, kWaveK = 1024;
 static bool held_in_registers(int K) { return K >= 8 && K <= kHeldK; }
+// Few rows: workgroups beside those of the rows make the weights' gradients, from dy and the codes read again, which is shorter than partial
+// sums and the launch that joins them (us, with that -> beside: 130 x 1000 6.6 -> 3.8, 512 x 512 6.2 -> 5.0, 256 x 4096 10.7 -> 4.3,
+// 1024 x 4096 17.3 -> 13.3; 1024 x 1024 7.6 -> 8.0, 2048 x 4096 17.3 -> 23.7).
+static bool gradients_beside(int64_t rows, int K) { return held_in_registers(K) && rows <= (K <= kWaveK ? 512 : 1024); }
 // Workgroups: enough that what they ask for hides the memory's latency, and no more, since each leaves a partial sum of both gradients.
 static int norm_parts(int64_t rows, int K) {
     const int64_t most = !held_in_registers(K) ? 256 : 512, needed = held_in_registers(K) && K <= kWaveK ? (rows + kWaves - 1) / kWaves : rows;
@@ -461,14 +520,18 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
     if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
     if (workspace_bytes < norm_grad_bytes(rows, K)) return SPARQ_EWORKSPACE;
     v2f* sums = static_cast<v2f*>(workspace);
-    float* partial = dgamma || dbeta ? reinterpret_cast<float*>(static_cast<char*>(workspace) + (held_in_registers(K) ? 0 : round_up(rows * 8, 256))) : nullptr;
+    const bool gradients = dgamma || dbeta, beside = gradients && gradients_beside(rows, K);
+    float* partial = gradients && !beside ? reinterpret_cast<float*>(static_cast<char*>(workspace) + (held_in_registers(K) ? 0 : round_up(rows * 8, 256))) : nullptr;
     const NormGradParams p = {lddy, lddx, code_pitch(K, 8), scale_pitch(K), rows, K, (float)(1.0 / K), norm_parts(rows, K)};
     const uint8_t *c = static_cast<const uint8_t*>(codes), *sc = static_cast<const uint8_t*>(scales);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const T* from = static_cast<const T*>(dy);
         T* to = static_cast<T*>(dx);
-        const auto launch = [&](auto kernel) { kernel<<<p.parts, kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, to, partial, p); };
+        const auto launch = [&](auto kernel) {
+            const unsigned further = beside ? (unsigned)((K + ColumnGradients::kColumns - 1) / ColumnGradients::kColumns) : 0;
+            kernel<<<p.parts + further, kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, to, partial, dgamma, dbeta, p);
+        };
         const auto held = [&](auto whole, auto nt) {
             constexpr bool W = decltype(whole)::value, NT = decltype(nt)::value;
             if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W, NT>);
