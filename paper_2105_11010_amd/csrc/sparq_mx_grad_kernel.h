@@ -7,6 +7,8 @@
 // any kind, one after the other, with checked loads: the last step of a reduction, and calls whose rows lie too far apart for
 // sparq_mx_grad_wide_kernel.h, which takes the others.
 #pragma once
+#include <type_traits>
+
 #include "sparq_mx_store.h"
 
 namespace sparq {
@@ -66,17 +68,20 @@ __device__ __forceinline__ float element(uint32_t w, int half) {
         return (float)__builtin_bit_cast(T, h);
     }
 }
-// COUNT neighbouring elements as they lie in memory, of which the first n are there
+// COUNT neighbouring elements as they lie in memory, of which the first n are there.  Without branches, which would have one load wait for
+// another: what is not there is read from `safe` and left out.
 template <class T, int COUNT>
-__device__ __forceinline__ void fetch(uint32_t (&w)[COUNT * sizeof(T) / 4], const T* at, int64_t n) {
+__device__ __forceinline__ void fetch(uint32_t (&w)[COUNT * sizeof(T) / 4], const T* at, int64_t n, const T* safe) {
+    typedef std::conditional_t<sizeof(T) == 4, uint32_t, uint16_t> Bits;
+    Bits v[COUNT];
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = *reinterpret_cast<const Bits*>(i < n ? at + i : safe);
+#pragma unroll
+    for (int i = 0; i < COUNT; ++i) v[i] = i < n ? v[i] : (Bits)0;
 #pragma unroll
     for (int i = 0; i < COUNT * (int)sizeof(T) / 4; ++i) {
-        if constexpr (sizeof(T) == 4) w[i] = i < n ? __builtin_bit_cast(uint32_t, at[i]) : 0u;
-        else {
-            const uint32_t lo = 2 * i < n ? __builtin_bit_cast(uint16_t, at[2 * i]) : 0u;
-            const uint32_t hi = 2 * i + 1 < n ? __builtin_bit_cast(uint16_t, at[2 * i + 1]) : 0u;
-            w[i] = lo | hi << 16;
-        }
+        if constexpr (sizeof(T) == 4) w[i] = v[i];
+        else w[i] = v[2 * i] | (uint32_t)v[2 * i + 1] << 16;
     }
 }
 
@@ -95,7 +100,7 @@ struct DyTile {
             const T* at = dy + r * p.lddy + j;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                fetch<T, N>(v[i], at, r + i < p.R ? p.J - j : 0);
+                fetch<T, N>(v[i], at, r + i < p.R ? p.J - j : 0, dy);
                 at += p.lddy;
             }
         } else {
@@ -104,7 +109,7 @@ struct DyTile {
             for (int i = 0; i < N; ++i) {
                 int64_t j = j0 + (t >> 3) + 32 * i;
                 j = j < p.J ? j : p.J - 1;                   // (rows past the last one make results that are not stored)
-                fetch<T, 8>(v[i], dy + j * p.lddy + r, p.R - r);
+                fetch<T, 8>(v[i], dy + j * p.lddy + r, p.R - r, dy);
             }
         }
     }
@@ -150,12 +155,15 @@ struct CodedTile {
         const uint8_t *at = p.codes + r * p.code_pitch + k * BITS / 8, *sc = p.scales + r * p.scale_pitch + (k >> 5);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
-            raw[i] = Raw{};
-            scale[i] = 127;
-            if (r + i < p.R) {
-                raw[i] = *reinterpret_cast<const Raw*>(at + i * p.code_pitch);
-                scale[i] = sc[i * p.scale_pitch];
-            }
+            const bool there = r + i < p.R;
+            raw[i] = *reinterpret_cast<const Raw*>(there ? at + i * p.code_pitch : p.codes);
+            scale[i] = *(there ? sc + i * p.scale_pitch : p.scales);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const bool there = r + i < p.R;
+            raw[i] = there ? raw[i] : Raw{};
+            scale[i] = there ? scale[i] : 127u;
         }
     }
     // columns 2 q and 2 q + 1
