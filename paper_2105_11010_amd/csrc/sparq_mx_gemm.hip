@@ -16,6 +16,8 @@ static GemmPlan gemm_plan(int64_t M, int N, int K) {
     // 64 x 4096 x 4096 8.2 -> 11, 32 x 8192 x 8192 16 -> 18.5, 48 x 8192 x 8192 20.9 -> 18.6, 64 x 8192 x 8192 24.9 -> 18.6).
     if (M <= 32 || (M <= kFewMost && M * N * K <= 1ll << 31)) return p;
     const auto tiles = [&](int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
+    // The larger tiles, one a CU at a time, unless they leave CUs without (us, 256 x 256 -> 128 x 128: 4096^3 47 -> 54, 3584^3 37 -> 47, 3000^3
+    // 30 -> 30, 4096 x 2048 x 4096 34 -> 28, 2900 x 3700 x 2500 30 -> 27, 2048^3 18 -> 10).
     p.tile = tiles(256) >= 192 ? 256 : 128;
     // Few tiles of a long reduction are divided; shorter ones, or more of them, are over before the parts would be joined (us, whole -> in
     // parts: 128 x 1024 x 8192 16.2 -> 13.6, 65 x 8192 x 8192 18.6 -> 16.8, 128 x 4096 x 4096 11.3 -> 14.6, 512 x 4096 x 4096 12 -> 23).

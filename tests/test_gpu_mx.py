@@ -244,7 +244,7 @@ def test_product_gradients(sq, M, N, K, t, o, pad, at):
     guard(ws, view)
 
 
-@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000), (4099, 257, 3201), (2049, 129, 1730), (261, 3300, 3000)])
+@pytest.mark.parametrize("J,R,K", [(4100, 205, 3300), (4096, 64, 3328), (4104, 40, 3201), (3336, 512, 4000), (4104, 333, 3400), (2056, 205, 1700), (264, 3300, 3000), (4099, 257, 3201), (2049, 129, 1730), (261, 3300, 3000), (1600, 4100, 1700)])
 @pytest.mark.parametrize("o,pad,at", [("bf16", 0, 0), ("f32", 6, 2), ("f16", 4, 1)])
 def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t="bf16"):
     """dx [J][K] over R outputs, dw [J][K] over R rows."""
@@ -264,7 +264,7 @@ def test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t="bf16"):
         guard(ws, view)
 
 
-@pytest.mark.parametrize("J,R,K", [(2056, 205, 1700), (2049, 129, 1730), (264, 3300, 3000), (261, 3299, 3000), (2048, 64, 1664)])
+@pytest.mark.parametrize("J,R,K", [(2056, 205, 1700), (2049, 129, 1730), (264, 3300, 3000), (261, 3299, 3000), (2048, 64, 1664), (1600, 4100, 1700)])
 @pytest.mark.parametrize("t,o,pad,at", [("f16", "f32", 0, 0), ("f32", "f32", 0, 0), ("f16", "f16", 5, 1), ("f32", "bf16", 3, 2)])
 def test_product_gradients_of_wider_types(sq, J, R, K, t, o, pad, at):
     test_product_gradients_in_large_tiles(sq, J, R, K, o, pad, at, t)
