@@ -62,7 +62,7 @@ sparq_status sparq_mx_gemm(const void *a_codes, const void *a_scales, const void
                            const float *bias, void *y, int32_t type, int64_t ldy, int64_t M, int32_t N, int32_t K,
                            void *workspace, size_t workspace_bytes, void *stream);
 
-/* The same with A = the 4-bit form of x [M][K], quantised on the way: a layer as it is served. */
+/* The same with A = the 4-bit form of x [M][K], quantised on the way: a layer as it is served.  K up to 2^23. */
 size_t sparq_mx_linear_workspace_bytes(int64_t M, int32_t N, int32_t K);
 sparq_status sparq_mx_linear(const void *x, int32_t x_type, int64_t ldx, const void *w_codes, const void *w_scales,
                              const float *bias, void *y, int32_t y_type, int64_t ldy, int64_t M, int32_t N, int32_t K,

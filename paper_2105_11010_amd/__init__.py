@@ -1,8 +1,7 @@
 """SPARQ trimmed convolution-as-GEMM on AMD MI355X (gfx950).
 
 Thin Python front end of ``libsparq.so`` (see ``include/sparq.h`` and, for the microscaled formats,
-``include/sparq_mx.h``): the names
-below are the C entry points, taking torch device tensors as plain buffers.
+``include/sparq_mx.h``): the names below are the C entry points, taking torch device tensors as plain buffers.
 """
 from .binding import (  # noqa: F401
     LIB_PATH, SparqConvDesc, SparqError, SparqMode, conv_desc, lib, mode, out_rows, strerror,

@@ -16,7 +16,8 @@ struct CodecParams {
 
 // A wavefront takes 512 values of one row, a lane eight of them, so that a block is four neighbouring lanes: the block's
 // largest magnitude is two exchanges inside a quad, loads are 16 bytes a lane (fp32: twice), codes leave as 4 and 8 bytes a
-// lane and the 16 scales as one byte of every fourth lane.  Bound by memory.
+// lane and the 16 scales as one byte of every fourth lane.  Bound by memory: 8192 x 8192 bf16 to 4 bits in 27 us (6.35 TB/s), to 8 in 32 (6.4), to
+// both at once in 37 (6.5), fp32 to 4 bits in 52 (5.8); the way back 25.6 (6.6), 30.5 and 43 (7.0).  A large copy: 6.65 TB/s.
 template <class T, bool F4, bool I8, bool NT>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict__ x, uint8_t* __restrict__ codes4,
                                                             uint8_t* __restrict__ scales4, uint8_t* __restrict__ codes8,

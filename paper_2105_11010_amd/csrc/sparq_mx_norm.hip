@@ -83,7 +83,8 @@ __device__ __forceinline__ void first_own(const Place& p, float (&v)[8]) {
 
 // WAVES wavefronts take a row of at least eight, CHUNKS x 8 values a lane, which stay in registers from the load to the result: one
 // pass over memory, the mean first and the squares of what differs from it second.  As many workgroups as have room go through the rows,
-// gamma and beta in registers and the next row on its way while this one is summed.
+// gamma and beta in registers and the next row on its way while this one is summed.  Bound by memory and, for each row, by the two sums one after
+// the other: 16384 x 4096 bf16 with checkpoint 60 us (5.6 TB/s), 65536 x 1024 66, fp32 117.
 template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
@@ -263,7 +264,7 @@ struct ColumnGradients {
 
 // dx, and the workgroup's share of the weights' gradients, in one pass: WAVES wavefronts take a row, CHUNKS x 8 values a lane, rows part,
 // part + parts, ..., the next row on its way while this one is summed and written.  What the workgroup's wavefronts added up is joined in
-// LDS in their order and leaves as one partial sum.
+// LDS in their order and leaves as one partial sum.  16384 x 4096 bf16 70 us with the sums' join (4.8 TB/s), 65536 x 1024 64, fp32 118.
 template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, const float* __restrict__ mean,
@@ -444,7 +445,8 @@ __global__ __launch_bounds__(kThreads) void norm_grad_columns_kernel(const T* __
     }
 }
 
-// Rows are held in registers up to this length, one wavefront a row up to the other.
+// Rows are held in registers up to this length, one wavefront a row up to the other (four instead for 65536 x 1024: 66 -> 83 us, backward 65 ->
+// 131).
 constexpr int kHeldK = 8192, kWaveK = 1024;
 static bool held_in_registers(int K) { return K >= 8 && K <= kHeldK; }
 // Few rows: workgroups beside those of the rows make the weights' gradients, from dy and the codes read again, which is shorter than partial
