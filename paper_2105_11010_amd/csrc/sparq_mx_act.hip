@@ -55,7 +55,7 @@ __device__ __forceinline__ void function_and_slope(float v, float& value, float&
 
 // A wavefront takes 512 values of a row, a lane eight, as the quantiser does.  8192 x 8192 bf16, gated, with both checkpoints: silu 83 us
 // (6.5 TB/s), bound by memory, as is its gradient (83); gelu 92-95 and 91-94, bound by its arithmetic; fp32 silu 163 and 170.
-template <class T, int F, bool UP, bool KEEP, bool NT>
+template <class T, int F, bool UP, bool KEEP, int STREAMING>
 __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gate, const T* __restrict__ up, T* __restrict__ y,
                                                        uint8_t* __restrict__ gate_codes, uint8_t* __restrict__ gate_scales,
                                                        uint8_t* __restrict__ up_codes, uint8_t* __restrict__ up_scales, const ActParams p) {
@@ -65,11 +65,11 @@ __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gat
     const uint32_t row = fastdiv(item, p.div_chunks);
     const int col = (int)(item - row * p.chunks) * kScaleUnit + 8 * lane, n = p.K - col;
     float g[8], u[8], o[8];
-    load_upto8<NT>(gate + row * p.ldg + col, n, g);
-    if constexpr (UP) load_upto8<NT>(up + row * p.ldu + col, n, u);
+    load_upto8<STREAMING == kAll>(gate + row * p.ldg + col, n, g);
+    if constexpr (UP) load_upto8<STREAMING == kAll>(up + row * p.ldu + col, n, u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) o[i] = function<F, sizeof(T) == 4>(g[i]) * (UP ? u[i] : 1.0f);
-    if (n > 0) store_upto8<NT>(y + row * p.ldy + col, n, o);
+    if (n > 0) store_upto8<STREAMING != kKept>(y + row * p.ldy + col, n, o);
     if constexpr (KEEP) {
         const int64_t codes_at = row * p.code_pitch + col, scale_at = row * p.scale_pitch + (col >> 5);
         auto keep = [&](const float (&v)[8], uint8_t* codes, uint8_t* scales) __attribute__((always_inline)) {
@@ -84,7 +84,7 @@ __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gat
     }
 }
 
-template <class T, int F, bool UP, bool NT>
+template <class T, int F, bool UP, int STREAMING>
 __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ gate_codes,
                                                             const uint8_t* __restrict__ gate_scales, const uint8_t* __restrict__ up_codes,
                                                             const uint8_t* __restrict__ up_scales, T* __restrict__ dgate,
@@ -97,7 +97,7 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict_
     if (n <= 0) return;
     const int64_t codes_at = row * p.code_pitch + col, scale_at = row * p.scale_pitch + (col >> 5);
     float d[8], g[8], u[8], dg[8], du[8];
-    load_upto8<NT>(dy + row * p.ldy + col, n, d);
+    load_upto8<STREAMING == kAll>(dy + row * p.ldy + col, n, d);
     values8_of(*reinterpret_cast<const v2u*>(gate_codes + codes_at), gate_scales[scale_at], g);
     if constexpr (UP) values8_of(*reinterpret_cast<const v2u*>(up_codes + codes_at), up_scales[scale_at], u);
 #pragma unroll
@@ -107,8 +107,8 @@ __global__ __launch_bounds__(kThreads) void act_grad_kernel(const T* __restrict_
         dg[i] = (UP ? d[i] * u[i] : d[i]) * slope;
         du[i] = d[i] * value;
     }
-    store_upto8<NT>(dgate + row * p.ldg + col, n, dg);
-    if constexpr (UP) store_upto8<NT>(dup + row * p.ldu + col, n, du);
+    store_upto8<STREAMING != kKept>(dgate + row * p.ldg + col, n, dg);
+    if constexpr (UP) store_upto8<STREAMING != kKept>(dup + row * p.ldu + col, n, du);
 }
 
 static bool act_params(int64_t rows, int K, int64_t ldg, int64_t ldu, int64_t ldy, ActParams* p) {
@@ -148,10 +148,11 @@ extern "C" sparq_status sparq_mx_act(int32_t function, const void* gate, int64_t
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
-            with_flag(streamed<T>(rows * K * ((up ? 3 : 2) * (int64_t)sizeof(T) + (gate_codes ? 1 : 0) + (up_codes ? 1 : 0))), [&](auto nt) {
-                constexpr bool NT = decltype(nt)::value;
-                if (up) keep ? launch(act_kernel<T, F, true, true, NT>) : launch(act_kernel<T, F, true, false, NT>);
-                else keep ? launch(act_kernel<T, F, false, true, NT>) : launch(act_kernel<T, F, false, false, NT>);
+            const int64_t result = rows * K * (int64_t)sizeof(T);
+            with_streaming<T>((up ? 3 : 2) * result + rows * K * ((gate_codes ? 1 : 0) + (up_codes ? 1 : 0)), result, [&](auto streaming) {
+                constexpr int S = decltype(streaming)::value;
+                if (up) keep ? launch(act_kernel<T, F, true, true, S>) : launch(act_kernel<T, F, true, false, S>);
+                else keep ? launch(act_kernel<T, F, false, true, S>) : launch(act_kernel<T, F, false, false, S>);
             });
         };
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});
@@ -182,9 +183,10 @@ extern "C" sparq_status sparq_mx_act_grad(int32_t function, const void* dy, int6
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
-            with_flag(streamed<T>(rows * K * ((up ? 3 : 2) * (int64_t)sizeof(T) + (up ? 2 : 1))), [&](auto nt) {
-                constexpr bool NT = decltype(nt)::value;
-                up ? launch(act_grad_kernel<T, F, true, NT>) : launch(act_grad_kernel<T, F, false, NT>);
+            const int64_t result = rows * K * (int64_t)sizeof(T);
+            with_streaming<T>((up ? 3 : 2) * result + rows * K * (up ? 2 : 1), (up ? 2 : 1) * result, [&](auto streaming) {
+                constexpr int S = decltype(streaming)::value;
+                up ? launch(act_grad_kernel<T, F, true, S>) : launch(act_grad_kernel<T, F, false, S>);
             });
         };
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});

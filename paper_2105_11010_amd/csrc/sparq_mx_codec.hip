@@ -18,7 +18,7 @@ struct CodecParams {
 // largest magnitude is two exchanges inside a quad, loads are 16 bytes a lane (fp32: twice), codes leave as 4 and 8 bytes a
 // lane and the 16 scales as one byte of every fourth lane.  Bound by memory: 8192 x 8192 bf16 to 4 bits in 27 us (6.35 TB/s), to 8 in 32 (6.4), to
 // both at once in 37 (6.5), fp32 to 4 bits in 52 (5.8); the way back 25.6 (6.6), 30.5 and 43 (7.0).  A large copy: 6.65 TB/s.
-template <class T, bool F4, bool I8, bool NT>
+template <class T, bool F4, bool I8, int STREAMING>
 __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict__ x, uint8_t* __restrict__ codes4,
                                                             uint8_t* __restrict__ scales4, uint8_t* __restrict__ codes8,
                                                             uint8_t* __restrict__ scales8, const CodecParams p) {
@@ -28,7 +28,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict_
     const uint32_t row = fastdiv(item, p.div_chunks);
     const int col = (int)(item - row * p.chunks) * kScaleUnit + 8 * lane;
     float v[8];
-    load_upto8<NT>(x + row * p.ld + col, p.K - col, v);
+    load_upto8<STREAMING == kAll>(x + row * p.ld + col, p.K - col, v);
     const uint32_t top = block_top(v);
     const int64_t scale_at = row * p.scale_pitch + (col >> 5);
     if constexpr (F4) {
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(kThreads) void quantize_kernel(const T* __restrict_
     }
 }
 
-template <class T, int BITS, bool NT>
+template <class T, int BITS, int STREAMING>
 __global__ __launch_bounds__(kThreads) void dequantize_kernel(const uint8_t* __restrict__ codes, const uint8_t* __restrict__ scales,
                                                               T* __restrict__ y, const CodecParams p) {
     const int lane = threadIdx.x & 63;
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(const uint8_t* __r
             if constexpr (BITS == 4) values4_of(*reinterpret_cast<const uint16_t*>(codes + row * p.code4_pitch + (col >> 1)), byte, v);
             else values8_of(v2u{*reinterpret_cast<const uint32_t*>(codes + row * p.code8_pitch + col), 0}, byte, v);
             T* to = y + row * p.ld + col;
-            if (n >= 4) word_to<NT>(to, v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+            if (n >= 4) word_to<STREAMING != kKept>(to, v4u{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
             else {
 #pragma unroll
                 for (int i = 0; i < 3; ++i)
@@ -77,7 +77,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(const uint8_t* __r
     float v[8];
     if constexpr (BITS == 4) values4_of(*reinterpret_cast<const uint32_t*>(codes + row * p.code4_pitch + (col >> 1)), byte, v);
     else values8_of(*reinterpret_cast<const v2u*>(codes + row * p.code8_pitch + col), byte, v);
-    store_upto8<NT>(y + row * p.ld + col, p.K - col, v);
+    store_upto8<STREAMING != kKept>(y + row * p.ld + col, p.K - col, v);
 }
 
 // false: more rows than a launch counts
@@ -96,9 +96,10 @@ sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows,
     const uint32_t grid = (p.items + kWaves - 1) / kWaves;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        with_flag(streamed<T>(rows * (K * (int64_t)sizeof(T) + (codes4 ? p.code4_pitch : 0) + (codes8 ? p.code8_pitch : 0))), [&](auto nt) {
-            constexpr bool NT = decltype(nt)::value;
-            const auto kernel = codes4 && codes8 ? quantize_kernel<T, true, true, NT> : codes4 ? quantize_kernel<T, true, false, NT> : quantize_kernel<T, false, true, NT>;
+        const int64_t bytes = rows * (K * (int64_t)sizeof(T) + (codes4 ? p.code4_pitch : 0) + (codes8 ? p.code8_pitch : 0));
+        with_streaming<T>(bytes, bytes, [&](auto streaming) {
+            constexpr int S = decltype(streaming)::value == kAll ? kAll : kKept;      // (codes are read soon)
+            const auto kernel = codes4 && codes8 ? quantize_kernel<T, true, true, S> : codes4 ? quantize_kernel<T, true, false, S> : quantize_kernel<T, false, true, S>;
             kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(x), static_cast<uint8_t*>(codes4), static_cast<uint8_t*>(scales4),
                                                   static_cast<uint8_t*>(codes8), static_cast<uint8_t*>(scales8), p);
         });
@@ -137,11 +138,14 @@ extern "C" sparq_status sparq_mx_dequantize(const void* codes, const void* scale
     const hipStream_t s = static_cast<hipStream_t>(stream);
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        with_flag(rows * (K * (int64_t)sizeof(T) + code_pitch(K, bits)) >= kStreamedBytes, [&](auto nt) {
-            constexpr bool NT = decltype(nt)::value;
-            const auto kernel = bits == 4 ? dequantize_kernel<T, 4, NT> : dequantize_kernel<T, 8, NT>;
+        const int64_t result = rows * K * (int64_t)sizeof(T), bytes = result + rows * (int64_t)code_pitch(K, bits);
+        const auto launch = [&](auto streaming) {
+            constexpr int S = decltype(streaming)::value;
+            const auto kernel = bits == 4 ? dequantize_kernel<T, 4, S> : dequantize_kernel<T, 8, S>;
             kernel<<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<T*>(y), p);
-        });
+        };
+        if (sizeof(T) == 4 && bytes >= kStreamedBytes) launch(std::integral_constant<int, kAll>{});      // (fp32 here in whole runs of 16 bytes a lane)
+        else with_streaming<T>(bytes, result, launch);
     });
     return launch_status();
 }

@@ -44,12 +44,18 @@ inline bool extent_ok(int64_t rows, int64_t ld) { return rows == 0 || ld <= (INT
 // A call that moves this many bytes streams them past the caches (us, kept -> streamed: 16384 x 8192 bf16 from 4-bit codes 72 -> 47, the gated
 // activation of 8192 x 8192 94 -> 83; 16384 x 4096 bf16 to 4-bit codes, 174 MB, 27 -> 31, and what follows a smaller call finds it there).
 // Not fp32 tensors, whose lanes' halves of 32 bytes go one after the other (16384 x 4096 from 4-bit codes 70 -> 104).
-template <class T>
-inline bool streamed(int64_t bytes) { return sizeof(T) == 2 && bytes >= kStreamedBytes; }
-template <class F>
-inline void with_flag(bool flag, F&& f) {
-    if (flag) f(std::true_type{});
-    else f(std::false_type{});
+// Results of at most 16 MB go past them too (kResults): what a kernel leaves in the XCDs' caches is written back at its end, and with this, not then
+// (us, left -> past, and with a quantiser that reads the result behind it: gated activation 1024 x 4096 7.5 -> 6.5, 10.4 -> 9.4; its gradient 6.8 -> 5.0,
+// 13.4 -> 12.2; 8-bit codes to 2048 x 4096 5.1 -> 4.3, 8.9 -> 8.4; norm 2048 x 4096 9.2 -> 7.5, 17.7 -> 16.7; of larger ones the reader is slower than the
+// writer gains: norm 4096 x 4096 14.5 -> 14.1, 23.4 -> 24.6).
+enum Streaming { kKept, kResults, kAll };
+template <class T, class F>
+inline void with_streaming(int64_t bytes, int64_t results, F&& f) {
+    if constexpr (sizeof(T) == 2) {
+        if (bytes >= kStreamedBytes) return f(std::integral_constant<int, kAll>{});
+        if (results <= 16 << 20) return f(std::integral_constant<int, kResults>{});
+    }
+    f(std::integral_constant<int, kKept>{});
 }
 
 template <class F>
@@ -64,7 +70,7 @@ inline void with_type(int type, F&& f) {
 typedef v4u v4u_at4 __attribute__((aligned(4)));
 typedef v4u v4u_at2 __attribute__((aligned(2)));
 
-// NT: non-temporal, for what is streamed once and is larger than the last-level cache (streamed below).
+// NT: non-temporal, for what is streamed once and is not to stay in the caches (Streaming above).
 template <bool NT, class T>
 __device__ __forceinline__ v4u word_at(const T* p) {
     typedef std::conditional_t<sizeof(T) == 4, const v4u_at4, const v4u_at2> V;

@@ -85,7 +85,7 @@ __device__ __forceinline__ void first_own(const Place& p, float (&v)[8]) {
 // pass over memory, the mean first and the squares of what differs from it second.  As many workgroups as have room go through the rows,
 // gamma and beta in registers and the next row on its way while this one is summed.  Bound by memory and, for each row, by the two sums one after
 // the other: 16384 x 4096 bf16 with checkpoint 60 us (5.6 TB/s), 65536 x 1024 66, fp32 117.
-template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
+template <class T, int WAVES, int CHUNKS, bool WHOLE, int STREAMING>
 __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x, const float* __restrict__ gamma,
                                                         const float* __restrict__ beta, T* __restrict__ y, float* __restrict__ mean_out,
                                                         float* __restrict__ rstd_out, uint8_t* __restrict__ codes,
@@ -102,7 +102,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x,
     auto fetch = [&](int64_t row) __attribute__((always_inline)) {
         row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
 #pragma unroll
-        for (int c = 0; c < CHUNKS; ++c) load_raw<NT>(x + row * p.ldx + at[c].from, raw[c]);
+        for (int c = 0; c < CHUNKS; ++c) load_raw<STREAMING == kAll>(x + row * p.ldx + at[c].from, raw[c]);
     };
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) at[c] = place_of<WHOLE>(c * kSpan + 8 * t, p.K);
@@ -143,7 +143,7 @@ __global__ __launch_bounds__(kThreads) void norm_kernel(const T* __restrict__ x,
             float o[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = (v[c][i] - mean) * rstd * g[c][i] + b[c][i];
-            store_own<WHOLE, NT>(y + row * p.ldy, at[c], o);
+            store_own<WHOLE, STREAMING != kKept>(y + row * p.ldy, at[c], o);
             if (codes && at[c].col - 8 * lane < p.K) {       // the wavefront's 512 values begin inside the row
                 if constexpr (!WHOLE) first_own(at[c], v[c]);
                 if (!at[c].inside) {
@@ -265,7 +265,7 @@ struct ColumnGradients {
 // dx, and the workgroup's share of the weights' gradients, in one pass: WAVES wavefronts take a row, CHUNKS x 8 values a lane, rows part,
 // part + parts, ..., the next row on its way while this one is summed and written.  What the workgroup's wavefronts added up is joined in
 // LDS in their order and leaves as one partial sum.  16384 x 4096 bf16 70 us with the sums' join (4.8 TB/s), 65536 x 1024 64, fp32 118.
-template <class T, int WAVES, int CHUNKS, bool WHOLE, bool NT>
+template <class T, int WAVES, int CHUNKS, bool WHOLE, int STREAMING>
 __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict__ dy, const uint8_t* __restrict__ codes,
                                                              const uint8_t* __restrict__ scales, const float* __restrict__ mean,
                                                              const float* __restrict__ rstd, const float* __restrict__ gamma, T* __restrict__ dx,
@@ -298,7 +298,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict
         row = row < p.rows ? row : p.rows - 1;               // (past the end: a row again, for nobody)
 #pragma unroll
         for (int c = 0; c < CHUNKS; ++c) {
-            load_raw<NT>(dy + row * p.ldy + at[c].from, h.dy[c]);
+            load_raw<STREAMING == kAll>(dy + row * p.ldy + at[c].from, h.dy[c]);
             __builtin_memcpy(&h.x[c], codes + row * p.code_pitch + at[c].from, 8);
             h.scale[c] = scales[row * p.scale_pitch + ((at[c].inside ? at[c].col : at[c].from) >> 5)];
         }
@@ -352,7 +352,7 @@ __global__ __launch_bounds__(kThreads) void norm_grad_kernel(const T* __restrict
                 dg[c][i] += d[c][i] * h[c][i];
                 db[c][i] += d[c][i];
             }
-            store_own<WHOLE, NT>(dx + row * p.ldx, at[c], o);
+            store_own<WHOLE, STREAMING == kAll>(dx + row * p.ldx, at[c], o);
         }
     }
     if (!partial) return;
@@ -487,17 +487,20 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
                 static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, static_cast<uint8_t*>(codes),
                 static_cast<uint8_t*>(scales), p);
         };
-        const auto held = [&](auto whole, auto nt) {
-            constexpr bool W = decltype(whole)::value, NT = decltype(nt)::value;
-            if (K <= 512) launch(norm_kernel<T, 1, 1, W, NT>, 4, 8);
-            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W, NT>, 4, 5);
-            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W, NT>, 1, 8);
-            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W, NT>, 1, 5);
-            else launch(norm_kernel<T, 4, 4, W, NT>, 1, 3);
+        const auto held = [&](auto whole, auto streaming) {
+            constexpr bool W = decltype(whole)::value;
+            constexpr int S = decltype(streaming)::value;
+            if (K <= 512) launch(norm_kernel<T, 1, 1, W, S>, 4, 8);
+            else if (K <= kWaveK) launch(norm_kernel<T, 1, 2, W, S>, 4, 5);
+            else if (K <= 2048) launch(norm_kernel<T, 4, 1, W, S>, 1, 8);
+            else if (K <= 4096) launch(norm_kernel<T, 4, 2, W, S>, 1, 5);
+            else launch(norm_kernel<T, 4, 4, W, S>, 1, 3);
         };
         if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1, 0);
-        else if (K % 8 == 0) with_flag(streamed<T>(rows * K * (2 * (int64_t)sizeof(T) + (codes ? 1 : 0))), [&](auto nt) { held(std::true_type{}, nt); });
-        else held(std::false_type{}, std::false_type{});
+        else if (K % 8 == 0) {
+            const int64_t result = rows * K * (int64_t)sizeof(T);
+            with_streaming<T>(2 * result + (codes ? rows * K : 0), result, [&](auto streaming) { held(std::true_type{}, streaming); });
+        } else held(std::false_type{}, std::integral_constant<int, kKept>{});
     });
     return launch_status();
 }
@@ -534,17 +537,19 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
             const unsigned further = beside ? (unsigned)((K + ColumnGradients::kColumns - 1) / ColumnGradients::kColumns) : 0;
             kernel<<<p.parts + further, kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, to, partial, dgamma, dbeta, p);
         };
-        const auto held = [&](auto whole, auto nt) {
-            constexpr bool W = decltype(whole)::value, NT = decltype(nt)::value;
-            if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W, NT>);
-            else if (K <= kWaveK) launch(norm_grad_kernel<T, 1, 2, W, NT>);
-            else if (K <= 2048) launch(norm_grad_kernel<T, 4, 1, W, NT>);
-            else if (K <= 4096) launch(norm_grad_kernel<T, 4, 2, W, NT>);
-            else launch(norm_grad_kernel<T, 4, 4, W, NT>);
+        const auto held = [&](auto whole, auto streaming) {
+            constexpr bool W = decltype(whole)::value;
+            constexpr int S = decltype(streaming)::value == kAll ? kAll : kKept;      // (dx 2048 x 4096 past the caches: 17.1 -> 17.5 us)
+            if (K <= 512) launch(norm_grad_kernel<T, 1, 1, W, S>);
+            else if (K <= kWaveK) launch(norm_grad_kernel<T, 1, 2, W, S>);
+            else if (K <= 2048) launch(norm_grad_kernel<T, 4, 1, W, S>);
+            else if (K <= 4096) launch(norm_grad_kernel<T, 4, 2, W, S>);
+            else launch(norm_grad_kernel<T, 4, 4, W, S>);
         };
         if (held_in_registers(K)) {
-            if (K % 8 == 0) with_flag(streamed<T>(rows * K * (2 * (int64_t)sizeof(T) + 1)), [&](auto nt) { held(std::true_type{}, nt); });
-            else held(std::false_type{}, std::false_type{});
+            const int64_t result = rows * K * (int64_t)sizeof(T);
+            if (K % 8 == 0) with_streaming<T>(2 * result + rows * K, result, [&](auto streaming) { held(std::true_type{}, streaming); });
+            else held(std::false_type{}, std::integral_constant<int, kKept>{});
         } else {
             norm_grad_rows_kernel<T><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, sums, p);
             norm_grad_columns_kernel<T><<<dim3((unsigned)((K + 8ll * kThreads - 1) / (8 * kThreads)), p.parts), kThreads, 0, s>>>(
