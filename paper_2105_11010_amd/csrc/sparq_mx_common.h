@@ -118,7 +118,14 @@ __device__ __forceinline__ void load_upto8(const T* p, int n, float (&v)[8]) {
     if (n >= 8) load8<NT>(p, v);
     else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)p[i] : 0.0f;
+        for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+        if (n > 0) {                                         // (a branch an element would have one load wait for another)
+            T e[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) e[i] = p[i < n ? i : 0];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = i < n ? (float)e[i] : 0.0f;
+        }
     }
 }
 

@@ -26,9 +26,10 @@ static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
     const auto tiles = [&](int t) { return ((J + t - 1) / t) * ((K + t - 1) / t); };
     // 256 x 256 results, one such tile a CU at a time, or 128 x 128, two a CU: by the rounds that 256 CUs make of them, of which the former's last half
     // as long again (us, 256 -> 128: dx 4096^3 110 -> 144, 3000^3 68 -> 87, 2048^3 42 -> 22; dw 134 -> 168, 85 -> 102, 57 -> 32, of 4096 x 2048 x 4096
-    // 107 -> 84).  64 x 64 where those leave CUs without (128 -> 64: dx 2048^3 24 -> 34, dw 8192 x 1024 x 1024 35 -> 57, 1024 x 4096 x 1024 18 -> 22).
+    // 107 -> 84); dw of a few rows is all results, which two workgroups a CU write better than one (64 x 8192 x 8192 63 -> 47, 256 x 4096 x 4096 24 -> 21).
+    // 64 x 64 where those leave CUs without (128 -> 64: dx 2048^3 24 -> 34, dw 8192 x 1024 x 1024 35 -> 57, 1024 x 4096 x 1024 18 -> 22).
     const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / 16 > 1 ? steps / 16 : 1;
-    p.tile = bf16 && 3 * ((tiles(256) + 255) / 256) <= 2 * ((tiles(128) + 511) / 512) ? 256 : tiles(128) * most >= 192 ? 128 : 64;
+    p.tile = bf16 && !(dw && steps <= 4) && 3 * ((tiles(256) + 255) / 256) <= 2 * ((tiles(128) + 511) / 512) ? 256 : tiles(128) * most >= 192 ? 128 : 64;
     // Few tiles of a long reduction are divided, into as many parts of at least 16 steps as there is room for; shorter ones are over before
     // the parts would be joined, and tiles that fill most CUs gain from two parts only if those are long (us, whole -> two parts: dw 8192 x 3000
     // x 1000 114 -> 90, 8192 x 2048 x 2048 120 -> 106; dx 2048^3 24 -> 27; in parts of 16 steps -> 8: 700 x 1100 x 900 10 -> 14).

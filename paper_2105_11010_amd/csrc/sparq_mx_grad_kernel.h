@@ -242,17 +242,18 @@ struct Products {
 template <class T, int THREADS>
 struct ColumnSums {
     static constexpr int kColumns = THREADS == 1024 ? 64 : 32, kLanes = kColumns / 8, kRows = THREADS / kLanes, kSlices = THREADS / kColumns;
+    static constexpr int kAhead = THREADS == 1024 ? 4 : 2;                     // (beside a product's tiles: in the registers these have)
     static constexpr int kPitch = kColumns + 4, kFloats = kRows * kPitch;
     static __device__ __forceinline__ void run(const T* __restrict__ dy, int64_t ld, int64_t begin, int64_t end, int n, int first, float* __restrict__ sum, float* shared) {
         const int t = threadIdx.x, x = t % kLanes, r0 = t / kLanes, c = first + 8 * x;
         float s[8] = {};
         if (c < n)
-            for (int64_t r = begin + r0; r < end; r += 4 * kRows) {
-                float v[4][8];
+            for (int64_t r = begin + r0; r < end; r += kAhead * kRows) {
+                float v[kAhead][8];
 #pragma unroll
-                for (int u = 0; u < 4; ++u) load_upto8(dy + (r + u * kRows) * ld + c, r + u * kRows < end ? n - c : 0, v[u]);
+                for (int u = 0; u < kAhead; ++u) load_upto8(dy + (r + u * kRows) * ld + c, r + u * kRows < end ? n - c : 0, v[u]);
 #pragma unroll
-                for (int u = 0; u < 4; ++u)
+                for (int u = 0; u < kAhead; ++u)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) s[i] += v[u][i];
             }

@@ -9,9 +9,7 @@ namespace mx {
 // acc[i][j]: 32 x 32 results each, the lane's row 32 j + lane % 32, its columns 32 i + 8 q + 4 (lane / 32) + e (element 4 q + e).
 // They are rounded, turned in 32 x ROW_BYTES of LDS of the wavefront's own and stored in pieces of rows, 16 bytes a lane: stored from where
 // they are, 8 bytes of 32 rows at a time, an 8192 x 8192 bf16 result took 100 us where whole rows take 30.  A row's 16-byte units are
-// permuted by the row, or all rows would be written to the same banks.  The stores go past the caches, so that little is left to be written back at
-// the kernel's end (gemm 8192 x 8192 x 1024 70 -> 59 us, with a quantiser that reads the result behind it 98 -> 93; 2048^3 9.3 -> 8.9, 15.2 -> 14.6;
-// 4096^3 46.2 -> 45.0, 57.2 -> 57.3).
+// permuted by the row, or all rows would be written to the same banks.
 // row0, col0: of the wavefront's first result; bias: one value a column, or a buffer without records for none.
 template <class O, int FI, int FJ, int ROW_BYTES>
 __device__ __forceinline__ void store_results(const v16f (&acc)[FI][FJ], O* out, int64_t ldo, int64_t row0, int64_t rows, int col0, int cols,
@@ -45,7 +43,7 @@ __device__ __forceinline__ void store_results(const v16f (&acc)[FI][FJ], O* out,
                 const v4u w = *reinterpret_cast<const v4u*>(turn + (r + at) * ROW_BYTES + ((unit ^ ((r + at) & (UNITS - 1))) << 4));
                 if (row0 + 32 * j + r + at < rows && n > 0) {
                     O* to = to_piece + (int64_t)(32 * j + r) * ldo;
-                    if (n >= PER) word_to<true>(to, w);
+                    if (n >= PER) __builtin_memcpy(to, &w, 16);
                     else {
                         O v[PER];
                         __builtin_memcpy(v, &w, 16);
