@@ -5,7 +5,7 @@
 // group on its way while this one is multiplied, and their sums are joined in LDS in the wavefronts' order.
 // X not void: A is quantised on the way, by each wavefront for the groups it multiplies, while the weights come.
 // A call for 1 x 4096 x 4096 takes 3.9 us, of which a launch's 3 us and the wait for one round trip to memory are the most: 8.9 MB would pass in
-// 1.3.  1 x 8192 x 8192 (36 MB of weights) takes 9.4, 3.8 TB/s; codes for 64 x 4096 x 4096 8.2.
+// 1.3.  1 x 8192 x 8192 (36 MB of weights) takes 9.4, 3.8 TB/s; codes for 32 x 4096 x 4096 5.6.
 #pragma once
 #include <type_traits>
 

@@ -6,21 +6,23 @@ namespace sparq {
 namespace mx {
 
 struct GemmPlan {
-    int tile;                // 256 or 128: results a workgroup makes along either side; 0: few rows, a kernel of their own
+    int tile;                // 256, 128 or 64: results a workgroup makes along either side; 0: few rows, a kernel of their own
     int parts;               // of the reduction
     size_t bytes;            // of partial results
 };
 static GemmPlan gemm_plan(int64_t M, int N, int K) {
     GemmPlan p = {};
-    // Few rows: the kernel that reads the weights at memory's pace, while its rereading of A is no longer than that (us, it -> 128 x 128 tiles:
-    // 64 x 4096 x 4096 8.2 -> 11, 32 x 8192 x 8192 16 -> 18.5, 48 x 8192 x 8192 20.9 -> 18.6, 64 x 8192 x 8192 24.9 -> 18.6).
-    if (M <= 32 || (M <= kFewMost && M * N * K <= 1ll << 31)) return p;
+    // Few rows: the kernel that reads the weights at memory's pace, while its rereading of A is no longer than that (us, it -> 64 x 64 tiles:
+    // 17 x 4096 x 4096 4.7 -> 6.4, 32 x 4096 x 4096 5.6 -> 7.0, 48 x 4096 x 4096 7.0 -> 6.6, 64 x 4096 x 4096 8.2 -> 6.9, 32 x 8192 x 8192 16 -> 12.5).
+    if (M <= 16 || (M <= kFewMost && M * N * K <= 5ll << 27)) return p;
     const auto tiles = [&](int t) { return ((M + t - 1) / t) * ((N + t - 1) / t); };
     // The larger tiles, one a CU at a time, unless they leave CUs without (us, 256 x 256 -> 128 x 128: 4096^3 47 -> 54, 3584^3 37 -> 47, 3000^3
-    // 30 -> 30, 4096 x 2048 x 4096 34 -> 28, 2900 x 3700 x 2500 30 -> 27, 2048^3 18 -> 10).
-    p.tile = tiles(256) >= 192 ? 256 : 128;
+    // 30 -> 30, 4096 x 2048 x 4096 34 -> 28, 2900 x 3700 x 2500 30 -> 27, 2048^3 18 -> 10; 128 x 128, two a CU, -> 64 x 64, three: 2048^3 9.4 -> 13,
+    // 600 x 3000 x 8192 21.8 -> 23.6, 512 x 3000 x 2048 7.8 -> 7.3, 200 x 3000 x 3000 9.0 -> 6.1, 515 x 771 x 577 5.9 -> 4.5): what a CU can load of
+    // codes bounds each of them.
+    p.tile = tiles(256) >= 192 ? 256 : tiles(128) >= 112 ? 128 : 64;
     // Few tiles of a long reduction are divided; shorter ones, or more of them, are over before the parts would be joined (us, whole -> in
-    // parts: 128 x 1024 x 8192 16.2 -> 13.6, 65 x 8192 x 8192 18.6 -> 16.8, 128 x 4096 x 4096 11.3 -> 14.6, 512 x 4096 x 4096 12 -> 23).
+    // parts: 70 x 300 x 16000 17.2 -> 9.6, 65 x 1000 x 8192 10.2 -> 9.3; with up to 128 tiles of 32 steps: 100 x 500 x 4096 6.7 -> 8.7).
     const int64_t n = tiles(p.tile), steps = (K + kCodeUnit - 1) / kCodeUnit, most = steps / 16;
     p.parts = n <= 64 && steps >= 64 ? (int)(128 / n < most ? 128 / n : most) : 1;
     p.bytes = p.parts > 1 ? (size_t)round_up(p.parts * M * N * 4, 256) : 0;
@@ -79,7 +81,7 @@ static sparq_status gemm(const void* a, const void* as, const void* w, const voi
     with_type(parted ? SPARQ_MX_F32 : type, [&](auto o) {
         typedef decltype(o) O;
         void* to = parted ? workspace : y;
-        s = t == 256 ? launch_tile<O, 256>(p, to, stream) : launch_tile<O, 128>(p, to, stream);
+        s = t == 256 ? launch_tile<O, 256>(p, to, stream) : t == 128 ? launch_tile<O, 128>(p, to, stream) : launch_tile<O, 64>(p, to, stream);
     });
     if (s != SPARQ_OK || !parted) return s;
     return launch_join(static_cast<const float*>(workspace), bias, y, type, M, N, ldy, parts, stream);

@@ -93,9 +93,9 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         if constexpr (TM == 256) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ras, (LdsPtr)to, 16, scales_from, (load_step >> 2) * 16, 0, 0);
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rws, (LdsPtr)(to + TM * 16), 16, scales_from, (load_step >> 2) * 16, 0, 0);
-        } else if (wave < 2) {
+        } else if (wave < TM / 64) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(ras, (LdsPtr)to, 16, scales_from, (load_step >> 2) * 16, 0, 0);
-        } else {
+        } else if (wave < TM / 32) {
             __builtin_amdgcn_raw_ptr_buffer_load_lds(rws, (LdsPtr)to, 16, scales_from - TM * p.scale_pitch, (load_step >> 2) * 16, 0, 0);
         }
     };
@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         if (i < TM / 64) __builtin_amdgcn_raw_ptr_buffer_load_lds(ra, (LdsPtr)to, 16, from[i], col, 0, 0);
         else __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, (LdsPtr)to, 16, from[i - TM / 64], col, 0, 0);
     };
-    static_assert(TM == TN && (TM == 256 || TM == 128), "rows of scales: one load a wavefront and operand, or one a wavefront");
+    static_assert(TM == TN && (TM == 256 || TM == 128 || TM == 64), "rows of scales: one load a wavefront and operand, or one a wavefront at most");
 
     struct Operands {
         v4i a[FM], w[FN];
@@ -184,7 +184,9 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
             for (int n = reads.first; n < reads.second; ++n) read(first, (place + 1) & 3, 0, n);
             if (place == 0 && i == 0) load_scales(group ^ 1);
             for (int n = loads.first; n < loads.second; ++n) load(place, n);
-            if (2 * i >= kAll)
+            if (kAll == 1) {
+                for (int n = 0; n < kReads; ++n) shift_scale(next_scales, n);
+            } else if (2 * i >= kAll)
                 for (int n = early.first - kReads; n < last - kReads; ++n) shift_scale(next_scales, n);
         });
         scales = next_scales;

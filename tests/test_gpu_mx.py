@@ -184,7 +184,7 @@ def test_product(sq, M, N, K, t, bias, pad, at):
 
 
 # many results, so that the largest tiles are used: whole ones, cut ones, and reductions that end inside a step or before the first ends
-@pytest.mark.parametrize("M,N,K", [(4100, 3300, 100), (4096, 3328, 640), (3333, 4001, 1500)])
+@pytest.mark.parametrize("M,N,K", [(4100, 3300, 100), (4096, 3328, 640), (3333, 4001, 1500), (1500, 1300, 700), (1409, 1300, 129), (2001, 960, 1100)])
 @pytest.mark.parametrize("t,bias", [("bf16", True), ("f32", False)])
 def test_product_in_large_tiles(sq, M, N, K, t, bias):
     test_product(sq, M, N, K, t, bias, 0, 0)
