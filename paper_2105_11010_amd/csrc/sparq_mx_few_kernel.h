@@ -73,13 +73,45 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
     for (int group = wave; group < p.groups; group += WAVES) {
         const Group now = held;
         if constexpr (kQuantise) {
-            const int col = group * kScaleUnit + 8 * lane;
-            const X* x = static_cast<const X*>(p.x) + col;
+            // (Four rows' loads at once, none in a branch that would have one wait for another: lanes past a row's whole runs read its first.)
+            const int col = group * kScaleUnit + 8 * lane, n = p.K - col;
+            const X* const x = static_cast<const X*>(p.x);
             for (int m0 = 0; m0 < p.M; m0 += 4) {
                 float v[4][8];
+                const X* row[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (m0 + i < p.M) load_upto8(x + (m0 + i) * p.ldx, p.K - col, v[i]);
+                for (int i = 0; i < 4; ++i) row[i] = x + (m0 + i < p.M ? m0 + i : p.M - 1) * p.ldx;
+                if (p.K >= 8) {
+                    Raw8<X> raw[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        raw[i] = Raw8<X>{};
+                        if (m0 + i < p.M) load_raw<false>(row[i] + (n >= 8 ? col : 0), raw[i]);
+                    }
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        if (m0 + i >= p.M) break;
+                        values_of(raw[i], v[i]);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[i][e] = n >= 8 ? v[i][e] : 0.0f;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[i][e] = 0.0f;
+                }
+                if (p.K % 8 && n > 0 && n < 8) {             // the lane that holds a row's end
+                    X end[4][8];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) end[i][e] = row[i][col + (e < n ? e : 0)];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) v[i][e] = e < n ? (float)end[i][e] : 0.0f;
+                }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     if (m0 + i >= p.M) break;

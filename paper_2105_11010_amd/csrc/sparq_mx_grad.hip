@@ -21,18 +21,22 @@ struct GradPlan {
     int slabs;               // of rows for the column sums
     size_t partial_bytes, bytes;
 };
-static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
+static GradPlan grad_plan(int dy_type, int64_t J, int64_t R, int K, bool dw) {
     GradPlan p = {};
     const auto tiles = [&](int t) { return ((J + t - 1) / t) * ((K + t - 1) / t); };
     // 256 x 256 results, one such tile a CU at a time, or 128 x 128, two a CU: by the rounds that 256 CUs make of them, of which the former's last half
     // as long again (us, 256 -> 128: dx 4096^3 110 -> 144, 3000^3 68 -> 87, 2048^3 42 -> 22; dw 134 -> 168, 85 -> 102, 57 -> 32, of 4096 x 2048 x 4096
     // 107 -> 84); dw of a few rows is all results, which two workgroups a CU write better than one (64 x 8192 x 8192 63 -> 47, 256 x 4096 x 4096 24 -> 21).
     // 64 x 64 where those leave CUs without (128 -> 64: dx 2048^3 24 -> 34, dw 8192 x 1024 x 1024 35 -> 57, 1024 x 4096 x 1024 18 -> 22).
-    const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / 16 > 1 ? steps / 16 : 1;
+    const bool bf16 = dy_type == SPARQ_MX_BF16;
+    const int64_t least = (bf16 ? 16 : dy_type == SPARQ_MX_F16 ? 8 : 6) >> (J * K <= 1 << 17 ? 1 : 0);       // steps of a part, by what one takes
+    const int64_t steps = (R + kGradStep - 1) / kGradStep, most = steps / least > 1 ? steps / least : 1;
     p.tile = bf16 && !(dw && steps <= 4) && 3 * ((tiles(256) + 255) / 256) <= 2 * ((tiles(128) + 511) / 512) ? 256 : tiles(128) * most >= 192 ? 128 : 64;
-    // Few tiles of a long reduction are divided, into as many parts of at least 16 steps as there is room for; shorter ones are over before
-    // the parts would be joined, and tiles that fill most CUs gain from two parts only if those are long (us, whole -> two parts: dw 8192 x 3000
-    // x 1000 114 -> 90, 8192 x 2048 x 2048 120 -> 106; dx 2048^3 24 -> 27; in parts of 16 steps -> 8: 700 x 1100 x 900 10 -> 14).
+    // Few tiles of a long reduction are divided, into as many parts of at least `least` steps as there is room for (us, of 16 steps -> of these: dw 1648
+    // x 217 x 55 fp16 20.7 -> 12.3, 1757 x 1234 x 114 fp32 31 -> 17, 1664 x 17 x 39 bf16 13.5 -> 10.4; dx 24 x 3008 x 49 fp16 18.9 -> 13.0; bf16 in parts of
+    // eight where there are more results: 700 x 1100 x 900 10 -> 14); shorter ones are over before the parts would be joined, and tiles that fill
+    // most CUs gain from two parts only if those are long (whole -> two parts: dw 8192 x 3000 x 1000 114 -> 90, 8192 x 2048 x 2048 120 -> 106; dx
+    // 2048^3 24 -> 27).
     const int64_t n = tiles(p.tile), places = (p.tile == 128 ? (bf16 ? 512 : 256) : 1024) / n, parts = places < most ? places : most;
     const bool divided = p.tile != 256 && (n < 192 || (n <= 256 && steps >= 64));
     p.parts = !divided || parts < 1 ? 1 : (int)(parts > 64 ? 64 : parts);
@@ -42,10 +46,14 @@ static GradPlan grad_plan(bool bf16, int64_t J, int64_t R, int K, bool dw) {
     p.bytes = p.partial_bytes + (p.slabs > 1 ? (size_t)round_up((int64_t)p.slabs * J * 4, 256) : 0);
     return p;
 }
-// The workspace does not depend on dy's type: the larger.
+// The workspace does not depend on dy's type: the largest.
 static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
-    const size_t a = grad_plan(false, J, R, K, dw).bytes, b = grad_plan(true, J, R, K, dw).bytes;
-    return a > b ? a : b;
+    size_t most = 0;
+    for (const int type : {SPARQ_MX_F32, SPARQ_MX_F16, SPARQ_MX_BF16}) {
+        const size_t bytes = grad_plan(type, J, R, K, dw).bytes;
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 // Steps that are read without checks, in runs of eight: none if rows' distances do not fit the loads' 32-bit offsets.  A run that dw's last
 // column cuts reads on into the next rows (one, unless rows are shorter than a run): the last rows, which it would leave, are not among them.
@@ -117,7 +125,7 @@ extern "C" sparq_status sparq_mx_linear_dx(const void* dy, int32_t dy_type, int6
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
     if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan(dy_type == SPARQ_MX_BF16, M, N, K, false);
+    const GradPlan plan = grad_plan(dy_type, M, N, K, false);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     return grad(dy, dy_type, lddy, w_codes, w_scales, 4, dx, dx_type, lddx, nullptr, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
@@ -130,7 +138,7 @@ extern "C" sparq_status sparq_mx_linear_dw(const void* dy, int32_t dy_type, int6
     if (!tensor_ok(dw, dw_type, lddw, K) || !extent_ok(N, lddw) || !aligned(db, 4)) return SPARQ_EINVAL;
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K)))
         return SPARQ_EINVAL;
-    const GradPlan plan = grad_plan(dy_type == SPARQ_MX_BF16, N, M, K, true);
+    const GradPlan plan = grad_plan(dy_type, N, M, K, true);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
     const hipStream_t s = static_cast<hipStream_t>(stream);

@@ -191,7 +191,7 @@ def test_product_in_large_tiles(sq, M, N, K, t, bias):
 
 
 # few results of a long reduction, which is divided; few rows whose weights are too many for x to be quantised on the way; most of the few rows
-@pytest.mark.parametrize("M,N,K", [(70, 100, 8300), (130, 65, 9000), (16, 3000, 3000), (64, 515, 2056), (49, 2000, 1100)])
+@pytest.mark.parametrize("M,N,K", [(70, 100, 8300), (130, 65, 9000), (16, 3000, 3000), (64, 515, 2056), (49, 2000, 1100), (15, 53, 128), (7, 40, 5), (13, 65, 735), (6, 33, 1031)])
 @pytest.mark.parametrize("t,bias,pad,at", [("bf16", True, 0, 0), ("f32", False, 3, 1)])
 def test_product_of_other_shapes(sq, M, N, K, t, bias, pad, at):
     test_product(sq, M, N, K, t, bias, pad, at)
@@ -271,7 +271,7 @@ def test_product_gradients_of_wider_types(sq, J, R, K, t, o, pad, at):
 
 
 # fewer columns of dy than a read takes, whose reads run on into the next rows; bias gradients of a few rows, of slabs, and of many elements
-@pytest.mark.parametrize("M,N,K", [(700, 1, 300), (577, 2, 128), (640, 5, 64), (131, 7, 100), (900, 9, 130), (1000, 200, 333), (2100, 2100, 64), (1040, 4101, 33)])
+@pytest.mark.parametrize("M,N,K", [(700, 1, 300), (577, 2, 128), (640, 5, 64), (131, 7, 100), (900, 9, 130), (1000, 200, 333), (24, 3008, 49), (1757, 300, 114), (2100, 2100, 64), (1040, 4101, 33)])
 @pytest.mark.parametrize("t,o,pad,at", [("bf16", "f32", 0, 0), ("f16", "f16", 1, 0), ("f32", "f32", 0, 0)])
 def test_product_gradients_of_few_columns(sq, M, N, K, t, o, pad, at):
     test_product_gradients(sq, M, N, K, t, o, pad, at)
