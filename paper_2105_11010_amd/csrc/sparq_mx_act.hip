@@ -16,19 +16,21 @@ struct ActParams {
     FastDiv div_chunks;
 };
 
-// f(v) and f'(v).  PRECISE (fp32 tensors): the library's exponential and division; else the instructions' (2 and 1 ulp of fp32),
-// far below what a 16-bit result keeps.
+// f(v) and f'(v).  PRECISE (fp32 tensors): the library's exponential, erfc and division; else the instructions' (2 and 1 ulp of fp32) and the
+// approximation below, whose errors are relative ones far below what a 16-bit result keeps, below 0 as well, where f is all tail.
 template <bool PRECISE>
 __device__ __forceinline__ float sigmoid(float v) {
     if constexpr (PRECISE) return 1.0f / (1.0f + expf(-v));
     else return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(v * -1.44269504f));
 }
-// The normal distribution's integral and exp(-v^2 / 2), for 16-bit results: erfc by Abramowitz and Stegun's formula 7.1.26, a
-// polynomial in 1 / (1 + 0.3275911 |v| / sqrt 2) times that exponential, whose error is 1.5e-7 (half of it in the integral).
+// The normal distribution's integral and exp(-v^2 / 2), for 16-bit results.  Below 0 the integral is that exponential times a function that
+// falls like 1 / |v|: t p(t), t = 1 / (1 + 0.264 |v|), p fitted to the least largest relative error for |v| up to 13.5 (beyond, the exponential is
+// zero), 5.4e-7.  With fp32's roundings, most of them of v^2 in the exponent, the integral is off by at most (32 + 2 v^2) 2^-24 of itself.
 __device__ __forceinline__ float normal_integral(float v, float& density) {
-    const float t = __builtin_amdgcn_rcpf(1.0f + 0.231641888f * __builtin_fabsf(v));
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.264f * __builtin_fabsf(v));
     density = __builtin_amdgcn_exp2f(v * v * -0.721347520f);
-    const float tail = 0.5f * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f)))) * density;
+    const float p = 0.10517378f + t * (0.10781906f + t * (0.08047569f + t * (0.14862743f + t * (-0.076199844f + t * (0.20336618f + t * -0.06926256f)))));
+    const float tail = t * p * density;
     return v < 0.0f ? tail : 1.0f - tail;
 }
 template <int F, bool PRECISE>
@@ -54,7 +56,7 @@ __device__ __forceinline__ void function_and_slope(float v, float& value, float&
 }
 
 // A wavefront takes 512 values of a row, a lane eight, as the quantiser does.  8192 x 8192 bf16, gated, with both checkpoints: silu 83 us
-// (6.5 TB/s), bound by memory, as is its gradient (83); gelu 92-95 and 91-94, bound by its arithmetic; fp32 silu 163 and 170.
+// (6.5 TB/s), bound by memory, as is its gradient (83); gelu 93-95 and 87-89, bound by its arithmetic; fp32 silu 163 and 170.
 template <class T, int F, bool UP, bool KEEP, int STREAMING>
 __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gate, const T* __restrict__ up, T* __restrict__ y,
                                                        uint8_t* __restrict__ gate_codes, uint8_t* __restrict__ gate_scales,

@@ -1,0 +1,76 @@
+"""The microscaled operators on the GPU over what their types hold: every 16-bit value through the activations.
+Against the plain reference in 64 bits (tests/mx_reference.py); tolerances stand at the tests, fixed before any run.
+u = 2^-24 is fp32's unit roundoff."""
+import numpy as np
+import pytest
+import torch
+
+import mx_reference as R
+from test_gpu_mx import DEV, TYPES, Result, close, coded_buffers, matrix, sq, u  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+# ---- activations -------------------------------------------------------------------------------------------------------------
+def all_values(t):
+    """Every finite value of a 16-bit type, as float64."""
+    bits = torch.arange(1 << 16, dtype=torch.int32).to(torch.int16).view(TYPES[t]).double()
+    return bits[bits.isfinite()].numpy()
+
+
+def relative(name, v):
+    """The relative error of f(v), and of the factor of v in it, before it is rounded to 16 bits.  gelu: 9 u of the fitted function, 3 u v^2 log2(e)/2
+    ln 2 = 1.5 v^2 u of the exponent's three roundings, 20 u of the others.  silu: 2 u |v| of the exponent's two, 8 u of the others."""
+    return (32 + 2 * v * v) * u if name == "gelu" else (8 + 2 * np.abs(v)) * u
+
+
+# What fp32 does not hold between: the exponential below 2^-126 (gelu), a quotient below 2^-126 (silu), times |v| < 128 there.
+LEAST = 2.0 ** -119
+
+
+@pytest.mark.parametrize("name", ("silu", "gelu"))
+@pytest.mark.parametrize("t", ("f16", "bf16"))
+def test_act_of_every_16_bit_value(sq, name, t):  # noqa: F811
+    """Relative to the value itself, in the far tail as elsewhere."""
+    v = all_values(t)[None]
+    y = Result(1, v.shape[1], t)
+    sq.sparq_mx_act(name, matrix(v, t), y.view)
+    with np.errstate(over="ignore"):
+        f = R.function(name, v)
+        off = np.where(np.abs(v) < 1e3, relative(name, np.clip(v, -1e3, 1e3)), 8 * u) * np.abs(f)
+    close(y.get(), f, off + LEAST, t)
+
+
+@pytest.mark.parametrize("name", ("silu", "gelu"))
+@pytest.mark.parametrize("t", ("f16", "bf16"))
+def test_act_gradient_over_the_tail(sq, name, t):  # noqa: F811
+    """Checkpoints of blocks of every power of two up to 16: all their codes, so that the tail is met in every binade.  f' = c + v c' with c in
+    (0, 1): the two terms' errors, relative each, and the sum's rounding."""
+    k = np.arange(-127, 128)
+    x = np.concatenate([np.concatenate([np.append(np.sign(k[i]) * 127, k[i:i + 31]) for i in range(0, 255, 31)] + [np.zeros(32)])[: 32 * 9] * 2.0 ** (e - 6)
+                        for e in range(-4, 5)])
+    x = np.where(np.arange(x.size) % 32 == 0, np.where(x == 0, 127 * 2.0 ** -20, x), x)[None]
+    c, s = coded_buffers(sq, 1, x.shape[1], 8)
+    sq.sparq_mx_quantize(matrix(x, "f32"), codes8=c.t, scales8=s.t)
+    X = R.quantised(x, 8)
+    assert X.min() < -15 and X.max() > 15
+    dg, du = Result(1, x.shape[1], t), Result(1, x.shape[1], t)
+    one = matrix(np.ones_like(x), t)
+    sq.sparq_mx_act_grad(name, one, c.t, s.t, dg.view, up_codes=c.t, up_scales=s.t, dup=du.view)
+    f, d = R.function(name, X), R.slope(name, X)
+    factor = f / np.where(X == 0, 1, X)
+    close(du.get(), f, relative(name, X) * np.abs(f) + LEAST, t)
+    # dgate = dy up f', here X f'
+    off = (relative(name, X) + 4 * u) * (np.abs(factor) + np.abs(d - factor)) * np.abs(X)
+    close(dg.get(), X * d, off + LEAST, t)
+
+
+@pytest.mark.parametrize("name", ("silu", "gelu"))
+def test_act_of_fp32_over_the_tail(sq, name):  # noqa: F811
+    """fp32 goes through the library's functions, 32 u (16 units of the last place) and a few roundings; the exponent's or erfc's argument, off by
+    2 u, adds 2 u |v| or 2 u v^2."""
+    v = torch.linspace(-13, 13, 52001, dtype=torch.float64).float().double().numpy()[None]
+    y = Result(1, v.shape[1], "f32")
+    sq.sparq_mx_act(name, matrix(v, "f32"), y.view)
+    f = R.function(name, v)
+    close(y.get(), f, (40 + (2 * v * v if name == "gelu" else 2 * np.abs(v))) * u * np.abs(f) + LEAST, "f32")
