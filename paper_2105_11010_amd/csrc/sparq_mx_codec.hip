@@ -80,7 +80,7 @@ __global__ __launch_bounds__(kThreads) void dequantize_kernel(const uint8_t* __r
     store_upto8<STREAMING != kKept>(y + row * p.ld + col, p.K - col, v);
 }
 
-// false: more rows than a launch counts
+// false: more rows than a call counts
 static bool codec_params(int64_t rows, int K, int64_t ld, CodecParams* p) {
     const int64_t chunks = (K + kScaleUnit - 1) / kScaleUnit, items = rows * chunks;
     if (rows >= (1ll << 31) || items >= (1ll << 31)) return false;
@@ -89,22 +89,35 @@ static bool codec_params(int64_t rows, int K, int64_t ld, CodecParams* p) {
     return true;
 }
 
+// f(p, grid, first): launches for the rows from `first` on, p of as many of them as a launch takes
+template <class F>
+static sparq_status in_codec_launches(int64_t rows, CodecParams p, F&& f) {
+    return in_launches(rows, 64ll * p.chunks, [&](int64_t first, int64_t n) {
+        p.items = (uint32_t)(n * p.chunks);
+        f(p, (p.items + kWaves - 1) / kWaves, first);
+        return launch_status();
+    });
+}
+
 sparq_status launch_quantize(const void* x, int type, int64_t ldx, int64_t rows, int K, void* codes4, void* scales4, void* codes8,
                              void* scales8, hipStream_t stream) {
     CodecParams p;
     if (!codec_params(rows, K, ldx, &p)) return SPARQ_EUNSUPPORTED;
-    const uint32_t grid = (p.items + kWaves - 1) / kWaves;
+    sparq_status s = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const int64_t bytes = rows * (K * (int64_t)sizeof(T) + (codes4 ? p.code4_pitch : 0) + (codes8 ? p.code8_pitch : 0));
         with_streaming<T>(bytes, bytes, [&](auto streaming) {
             constexpr int S = decltype(streaming)::value == kAll ? kAll : kKept;      // (codes are read soon)
             const auto kernel = codes4 && codes8 ? quantize_kernel<T, true, true, S> : codes4 ? quantize_kernel<T, true, false, S> : quantize_kernel<T, false, true, S>;
-            kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(x), static_cast<uint8_t*>(codes4), static_cast<uint8_t*>(scales4),
-                                                  static_cast<uint8_t*>(codes8), static_cast<uint8_t*>(scales8), p);
+            s = in_codec_launches(rows, p, [&](const CodecParams& q, uint32_t grid, int64_t first) {
+                kernel<<<grid, kThreads, 0, stream>>>(static_cast<const T*>(x) + first * ldx, row_of(codes4, first, p.code4_pitch),
+                                                      row_of(scales4, first, p.scale_pitch), row_of(codes8, first, p.code8_pitch),
+                                                      row_of(scales8, first, p.scale_pitch), q);
+            });
         });
     });
-    return launch_status();
+    return s;
 }
 
 }  // namespace mx
@@ -134,18 +147,21 @@ extern "C" sparq_status sparq_mx_dequantize(const void* codes, const void* scale
     if (!tensor_ok(y, type, ldy, K) || !extent_ok(rows, ldy) || !extent_ok(rows, K) || !coded_ok(codes, scales)) return SPARQ_EINVAL;
     CodecParams p;
     if (!codec_params(rows, K, ldy, &p)) return SPARQ_EUNSUPPORTED;
-    const uint32_t grid = (p.items + kWaves - 1) / kWaves;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const hipStream_t stream_ = static_cast<hipStream_t>(stream);
+    sparq_status s = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const int64_t result = rows * K * (int64_t)sizeof(T), bytes = result + rows * (int64_t)code_pitch(K, bits);
         const auto launch = [&](auto streaming) {
             constexpr int S = decltype(streaming)::value;
             const auto kernel = bits == 4 ? dequantize_kernel<T, 4, S> : dequantize_kernel<T, 8, S>;
-            kernel<<<grid, kThreads, 0, s>>>(static_cast<const uint8_t*>(codes), static_cast<const uint8_t*>(scales), static_cast<T*>(y), p);
+            s = in_codec_launches(rows, p, [&](const CodecParams& q, uint32_t grid, int64_t first) {
+                kernel<<<grid, kThreads, 0, stream_>>>(row_of(codes, first, code_pitch(K, bits)), row_of(scales, first, p.scale_pitch),
+                                                       static_cast<T*>(y) + first * ldy, q);
+            });
         };
         if (sizeof(T) == 4 && bytes >= kStreamedBytes) launch(std::integral_constant<int, kAll>{});      // (fp32 here in whole runs of 16 bytes a lane)
         else with_streaming<T>(bytes, result, launch);
     });
-    return launch_status();
+    return s;
 }

@@ -58,6 +58,20 @@ inline void with_streaming(int64_t bytes, int64_t results, F&& f) {
     f(std::integral_constant<int, kKept>{});
 }
 
+// A launch has fewer than 2^32 threads along an axis, and of a larger grid only what is left over is run, without an error: f(first, rows) for as
+// many rows at a time as make 2^31 threads.
+template <class F>
+inline sparq_status in_launches(int64_t rows, int64_t threads_a_row, F&& f) {
+    const int64_t most = (1ll << 31) / threads_a_row;
+    sparq_status s = SPARQ_OK;
+    for (int64_t first = 0; first < rows && s == SPARQ_OK; first += most) s = f(first, rows - first < most ? rows - first : most);
+    return s;
+}
+
+// Row `first` of codes or scales (NULL: none)
+inline uint8_t* row_of(void* p, int64_t first, int64_t pitch) { return p ? static_cast<uint8_t*>(p) + first * pitch : nullptr; }
+inline const uint8_t* row_of(const void* p, int64_t first, int64_t pitch) { return p ? static_cast<const uint8_t*>(p) + first * pitch : nullptr; }
+
 template <class F>
 inline void with_type(int type, F&& f) {
     if (type == SPARQ_MX_F32) f(float{});

@@ -1,4 +1,5 @@
-"""The microscaled operators on the GPU over what their types hold: every 16-bit value through the activations.
+"""The microscaled operators on the GPU over what their types hold and what a launch counts: every 16-bit value through the activations, calls of more
+rows or columns than one launch takes.
 Against the plain reference in 64 bits (tests/mx_reference.py); tolerances stand at the tests, fixed before any run.
 u = 2^-24 is fp32's unit roundoff."""
 import numpy as np
@@ -74,3 +75,36 @@ def test_act_of_fp32_over_the_tail(sq, name):  # noqa: F811
     sq.sparq_mx_act(name, matrix(v, "f32"), y.view)
     f = R.function(name, v)
     close(y.get(), f, (40 + (2 * v * v if name == "gelu" else 2 * np.abs(v))) * u * np.abs(f) + LEAST, "f32")
+
+
+# ---- what a launch counts ----------------------------------------------------------------------------------------------------
+# A launch has fewer than 2^32 threads along an axis; calls within the documented sizes that would need more.  Each is held, to the bit, to
+# calls for its pieces.
+def coded(sq, rows, K, bits):  # noqa: F811
+    return (torch.zeros(rows, sq.sparq_mx_code_bytes(K, bits), dtype=torch.uint8, device=DEV),
+            torch.zeros(rows, sq.sparq_mx_scale_bytes(K), dtype=torch.uint8, device=DEV))
+
+
+@pytest.fixture
+def emptied():
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_codec_of_more_rows_than_a_launch_has_wavefronts(sq, emptied):  # noqa: F811
+    rows, K, piece = (1 << 26) + 5, 1, 1 << 25
+    x = torch.randn(rows, K, device=DEV, dtype=torch.float16, generator=torch.Generator(DEV).manual_seed(21))
+    for bits in (4, 8):
+        c, s = coded(sq, rows, K, bits)
+        sq.sparq_mx_quantize(x, **{f"codes{bits}": c, f"scales{bits}": s})
+        y = torch.full_like(x, 7.0)
+        sq.sparq_mx_dequantize(c, s, bits, y)
+        for r in range(0, rows, piece):
+            p = slice(r, min(rows, r + piece))
+            c1, s1 = coded(sq, p.stop - r, K, bits)
+            sq.sparq_mx_quantize(x[p], **{f"codes{bits}": c1, f"scales{bits}": s1})
+            assert torch.equal(c[p], c1) and torch.equal(s[p], s1), (bits, r)
+            y1 = torch.full_like(x[p], 9.0)
+            sq.sparq_mx_dequantize(c1, s1, bits, y1)
+            assert torch.equal(y[p], y1), (bits, r)
