@@ -120,6 +120,15 @@ static bool act_params(int64_t rows, int K, int64_t ldg, int64_t ldu, int64_t ld
           make_fastdiv((uint32_t)chunks)};
     return true;
 }
+// f(p, grid, first): launches for the rows from `first` on, p of as many of them as a launch takes
+template <class F>
+static sparq_status in_act_launches(int64_t rows, ActParams p, F&& f) {
+    return in_launches(rows, 64ll * p.chunks, [&](int64_t first, int64_t n) {
+        p.items = (uint32_t)(n * p.chunks);
+        f(p, (p.items + kWaves - 1) / kWaves, first);
+        return launch_status();
+    });
+}
 static bool function_valid(int f) { return f == SPARQ_MX_SILU || f == SPARQ_MX_GELU; }
 
 }  // namespace mx
@@ -138,15 +147,17 @@ extern "C" sparq_status sparq_mx_act(int32_t function, const void* gate, int64_t
     if (!coded_ok_or_none(gate_codes, gate_scales) || !coded_ok_or_none(up_codes, up_scales) || (up_codes && !up)) return SPARQ_EINVAL;
     ActParams p;
     if (!act_params(rows, K, ldg, ldu, ldy, &p)) return SPARQ_EUNSUPPORTED;
-    const uint32_t grid = (p.items + kWaves - 1) / kWaves;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
+    sparq_status s = SPARQ_OK;
     const bool keep = gate_codes || up_codes;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const auto launch = [&](auto kernel) {
-            kernel<<<grid, kThreads, 0, s>>>(static_cast<const T*>(gate), static_cast<const T*>(up), static_cast<T*>(y),
-                                             static_cast<uint8_t*>(gate_codes), static_cast<uint8_t*>(gate_scales),
-                                             static_cast<uint8_t*>(up_codes), static_cast<uint8_t*>(up_scales), p);
+            s = in_act_launches(rows, p, [&](const ActParams& q, uint32_t grid, int64_t first) {
+                kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+                    static_cast<const T*>(gate) + first * ldg, up ? static_cast<const T*>(up) + first * ldu : nullptr, static_cast<T*>(y) + first * ldy,
+                    row_of(gate_codes, first, p.code_pitch), row_of(gate_scales, first, p.scale_pitch), row_of(up_codes, first, p.code_pitch),
+                    row_of(up_scales, first, p.scale_pitch), q);
+            });
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
@@ -160,7 +171,7 @@ extern "C" sparq_status sparq_mx_act(int32_t function, const void* gate, int64_t
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});
         else of(std::integral_constant<int, SPARQ_MX_GELU>{});
     });
-    return launch_status();
+    return s;
 }
 
 extern "C" sparq_status sparq_mx_act_grad(int32_t function, const void* dy, int64_t lddy, const void* gate_codes, const void* gate_scales,
@@ -174,14 +185,16 @@ extern "C" sparq_status sparq_mx_act_grad(int32_t function, const void* dy, int6
     if (!coded_ok(gate_codes, gate_scales) || (up && !coded_ok(up_codes, up_scales))) return SPARQ_EINVAL;
     ActParams p;
     if (!act_params(rows, K, lddg, lddu, lddy, &p)) return SPARQ_EUNSUPPORTED;
-    const uint32_t grid = (p.items + kWaves - 1) / kWaves;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
+    sparq_status s = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const auto launch = [&](auto kernel) {
-            kernel<<<grid, kThreads, 0, s>>>(static_cast<const T*>(dy), static_cast<const uint8_t*>(gate_codes),
-                                             static_cast<const uint8_t*>(gate_scales), static_cast<const uint8_t*>(up_codes),
-                                             static_cast<const uint8_t*>(up_scales), static_cast<T*>(dgate), static_cast<T*>(dup), p);
+            s = in_act_launches(rows, p, [&](const ActParams& q, uint32_t grid, int64_t first) {
+                kernel<<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+                    static_cast<const T*>(dy) + first * lddy, row_of(gate_codes, first, p.code_pitch), row_of(gate_scales, first, p.scale_pitch),
+                    row_of(up_codes, first, p.code_pitch), row_of(up_scales, first, p.scale_pitch), static_cast<T*>(dgate) + first * lddg,
+                    up ? static_cast<T*>(dup) + first * lddu : nullptr, q);
+            });
         };
         const auto of = [&](auto f) {
             constexpr int F = decltype(f)::value;
@@ -194,5 +207,5 @@ extern "C" sparq_status sparq_mx_act_grad(int32_t function, const void* dy, int6
         if (function == SPARQ_MX_SILU) of(std::integral_constant<int, SPARQ_MX_SILU>{});
         else of(std::integral_constant<int, SPARQ_MX_GELU>{});
     });
-    return launch_status();
+    return s;
 }

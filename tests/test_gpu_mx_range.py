@@ -108,3 +108,21 @@ def test_codec_of_more_rows_than_a_launch_has_wavefronts(sq, emptied):  # noqa: 
             y1 = torch.full_like(x[p], 9.0)
             sq.sparq_mx_dequantize(c1, s1, bits, y1)
             assert torch.equal(y[p], y1), (bits, r)
+
+
+def test_act_of_more_rows_than_a_launch_has_wavefronts(sq, emptied):  # noqa: F811
+    rows, K, piece = (1 << 26) + 5, 2, 1 << 25
+    g = torch.Generator(DEV).manual_seed(22)
+    gate, up, dy = (torch.randn(rows, K, device=DEV, dtype=torch.bfloat16, generator=g) for _ in range(3))
+    gc, uc = coded(sq, rows, K, 8), coded(sq, rows, K, 8)
+    y, dg, du = (torch.full_like(gate, 7.0) for _ in range(3))
+    sq.sparq_mx_act("silu", gate, y, up=up, gate_codes=gc[0], gate_scales=gc[1], up_codes=uc[0], up_scales=uc[1])
+    sq.sparq_mx_act_grad("silu", dy, *gc, dg, up_codes=uc[0], up_scales=uc[1], dup=du)
+    for r in range(0, rows, piece):
+        p = slice(r, min(rows, r + piece))
+        g1, u1 = coded(sq, p.stop - r, K, 8), coded(sq, p.stop - r, K, 8)
+        y1, dg1, du1 = (torch.full_like(gate[p], 9.0) for _ in range(3))
+        sq.sparq_mx_act("silu", gate[p], y1, up=up[p], gate_codes=g1[0], gate_scales=g1[1], up_codes=u1[0], up_scales=u1[1])
+        sq.sparq_mx_act_grad("silu", dy[p], *g1, dg1, up_codes=u1[0], up_scales=u1[1], dup=du1)
+        for a, b in zip((gc[0][p], gc[1][p], uc[0][p], uc[1][p], y[p], dg[p], du[p]), (*g1, *u1, y1, dg1, du1)):
+            assert torch.equal(a, b), r
