@@ -479,13 +479,15 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
     if (rows >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
     const NormParams p = {ldx, ldy, code_pitch(K, 8), scale_pitch(K), rows, K, (int)round_up(K, kCodeUnit), eps, (float)(1.0 / K)};
     const hipStream_t s = static_cast<hipStream_t>(stream);
+    sparq_status done = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const auto launch = [&](auto kernel, int per_block, int per_cu) {
-            const int64_t blocks = (rows + per_block - 1) / per_block, places = per_cu ? (int64_t)per_cu * device_cu_count() : blocks;
+            const int64_t blocks = (rows + per_block - 1) / per_block, places = (int64_t)per_cu * device_cu_count();
             kernel<<<(unsigned)(blocks < places ? blocks : places), kThreads, 0, s>>>(
                 static_cast<const T*>(x), gamma, beta, static_cast<T*>(y), mean, rstd, static_cast<uint8_t*>(codes),
                 static_cast<uint8_t*>(scales), p);
+            done = launch_status();
         };
         const auto held = [&](auto whole, auto streaming) {
             constexpr bool W = decltype(whole)::value;
@@ -496,13 +498,19 @@ extern "C" sparq_status sparq_mx_norm(const void* x, int64_t ldx, const float* g
             else if (K <= 4096) launch(norm_kernel<T, 4, 2, W, S>, 1, 5);
             else launch(norm_kernel<T, 4, 4, W, S>, 1, 3);
         };
-        if (!held_in_registers(K)) launch(norm_long_kernel<T>, 1, 0);
-        else if (K % 8 == 0) {
+        if (!held_in_registers(K)) {
+            done = in_launches(rows, kThreads, [&](int64_t first, int64_t n) {
+                norm_long_kernel<T><<<(unsigned)n, kThreads, 0, s>>>(static_cast<const T*>(x) + first * ldx, gamma, beta, static_cast<T*>(y) + first * ldy,
+                                                                     mean ? mean + first : nullptr, rstd ? rstd + first : nullptr,
+                                                                     row_of(codes, first, p.code_pitch), row_of(scales, first, p.scale_pitch), p);
+                return launch_status();
+            });
+        } else if (K % 8 == 0) {
             const int64_t result = rows * K * (int64_t)sizeof(T);
             with_streaming<T>(2 * result + (codes ? rows * K : 0), result, [&](auto streaming) { held(std::true_type{}, streaming); });
         } else held(std::false_type{}, std::integral_constant<int, kKept>{});
     });
-    return launch_status();
+    return done;
 }
 
 extern "C" size_t sparq_mx_norm_grad_workspace_bytes(int64_t rows, int32_t K) {

@@ -126,3 +126,18 @@ def test_act_of_more_rows_than_a_launch_has_wavefronts(sq, emptied):  # noqa: F8
         sq.sparq_mx_act_grad("silu", dy[p], *g1, dg1, up_codes=u1[0], up_scales=u1[1], dup=du1)
         for a, b in zip((gc[0][p], gc[1][p], uc[0][p], uc[1][p], y[p], dg[p], du[p]), (*g1, *u1, y1, dg1, du1)):
             assert torch.equal(a, b), r
+
+
+def test_norm_of_more_short_rows_than_a_launch_has_workgroups(sq, emptied):  # noqa: F811
+    rows, K, piece = (1 << 24) + 9, 5, 1 << 23
+    g = torch.Generator(DEV).manual_seed(23)
+    x = torch.randn(rows, K, device=DEV, dtype=torch.float16, generator=g)
+    gamma, beta = torch.rand(K, device=DEV, generator=g) + 0.5, torch.rand(K, device=DEV, generator=g)
+    c, y, mean, rstd = coded(sq, rows, K, 8), torch.full_like(x, 7.0), torch.zeros(rows, device=DEV), torch.zeros(rows, device=DEV)
+    sq.sparq_mx_norm(x, gamma, beta, 1e-5, y, mean=mean, rstd=rstd, codes=c[0], scales=c[1])
+    for r in range(0, rows, piece):
+        p = slice(r, min(rows, r + piece))
+        c1, y1, m1, r1 = coded(sq, p.stop - r, K, 8), torch.full_like(x[p], 9.0), torch.ones(p.stop - r, device=DEV), torch.ones(p.stop - r, device=DEV)
+        sq.sparq_mx_norm(x[p], gamma, beta, 1e-5, y1, mean=m1, rstd=r1, codes=c1[0], scales=c1[1])
+        for a, b in zip((c[0][p], c[1][p], y[p], mean[p], rstd[p]), (*c1, y1, m1, r1)):
+            assert torch.equal(a, b), r
