@@ -537,6 +537,7 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
     float* partial = gradients && !beside ? reinterpret_cast<float*>(static_cast<char*>(workspace) + (held_in_registers(K) ? 0 : round_up(rows * 8, 256))) : nullptr;
     const NormGradParams p = {lddy, lddx, code_pitch(K, 8), scale_pitch(K), rows, K, (float)(1.0 / K), norm_parts(rows, K)};
     const uint8_t *c = static_cast<const uint8_t*>(codes), *sc = static_cast<const uint8_t*>(scales);
+    sparq_status done = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
         const T* from = static_cast<const T*>(dy);
@@ -559,11 +560,19 @@ extern "C" sparq_status sparq_mx_norm_grad(const void* dy, int64_t lddy, const v
             if (K % 8 == 0) with_streaming<T>(2 * result + rows * K, result, [&](auto streaming) { held(std::true_type{}, streaming); });
             else held(std::false_type{}, std::integral_constant<int, kKept>{});
         } else {
-            norm_grad_rows_kernel<T><<<(unsigned)((rows + kWaves - 1) / kWaves), kThreads, 0, s>>>(from, c, sc, mean, rstd, gamma, sums, p);
+            done = in_launches(rows, 64, [&](int64_t first, int64_t n) {
+                NormGradParams q = p;
+                q.rows = n;
+                norm_grad_rows_kernel<T><<<(unsigned)((n + kWaves - 1) / kWaves), kThreads, 0, s>>>(
+                    from + first * lddy, row_of(c, first, p.code_pitch), row_of(sc, first, p.scale_pitch), mean + first, rstd + first, gamma, sums + first, q);
+                return launch_status();
+            });
+            if (done != SPARQ_OK) return;
             norm_grad_columns_kernel<T><<<dim3((unsigned)((K + 8ll * kThreads - 1) / (8 * kThreads)), p.parts), kThreads, 0, s>>>(
                 from, c, sc, mean, rstd, gamma, sums, to, partial, p);
         }
     });
+    if (done != SPARQ_OK) return done;
     if (partial) return launch_join_columns(partial, dgamma, dbeta, K, 2 * K, p.parts, s);
     return launch_status();
 }

@@ -141,3 +141,29 @@ def test_norm_of_more_short_rows_than_a_launch_has_workgroups(sq, emptied):  # n
         sq.sparq_mx_norm(x[p], gamma, beta, 1e-5, y1, mean=m1, rstd=r1, codes=c1[0], scales=c1[1])
         for a, b in zip((c[0][p], c[1][p], y[p], mean[p], rstd[p]), (*c1, y1, m1, r1)):
             assert torch.equal(a, b), r
+
+
+def test_norm_gradient_of_more_short_rows_than_a_launch_has_wavefronts(sq, emptied):  # noqa: F811
+    rows, K, piece = (1 << 26) + 7, 3, 1 << 25
+    g = torch.Generator(DEV).manual_seed(24)
+    x, dy = (torch.randn(rows, K, device=DEV, dtype=torch.bfloat16, generator=g) for _ in range(2))
+    gamma = torch.rand(K, device=DEV, generator=g) + 0.5
+    c, dx = coded(sq, rows, K, 8), torch.full_like(x, 7.0)
+    mean, rstd = torch.randn(rows, device=DEV, generator=g), torch.rand(rows, device=DEV, generator=g) + 0.5
+    for r in range(0, rows, piece):
+        p = slice(r, min(rows, r + piece))
+        sq.sparq_mx_quantize(x[p], codes8=c[0][p], scales8=c[1][p])
+    dgamma, dbeta = torch.zeros(K, device=DEV), torch.zeros(K, device=DEV)
+    ws = torch.empty(sq.sparq_mx_norm_grad_workspace_bytes(rows, K), dtype=torch.uint8, device=DEV)
+    sq.sparq_mx_norm_grad(dy, *c, mean, rstd, gamma, dx, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+    h = torch.empty_like(x, dtype=torch.float32)
+    for r in range(0, rows, piece):
+        p = slice(r, min(rows, r + piece))
+        dx1, one, two = torch.full_like(x[p], 9.0), torch.zeros(K, device=DEV), torch.zeros(K, device=DEV)
+        sq.sparq_mx_norm_grad(dy[p], c[0][p], c[1][p], mean[p], rstd[p], gamma, dx1, dgamma=one, dbeta=two, workspace=ws)
+        assert torch.equal(dx[p], dx1), r
+        sq.sparq_mx_dequantize(c[0][p], c[1][p], 8, h[p])
+    # 256 sums of rows / 256 terms, and their sum: (rows / 256 + 256 + 8) u of the terms' magnitudes
+    h.sub_(mean[:, None]).mul_(rstd[:, None])
+    for got, terms in ((dgamma, h.double() * dy.double()), (dbeta, dy.double())):
+        assert bool(((got.double() - terms.sum(0)).abs() <= (rows / 256 + 264) * u * terms.abs().sum(0)).all())
