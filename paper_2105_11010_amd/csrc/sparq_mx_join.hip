@@ -47,12 +47,12 @@ sparq_status launch_join(const float* partial, const float* bias, void* out, int
     return launch_status();
 }
 
-// Sums over rows, few columns of many parts: 32 columns a workgroup, every 32nd part a thread, joined in LDS.
+// Sums over rows, few columns of many parts: 32 columns a workgroup (from column `from` on), every 32nd part a thread, joined in LDS.
 constexpr int kJoinThreads = 1024;
 __global__ __launch_bounds__(kJoinThreads) void join_columns_kernel(const float* __restrict__ partial, float* __restrict__ first,
-                                                                    float* __restrict__ second, int split, int columns, int parts) {
+                                                                    float* __restrict__ second, int split, int columns, int parts, int from) {
     __shared__ float shared[32][33];
-    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = blockIdx.x * 32 + x;
+    const int x = threadIdx.x & 31, y = threadIdx.x >> 5, c = from + blockIdx.x * 32 + x;
     float s = 0.0f;
     if (c < columns) {
 #pragma unroll 4
@@ -67,8 +67,10 @@ __global__ __launch_bounds__(kJoinThreads) void join_columns_kernel(const float*
     if (out) out[c < split ? c : c - split] = s;
 }
 sparq_status launch_join_columns(const float* partial, float* first, float* second, int split, int columns, int parts, hipStream_t stream) {
-    join_columns_kernel<<<(unsigned)((columns + 31ll) / 32), kJoinThreads, 0, stream>>>(partial, first, second, split, columns, parts);
-    return launch_status();
+    return in_launches((columns + 31ll) / 32, kJoinThreads, [&](int64_t at, int64_t n) {
+        join_columns_kernel<<<(unsigned)n, kJoinThreads, 0, stream>>>(partial, first, second, split, columns, parts, (int)(32 * at));
+        return launch_status();
+    });
 }
 
 }  // namespace mx

@@ -167,3 +167,21 @@ def test_norm_gradient_of_more_short_rows_than_a_launch_has_wavefronts(sq, empti
     h.sub_(mean[:, None]).mul_(rstd[:, None])
     for got, terms in ((dgamma, h.double() * dy.double()), (dbeta, dy.double())):
         assert bool(((got.double() - terms.sum(0)).abs() <= (rows / 256 + 264) * u * terms.abs().sum(0)).all())
+
+
+def test_norm_gradient_of_a_row_of_more_columns_than_a_launch_joins(sq, emptied):  # noqa: F811
+    """One row: dbeta is dy, dgamma dy h."""
+    K = (1 << 26) + 40
+    g = torch.Generator(DEV).manual_seed(25)
+    x, dy = (torch.randn(1, K, device=DEV, dtype=torch.bfloat16, generator=g) for _ in range(2))
+    c, gamma, y, dx = coded(sq, 1, K, 8), torch.ones(K, device=DEV), torch.empty_like(x), torch.empty_like(x)
+    mean, rstd = torch.empty(1, device=DEV), torch.empty(1, device=DEV)
+    sq.sparq_mx_norm(x, gamma, None, 1e-5, y, mean=mean, rstd=rstd, codes=c[0], scales=c[1])
+    dgamma, dbeta, X = torch.full((K,), 9.0, device=DEV), torch.full((K,), 9.0, device=DEV), torch.empty(1, K, device=DEV)
+    ws = torch.empty(sq.sparq_mx_norm_grad_workspace_bytes(1, K), dtype=torch.uint8, device=DEV)
+    sq.sparq_mx_norm_grad(dy, *c, mean, rstd, gamma, dx, dgamma=dgamma, dbeta=dbeta, workspace=ws)
+    assert torch.equal(dbeta, dy[0].float())
+    sq.sparq_mx_dequantize(*c, 8, X)
+    ref = (X.double() - mean.double()) * rstd.double() * dy.double()
+    off = 4 * u * (X.double().abs() + mean.double().abs()) * rstd.double() * dy.double().abs()
+    assert bool(((dgamma.double() - ref[0]).abs() <= off[0]).all())
