@@ -185,3 +185,25 @@ def test_norm_gradient_of_a_row_of_more_columns_than_a_launch_joins(sq, emptied)
     ref = (X.double() - mean.double()) * rstd.double() * dy.double()
     off = 4 * u * (X.double().abs() + mean.double().abs()) * rstd.double() * dy.double().abs()
     assert bool(((dgamma.double() - ref[0]).abs() <= off[0]).all())
+
+
+def test_few_rows_of_a_product_with_more_columns_than_a_launch_counts(sq, emptied):  # noqa: F811
+    M, N, K, piece = 1, 1 << 28, 64, 1 << 27
+    g = torch.Generator(DEV).manual_seed(26)
+    w, ws = torch.empty(N, sq.sparq_mx_code_bytes(K, 4), dtype=torch.uint8, device=DEV), torch.zeros(N, sq.sparq_mx_scale_bytes(K), dtype=torch.uint8, device=DEV)
+    w.random_(0, 256, generator=g)
+    w[:, K // 2:] = 0
+    ws[:, :2] = 127
+    bias = torch.randn(N, device=DEV, generator=g)
+    x = torch.randn(M, K, device=DEV, dtype=torch.bfloat16, generator=g)
+    x4 = coded(sq, M, K, 4)
+    sq.sparq_mx_quantize(x, *x4)
+    for product, first, rest in ((sq.sparq_mx_gemm, x4, (K,)), (sq.sparq_mx_linear, (x,), ())):
+        scratch = torch.empty(max(sq.sparq_mx_gemm_workspace_bytes(M, N, K), sq.sparq_mx_linear_workspace_bytes(M, N, K)) + 1, dtype=torch.uint8, device=DEV)
+        y = torch.full((M, N), 7.0, dtype=torch.bfloat16, device=DEV)
+        product(*first, w, ws, *rest, y, bias=bias, workspace=scratch)
+        for n in range(0, N, piece):
+            p = slice(n, n + piece)
+            y1 = torch.full((M, piece), 9.0, dtype=torch.bfloat16, device=DEV)
+            product(*first, w[p], ws[p], *rest, y1, bias=bias[p], workspace=scratch)
+            assert torch.equal(y[:, p], y1), n
