@@ -4,14 +4,14 @@
 namespace sparq {
 namespace mx {
 
-// Sums of dy's columns, a grid row a slab of its rows, for gradients as large as to keep memory busy on their own.
+// Sums of dy's columns from `first` on, a grid row a slab of its rows, for gradients as large as to keep memory busy on their own.
 constexpr int kSumThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const GradParams p) {
+__global__ __launch_bounds__(kSumThreads) void column_sum_kernel(const GradParams p, int first) {
     typedef ColumnSums<T, kSumThreads> Sums;
     __shared__ float shared[Sums::kFloats];
     const int64_t begin = blockIdx.y * p.slab, end = begin + p.slab < p.R ? begin + p.slab : p.R;
-    Sums::run(static_cast<const T*>(p.dy), p.lddy, begin, end, (int)p.J, blockIdx.x * Sums::kColumns, p.column_sums + blockIdx.y * p.J, shared);
+    Sums::run(static_cast<const T*>(p.dy), p.lddy, begin, end, (int)p.J, first + blockIdx.x * Sums::kColumns, p.column_sums + blockIdx.y * p.J, shared);
 }
 
 // ---- plan ----------------------------------------------------------------------------
@@ -84,9 +84,11 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     // last longer than it (us with either, in the launch -> in one before: 515 x 771 x 577 8.4 -> 13.4, 2048^3 36.9 -> 40.8, 4096 x 512 x 512
     // 16.8 -> 20.3; 8192 x 1024 x 1024 45.6 -> 42.5, 4096^3 150 -> 141, 8192 x 4096 x 4096 283 -> 272).
     if (column_sums && J * R > 1 << 22) {
-        with_type(dy_type, [&](auto t) { column_sum_kernel<decltype(t)><<<dim3((unsigned)((J + 63) / 64), p.slabs), kSumThreads, 0, stream>>>(p); });
+        const sparq_status s = in_launches((J + 63) / 64, kSumThreads, [&](int64_t first, int64_t n) {
+            with_type(dy_type, [&](auto t) { column_sum_kernel<decltype(t)><<<dim3((unsigned)n, p.slabs), kSumThreads, 0, stream>>>(p, (int)(64 * first)); });
+            return launch_status();
+        });
         p.slabs = 0;
-        const sparq_status s = launch_status();
         if (s != SPARQ_OK) return s;
     }
     p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);

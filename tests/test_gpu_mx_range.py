@@ -207,3 +207,18 @@ def test_few_rows_of_a_product_with_more_columns_than_a_launch_counts(sq, emptie
             y1 = torch.full((M, piece), 9.0, dtype=torch.bfloat16, device=DEV)
             product(*first, w[p], ws[p], *rest, y1, bias=bias[p], workspace=scratch)
             assert torch.equal(y[:, p], y1), n
+
+
+def test_gradient_of_the_bias_of_as_many_outputs_as_there_may_be(sq, emptied):  # noqa: F811
+    M, N, K = 3, 1 << 28, 1
+    g = torch.Generator(DEV).manual_seed(27)
+    x, dy = torch.randn(M, K, device=DEV, generator=g), torch.randn(M, N, device=DEV, dtype=torch.bfloat16, generator=g)
+    c = coded(sq, M, K, 8)
+    sq.sparq_mx_quantize(x, codes8=c[0], scales8=c[1])
+    X = torch.empty(M, K, device=DEV)
+    sq.sparq_mx_dequantize(*c, 8, X)
+    dw, db = torch.full((N, K), 9.0, device=DEV), torch.full((N,), 9.0, device=DEV)
+    ws = torch.empty(sq.sparq_mx_linear_dw_workspace_bytes(M, N, K), dtype=torch.uint8, device=DEV)
+    sq.sparq_mx_linear_dw(dy, *c, dw, db=db, workspace=ws)
+    assert bool(((db.double() - dy.double().sum(0)).abs() <= 4 * u * dy.double().abs().sum(0)).all())
+    assert bool(((dw[:, 0].double() - (dy.double() * X.double()).sum(0)).abs() <= 10 * u * (dy.double() * X.double()).abs().sum(0)).all())
