@@ -26,8 +26,8 @@
  *   - workspace: 256-byte aligned, at least the bytes its query names (NULL when that is 0), overwritten by the call;
  *     calls that share one must not overlap.
  *   - Results do not depend on timing: every sum is made in a fixed order.
- *   - K and N lie in [1, 2^28]; rows and M may be 0.  More rows than a launch counts (2^31 / the row's units of 512,
- *     and 2^31 tiles of results) return SPARQ_EUNSUPPORTED.
+ *   - K and N lie in [1, 2^28]; rows and M may be 0.  More rows than a call counts (2^31 / the row's units of 512; of
+ *     the product's results 2^31 tiles, of weights' gradients 2^24, 64 x 64 or larger) return SPARQ_EUNSUPPORTED.
  *   - No rows: nothing is written, except gradients summed over the rows, which are zeros then.
  */
 #ifndef SPARQ_MX_H

@@ -93,14 +93,31 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     }
     p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);
     const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
-    if (tiles_j * tiles_k + p.slabs * J >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
-    p.tiles_j = (int)tiles_j;
     p.tiles_k = (int)tiles_k;
     p.steps_per_part = (int)((steps + plan.parts - 1) / plan.parts);
     const bool parted = plan.parts > 1;
     p.ldo = parted ? K : ldo;
     p.part_stride = parted ? J * K : 0;
-    const sparq_status s = launch_grad(p, plan.parts, t, dy_type, bits == 8, parted ? workspace : out, parted ? SPARQ_MX_F32 : out_type, stream);
+    void* const to = parted ? workspace : out;
+    const int to_type = parted ? SPARQ_MX_F32 : out_type;
+    sparq_status s;
+    if (bits == 8) {
+        // (dw's rows and columns are at most 2^28: more tiles than one launch takes would be results of half a terabyte)
+        constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
+        if ((tiles_j * tiles_k + p.slabs * ((J + kColumns - 1) / kColumns)) * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
+        p.tiles_j = (int)tiles_j;
+        s = launch_grad(p, plan.parts, t, dy_type, true, to, to_type, stream);
+    } else {
+        // (more than one launch: no parts)
+        s = in_launches(tiles_j, tiles_k * kGradThreads, [&](int64_t first, int64_t n) {
+            GradParams q = p;                                // of the rows from here on
+            const int64_t row = first * t;
+            q.dy = static_cast<const char*>(dy) + row * lddy * (int64_t)type_bytes(dy_type);
+            q.J -= row;
+            q.tiles_j = (int)n;
+            return launch_grad(q, plan.parts, t, dy_type, false, static_cast<char*>(to) + row * p.ldo * (int64_t)type_bytes(to_type), to_type, stream);
+        });
+    }
     if (s != SPARQ_OK || !parted) return s;
     return launch_join(static_cast<const float*>(workspace), nullptr, out, out_type, J, K, ldo, plan.parts, stream);
 }

@@ -222,3 +222,15 @@ def test_gradient_of_the_bias_of_as_many_outputs_as_there_may_be(sq, emptied):  
     sq.sparq_mx_linear_dw(dy, *c, dw, db=db, workspace=ws)
     assert bool(((db.double() - dy.double().sum(0)).abs() <= 4 * u * dy.double().abs().sum(0)).all())
     assert bool(((dw[:, 0].double() - (dy.double() * X.double()).sum(0)).abs() <= 10 * u * (dy.double() * X.double()).abs().sum(0)).all())
+
+
+def test_product_gradient_of_more_rows_than_a_launch_has_tiles(sq, emptied):  # noqa: F811
+    """dx of one output is dy w: one product, rounded once."""
+    M = (1 << 31) + 200
+    dy = torch.empty(M, 1, dtype=torch.bfloat16, device=DEV).normal_(generator=torch.Generator(DEV).manual_seed(28))
+    w4 = coded(sq, 1, 1, 4)
+    sq.sparq_mx_quantize(torch.full((1, 1), 0.375, device=DEV), *w4)
+    dx = torch.full_like(dy, 7.0)
+    ws = torch.empty(sq.sparq_mx_linear_dx_workspace_bytes(M, 1, 1), dtype=torch.uint8, device=DEV)
+    sq.sparq_mx_linear_dx(dy, *w4, dx, workspace=ws)
+    assert torch.equal(dx, dy.mul_(0.375))
