@@ -66,6 +66,10 @@ static int64_t whole_steps(int64_t lddy, int64_t J, int64_t R, int64_t pitch, bo
 static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* codes, const void* scales, int bits, void* out, int out_type,
                          int64_t ldo, float* column_sums, int64_t J, int64_t R, int K, const GradPlan& plan, void* workspace, hipStream_t stream) {
     const int t = plan.tile;
+    const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t;
+    // (dw's rows and columns are at most 2^28: more tiles than one launch takes would be results of half a terabyte)
+    constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
+    if (bits == 8 && (tiles_j * tiles_k + (column_sums ? plan.slabs : 0) * ((J + kColumns - 1) / kColumns)) * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
     GradParams p = {};
     p.dy = dy;
     p.codes = static_cast<const uint8_t*>(codes);
@@ -92,7 +96,7 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
         if (s != SPARQ_OK) return s;
     }
     p.s_whole = whole_steps(lddy, J, R, p.code_pitch, bits == 8);
-    const int64_t tiles_j = (J + t - 1) / t, tiles_k = (K + t - 1) / t, steps = (R + kGradStep - 1) / kGradStep;
+    const int64_t steps = (R + kGradStep - 1) / kGradStep;
     p.tiles_k = (int)tiles_k;
     p.steps_per_part = (int)((steps + plan.parts - 1) / plan.parts);
     const bool parted = plan.parts > 1;
@@ -102,9 +106,6 @@ static sparq_status grad(const void* dy, int dy_type, int64_t lddy, const void* 
     const int to_type = parted ? SPARQ_MX_F32 : out_type;
     sparq_status s;
     if (bits == 8) {
-        // (dw's rows and columns are at most 2^28: more tiles than one launch takes would be results of half a terabyte)
-        constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
-        if ((tiles_j * tiles_k + p.slabs * ((J + kColumns - 1) / kColumns)) * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
         p.tiles_j = (int)tiles_j;
         s = launch_grad(p, plan.parts, t, dy_type, true, to, to_type, stream);
     } else {

@@ -17,3 +17,8 @@ MUCH = SZ(1 << 62)
 def test_more_tiles_of_weights_gradients_than_a_launch_counts():
     N, K = 1 << 24, 1 << 20
     assert sq.lib.sparq_mx_linear_dw(A, BF16, I64(N), A, A, A, BF16, I64(K), None, I64(512), N, K, A, MUCH, None) == EUNSUPPORTED
+
+
+def test_weights_gradients_are_refused_before_the_bias_is_begun():
+    N, K = 1 << 24, 1 << 20
+    assert sq.lib.sparq_mx_linear_dw(A, BF16, I64(N), A, A, A, BF16, I64(K), A, I64(512), N, K, A, MUCH, None) == EUNSUPPORTED
