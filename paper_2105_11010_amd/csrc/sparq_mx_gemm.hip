@@ -29,6 +29,12 @@ static GemmPlan gemm_plan(int64_t M, int N, int K) {
     return p;
 }
 
+// As many tiles, with their parts, as the kernel counts
+static bool countable(const GemmPlan& p, int64_t M, int64_t N) {
+    const int t = p.tile;
+    return t == 0 || (M + t - 1) / t * ((N + t - 1) / t) * p.parts < (1ll << 31);
+}
+
 template <class O, int TILE>
 static sparq_status launch_tile(const GemmParams& p, void* y, hipStream_t stream) {
     const auto kernel = gemm_kernel<O, TILE, TILE>;
@@ -56,7 +62,6 @@ static sparq_status gemm(const void* a, const void* as, const void* w, const voi
         return launch_few_rows(f, 0, y, type, stream);
     }
     const int64_t tiles_m = (M + t - 1) / t, tiles_n = (N + t - 1) / t;
-    if (tiles_m > INT32_MAX || tiles_m * tiles_n > INT32_MAX) return SPARQ_EUNSUPPORTED;
     const bool parted = plan.parts > 1;
     GemmParams p = {};
     p.a = static_cast<const uint8_t*>(a);
@@ -75,7 +80,6 @@ static sparq_status gemm(const void* a, const void* as, const void* w, const voi
     p.steps = (int)round_up((K + kCodeUnit - 1) / kCodeUnit, 4);
     p.steps_per_part = (int)round_up((p.steps + plan.parts - 1) / plan.parts, 4);
     const int parts = (p.steps + p.steps_per_part - 1) / p.steps_per_part;       // (as the plan has it, or fewer)
-    if (tiles_m * tiles_n * parts >= (1ll << 31)) return SPARQ_EUNSUPPORTED;
     p.items = (uint32_t)(tiles_m * tiles_n * parts);
     sparq_status s = SPARQ_OK;
     with_type(parted ? SPARQ_MX_F32 : type, [&](auto o) {
@@ -109,6 +113,7 @@ extern "C" sparq_status sparq_mx_gemm(const void* a_codes, const void* a_scales,
     const GemmPlan plan = gemm_plan(M, N, K);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
+    if (!countable(plan, M, N)) return SPARQ_EUNSUPPORTED;
     return gemm(a_codes, a_scales, w_codes, w_scales, bias, y, type, ldy, M, N, K, plan, workspace, static_cast<hipStream_t>(stream));
 }
 
@@ -143,6 +148,7 @@ extern "C" sparq_status sparq_mx_linear(const void* x, int32_t x_type, int64_t l
     const size_t coded = coded_bytes(M, N, K);
     if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
     if (workspace_bytes < coded + plan.bytes) return SPARQ_EWORKSPACE;
+    if (!countable(plan, M, N)) return SPARQ_EUNSUPPORTED;
     uint8_t *codes = static_cast<uint8_t*>(workspace), *scales = codes + round_up(M * code_pitch(K, 4), 256);
     const sparq_status q = launch_quantize(x, x_type, ldx, M, K, codes, scales, nullptr, nullptr, s);
     if (q != SPARQ_OK) return q;
