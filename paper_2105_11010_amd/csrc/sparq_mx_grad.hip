@@ -58,7 +58,7 @@ static size_t grad_bytes(int64_t J, int64_t R, int K, bool dw) {
 // Steps that are read without checks, in runs of eight: none if rows' distances do not fit the loads' 32-bit offsets.  A run that dw's last
 // column cuts reads on into the next rows (one, unless rows are shorter than a run): the last rows, which it would leave, are not among them.
 static int64_t whole_steps(int64_t lddy, int64_t J, int64_t R, int64_t pitch, bool dw) {
-    if (lddy >= 1 << 21 || pitch >= 1 << 24 || R >= 1ll << 36) return 0;
+    if (R == 0 || lddy >= 1 << 21 || pitch >= 1 << 24 || R >= 1ll << 36) return 0;       // (of no rows lddy may be anything)
     const int64_t over = dw ? round_up(J, 8) - J : 0, rows = R - (over + lddy - 1) / lddy;
     return rows > 0 ? rows / kGradStep : 0;
 }

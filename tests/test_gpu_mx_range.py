@@ -2,6 +2,8 @@
 rows or columns than one launch takes.
 Against the plain reference in 64 bits (tests/mx_reference.py); tolerances stand at the tests, fixed before any run.
 u = 2^-24 is fp32's unit roundoff."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -234,3 +236,20 @@ def test_product_gradient_of_more_rows_than_a_launch_has_tiles(sq, emptied):  # 
     ws = torch.empty(sq.sparq_mx_linear_dx_workspace_bytes(M, 1, 1), dtype=torch.uint8, device=DEV)
     sq.sparq_mx_linear_dx(dy, *w4, dx, workspace=ws)
     assert torch.equal(dx, dy.mul_(0.375))
+
+
+# ---- no rows -----------------------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("N,K", [(8, 64), (5, 33), (300, 1000)])
+def test_no_rows_and_no_dy_give_gradients_of_zero(sq, N, K):  # noqa: F811
+    """Through the C entry points, dy NULL and its rows 0 apart."""
+    n, z, big = None, ctypes.c_int64(0), ctypes.c_size_t(1 << 40)
+    pointer = lambda t: ctypes.c_void_p(t.data_ptr())      # noqa: E731
+    stream = ctypes.c_void_p(torch.cuda.current_stream().cuda_stream)
+    for t in (0, 1, 2):
+        dw, db = Result(N, K, "f32", 3, 1), torch.full((N,), 9.0, device=DEV)
+        ws = torch.empty(sq.sparq_mx_linear_dw_workspace_bytes(0, N, K) + 256, dtype=torch.uint8, device=DEV)
+        assert sq.lib.sparq_mx_linear_dw(n, t, z, n, n, pointer(dw.view), 0, ctypes.c_int64(dw.view.stride(0)), pointer(db), z, N, K, pointer(ws), big, stream) == 0
+        assert not dw.get().any() and not db.any()
+    dgamma, dbeta = torch.full((K,), 9.0, device=DEV), torch.full((K,), 9.0, device=DEV)
+    assert sq.lib.sparq_mx_norm_grad(n, z, n, n, n, n, n, n, z, 2, pointer(dgamma), pointer(dbeta), z, K, n, ctypes.c_size_t(0), stream) == 0
+    assert not dgamma.any() and not dbeta.any()
