@@ -32,7 +32,8 @@ struct GradParams {
 constexpr int kGradThreads = 256;
 constexpr int kGradStep = 64;
 
-// The bf16 parts of a value: their sum is the value (8 significand bits a part; fp16 has 11, fp32 24).
+// The bf16 parts of a value: their sum is the value (8 significand bits a part; fp16 has 11, fp32 24).  Each is what is left cut off behind its
+// eighth bit, not rounded: fp32's values above bf16's largest would be rounded to infinity.
 template <class T> inline constexpr int kParts = sizeof(T) == 4 ? 3 : 2;
 template <> inline constexpr int kParts<__bf16> = 1;
 template <int P>
@@ -40,10 +41,9 @@ __device__ __forceinline__ void split(float v, float (&part)[P]) {
     part[0] = v;
 #pragma unroll
     for (int i = 1; i < P; ++i) {
-        const float rounded = (float)(__bf16)part[i - 1];
-        const float rest = part[i - 1] - rounded;
-        part[i - 1] = rounded;
-        part[i] = __builtin_fabsf(rounded) < __builtin_inff() ? rest : 0.0f;       // NaN, infinity: nothing to add
+        const float whole = part[i - 1], cut = __uint_as_float(__float_as_uint(whole) & 0xFFFF0000u);
+        part[i - 1] = cut;
+        part[i] = __builtin_fabsf(whole) == __builtin_inff() ? 0.0f : whole - cut;       // infinity: nothing to add
     }
 }
 __device__ __forceinline__ uint32_t pack_bf16(float a, float b) { return pack2(a, b, __bf16{}); }

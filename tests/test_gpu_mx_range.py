@@ -9,7 +9,7 @@ import pytest
 import torch
 
 import mx_reference as R
-from test_gpu_mx import DEV, TYPES, Result, close, coded_buffers, matrix, sq, u  # noqa: F401
+from test_gpu_mx import DEV, TYPES, Result, close, coded_buffers, matrix, rng, sq, stored, u, values, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -253,3 +253,22 @@ def test_no_rows_and_no_dy_give_gradients_of_zero(sq, N, K):  # noqa: F811
     dgamma, dbeta = torch.full((K,), 9.0, device=DEV), torch.full((K,), 9.0, device=DEV)
     assert sq.lib.sparq_mx_norm_grad(n, z, n, n, n, n, n, n, z, 2, pointer(dgamma), pointer(dbeta), z, K, n, ctypes.c_size_t(0), stream) == 0
     assert not dgamma.any() and not dbeta.any()
+
+# ---- the product's gradients -------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("M,N,K", [(5, 7, 40), (200, 130, 300)])
+def test_product_gradients_of_the_largest_values(sq, M, N, K):  # noqa: F811
+    """fp32 has values above bf16's largest: they enter whole as well, and weights of zero leave nothing of them."""
+    g = rng(30, M, N, K)
+    x, w, dy = values(g, M, K, "f32", 2.0 ** -9), values(g, N, K, "f32", 2.0 ** -9), values(g, M, N, "f32", 2.0 ** 100)
+    top = float(np.finfo(np.float32).max)
+    for i in range(min(M, N)):
+        dy[i, i] = (top, -top, float(np.float32(top * (1 - 2.0 ** -9))), 1.5 * 2.0 ** 127)[i % 4]
+    w[:, 0], x[:, 0] = 0.0, 0.0
+    X, W = R.quantised(x, 8), R.quantised(w, 4)
+    dx, dw = Result(M, K, "f32"), Result(N, K, "f32")
+    dyd = matrix(dy, "f32")
+    sq.sparq_mx_linear_dx(dyd, *stored(sq, w, 4), dx.view, workspace=workspace(sq.sparq_mx_linear_dx_workspace_bytes(M, N, K))[1])
+    sq.sparq_mx_linear_dw(dyd, *stored(sq, x, 8), dw.view, workspace=workspace(sq.sparq_mx_linear_dw_workspace_bytes(M, N, K))[1])
+    assert not dx.get()[:, 0].any() and not dw.get()[:, 0].any()
+    close(dx.get(), dy @ W, 2 * (3 * N + 2) * u * (np.abs(dy) @ np.abs(W)), "f32")
+    close(dw.get(), dy.T @ X, 2 * (3 * M + 2) * u * (np.abs(dy).T @ np.abs(X)), "f32")
