@@ -50,3 +50,42 @@ print(set(got))
 """
     r = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, cwd=ROOT)
     assert r.returncode == 0 and r.stdout.strip() == "{%d}" % ELAUNCH, (r.returncode, r.stdout, r.stderr)
+
+
+# One byte less than the query names, everything else valid: EWORKSPACE and nothing else; sizes whose plan takes a workspace.
+def _workspaces():
+    M, N, K = 300, 8, 64
+    yield "linear", (A, BF16, I64(K), A, A, None, A, BF16, I64(N), I64(M), N, K), (M, N, K)
+    yield "linear", (A, F32, I64(8300), A, A, A, A, F32, I64(100), I64(70), 100, 8300), (70, 100, 8300)
+    yield "gemm", (A, A, A, A, None, A, BF16, I64(100), I64(70), 100, 8300), (70, 100, 8300)
+    yield "linear_dx", (A, F32, I64(3008), A, A, A, F32, I64(49), I64(24), 3008, 49), (24, 3008, 49)
+    yield "linear_dw", (A, F32, I64(1234), A, A, A, F32, I64(114), A, I64(1757), 1234, 114), (1757, 1234, 114)
+    yield "norm_grad", (A, I64(64), A, A, A, A, A, A, I64(64), BF16, A, A, I64(3), 64), (3, 64)
+
+
+@pytest.mark.parametrize("name,args,sizes", list(_workspaces()), ids=lambda v: v if isinstance(v, str) else "x".join(map(str, v)) if isinstance(v[0], int) else "")
+def test_a_workspace_one_byte_short(name, args, sizes):
+    f, need = getattr(sq.lib, "sparq_mx_" + name), getattr(sq, "sparq_mx_%s_workspace_bytes" % name)(*sizes)
+    assert need > 0
+    for short in (0, need - 1):
+        assert f(*args, A, SZ(short), None) == EWORKSPACE
+    for bad in (None, P(0x10010)):
+        assert f(*args, bad, SZ(need), None) == EINVAL
+
+
+# The argument lists that test_mx_abi.py varies are valid: with more rows than a call counts each is refused for that alone.
+MANY = I64(1 << 31)
+
+
+@pytest.mark.parametrize("name,args", [
+    ("quantize", (A, BF16, I64(64), MANY, 64, A, A, None, None, None)),
+    ("quantize", (A, BF16, I64(64), MANY, 64, A, A, A, A, None)),
+    ("dequantize", (A, A, 8, A, F32, I64(64), MANY, 64, None)),
+    ("act", (0, A, I64(64), A, I64(64), A, I64(64), BF16, A, A, A, A, MANY, 64, None)),
+    ("act_grad", (1, A, I64(64), A, A, A, A, A, I64(64), A, I64(64), BF16, MANY, 64, None)),
+    ("norm", (A, I64(64), A, None, ctypes.c_float(1e-5), A, I64(64), BF16, A, A, A, A, MANY, 64, None)),
+    ("norm_grad", (A, I64(64), A, A, A, A, A, A, I64(64), BF16, A, A, MANY, 64, A, MUCH, None)),
+    ("linear", (A, BF16, I64(64), A, A, None, A, BF16, I64(8), MANY, 8, 64, A, MUCH, None)),
+], ids=lambda v: v if isinstance(v, str) else "")
+def test_valid_but_for_the_number_of_rows(name, args):
+    assert getattr(sq.lib, "sparq_mx_" + name)(*args) == EUNSUPPORTED
