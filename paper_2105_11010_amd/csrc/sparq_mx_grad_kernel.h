@@ -20,7 +20,7 @@ struct GradParams {
     int64_t lddy, code_pitch, scale_pitch, ldo;
     int64_t J, R;                        // results [J][K], sums of R products
     int64_t part_stride;                 // results of a part of the reduction lie this far apart (parts > 1)
-    int32_t K, K128, blocks;             // row length, the same in whole units of codes, bytes of a row of scales
+    int32_t K, K128;                     // row length, the same in whole units of codes
     int32_t tiles_j, tiles_k;
     int32_t steps_per_part;              // steps of 64 products
     float* column_sums;                  // [slabs][J], of dy [R][J] (dw), by workgroups past the tiles', or by a launch before
