@@ -72,7 +72,8 @@ sparq_status sparq_mx_linear(const void *x, int32_t x_type, int64_t ldx, const v
  *   dx[m][k] = sum_n dy[m][n] W[n][k]      over the 4-bit weights,
  *   dw[n][k] = sum_m dy[m][n] X[m][k]      over the 8-bit checkpoint X of the layer's input,
  *   db[n]    = sum_m dy[m][n]              (fp32; NULL: not wanted).
- * dy enters whole: bf16 as it is, fp16 and fp32 as the sum of two and three bf16 parts. */
+ * dy enters whole: bf16 as it is, fp16 and fp32 as the sum of two and three bf16 parts (of fp32, what lies below 2^-133
+ * is left out). */
 size_t sparq_mx_linear_dx_workspace_bytes(int64_t M, int32_t N, int32_t K);
 sparq_status sparq_mx_linear_dx(const void *dy, int32_t dy_type, int64_t lddy, const void *w_codes, const void *w_scales,
                                 void *dx, int32_t dx_type, int64_t lddx, int64_t M, int32_t N, int32_t K,
@@ -83,6 +84,7 @@ sparq_status sparq_mx_linear_dw(const void *dy, int32_t dy_type, int64_t lddy, c
                                 void *workspace, size_t workspace_bytes, void *stream);
 
 /* y = f(gate) * up over [rows][K], f(v) = v / (1 + exp(-v)) or v (1 + erf(v / sqrt 2)) / 2; up may be NULL (y = f(gate)).
+ * Values of f below 2^-119 in magnitude may come as zero (fp32 does not hold what is between).
  * Where codes are given, the 8-bit checkpoints of gate and up are written as well (a pair of NULLs: not wanted). */
 sparq_status sparq_mx_act(int32_t function, const void *gate, int64_t ldg, const void *up, int64_t ldu,
                           void *y, int64_t ldy, int32_t type, void *gate_codes, void *gate_scales,

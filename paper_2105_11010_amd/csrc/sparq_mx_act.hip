@@ -56,7 +56,7 @@ __device__ __forceinline__ void function_and_slope(float v, float& value, float&
 }
 
 // A wavefront takes 512 values of a row, a lane eight, as the quantiser does.  8192 x 8192 bf16, gated, with both checkpoints: silu 83 us
-// (6.5 TB/s), bound by memory, as is its gradient (83); gelu 93-95 and 87-89, bound by its arithmetic; fp32 silu 163 and 170.
+// (6.5 TB/s), bound by memory, as is its gradient (83); gelu 93-95 and 87-89, bound by its arithmetic; fp32 silu 163 and 170, gelu 164 and 179.
 template <class T, int F, bool UP, bool KEEP, int STREAMING>
 __global__ __launch_bounds__(kThreads) void act_kernel(const T* __restrict__ gate, const T* __restrict__ up, T* __restrict__ y,
                                                        uint8_t* __restrict__ gate_codes, uint8_t* __restrict__ gate_scales,

@@ -1,11 +1,14 @@
 // The product of 4-bit operands for few rows: a decoding step, a serving batch.  y[m][n] = sum_k W[n][k] A[m][k] on
 // v_mfma_scale_f32_16x16x128_f8f6f4, the weights the first operand: a lane feeds 32 values of one row, its block, and ends with four
 // neighbouring n of one m.  Bound by the weights' way from memory.
-// A workgroup makes 16 columns of y; its wavefronts divide the reduction in groups of 512 values (a row's 16 bytes of scales), the next
-// group on its way while this one is multiplied, and their sums are joined in LDS in the wavefronts' order.
-// X not void: A is quantised on the way, by each wavefront for the groups it multiplies, while the weights come.
+// A workgroup makes 16 columns of y; its wavefronts divide the reduction in groups of 512 values (a row's 16 bytes of scales), and their sums
+// are joined in LDS in the wavefronts' order.
+// X not void: A is quantised on the way, by each wavefront for the groups it multiplies, and the next group's weights are asked for behind
+// that; a further group waits for them and then for its part of A.
+// A in codes: the loads are written a group ahead, but the compiler moves them behind the group before, and those of three times 16 rows
+// among the matrix instructions, ten trips to memory a group.  What the loads' order could still give is in that.
 // A call for 1 x 4096 x 4096 takes 3.9 us, of which a launch's 3 us and the wait for one round trip to memory are the most: 8.9 MB would pass in
-// 1.3.  1 x 8192 x 8192 (36 MB of weights) takes 9.4, 3.8 TB/s; codes for 32 x 4096 x 4096 5.6.
+// 1.3.  1 x 8192 x 8192 (36 MB of weights) takes 9.4, 3.8 TB/s, with A in codes 7.8; codes for 32 x 4096 x 4096 5.5.
 #pragma once
 #include <type_traits>
 

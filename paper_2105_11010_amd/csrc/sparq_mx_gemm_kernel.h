@@ -6,9 +6,11 @@
 // one's -- into four buffers in turn; scales likewise, 16 bytes of a row (four steps) at a time, into two.  One barrier a step.
 // Steps come in fours: past a row's end the scales are zeros, 2^-127 each, and what codes add there is 2^-254 of something: nothing
 // in fp32.
-// 8192 x 8192 x 4096 takes 160 us (3.4 PF; 8192 x 4096 x 4096 86, 4096^3 47).  The matrix instructions alone would take 61 at the clock they reach
-// without data; with data the card's power sets the clock (1.8 GHz), and without the loads the kernel takes 122.  What is between is the caches'
-// requests, 64 bytes each, 0.69 of one a channel and cycle.  (Loads of 128 bytes, two steps at a time, halve those but leave one pair of steps ahead in
+// 8192 x 8192 x 4096 takes 160-180 us (3.1-3.4 PF; 8192 x 4096 x 4096 86, 4096^3 47).  The matrix instructions alone would take 61 at the clock they
+// reach without data; with data the card's power sets the clock (1.8 GHz), and without the loads the kernel takes 122.  What is between is the
+// caches' requests, 64 bytes each, 0.69 of one a channel and cycle, and the first steps of every 256 x 256 tile: 20 (fp32 results) or 26 registers, LDS
+// addresses most of them, lie in scratch memory there, the compiler makes a tile's first four steps a copy of their own that reads them back, and
+// each such read is waited for with all loads before it, seven times a tile (of 8192 x 8192 x 1024, 68 us, that is half of the steps).  (Loads of 128 bytes, two steps at a time, halve those but leave one pair of steps ahead in
 // LDS: 202 us where this took 179.)
 #pragma once
 #include <type_traits>

@@ -9,8 +9,11 @@
 // read by all.  (dy straight to LDS, without registers: the compiler then waits for these loads before every turning read, and dx of
 // 8192 x 4096 x 4096 took 392 us instead of 268, before the steps' order was laid out as it is.)
 // Bound by the matrix instructions and, with data as large as this, by the card's power: 8192 x 4096 x 4096 takes 206-248 us for dx and 237-256
-// for dw (1.07-1.33 PF; the same instructions without loads and writes 1.57 PF).  fp16 dy, two instructions a product, 728 and 722 us, fp32, three,
-// 916 and 940.  A small layer is bound by the steps' latency: 515 x 771 x 577 7.7 and 8.4 us in 64 x 64 tiles, 12 or 13 steps.
+// for dw (1.07-1.33 PF; the same instructions without loads and writes 1.57 PF).  fp16 dy, two instructions a product, 673-728 and 706-722 us, fp32, three,
+// 904-916 and 940.  Tiles of 128 and 64 ask for V at a step's end (a thread has one run of it) and need it where the next
+// begins: of 128 every step waits for all loads behind its barrier, which bf16 hides in part by a second workgroup on the CU and fp16 and fp32, whose LDS
+// leaves no room for one, do not; of 64 that wait is what a small layer's time is, 515 x 771 x 577 7.7 and 8.4 us of 12 or 13 steps.  dw in 256 x 256 keeps 105
+// scalar registers in lanes of vector ones, about 110 moves a step between its matrix instructions.
 #pragma once
 #include <type_traits>
 
