@@ -1,7 +1,7 @@
 """SPARQ trimmed convolution-as-GEMM on AMD MI355X (gfx950).
 
 Thin Python front end of ``libsparq.so`` (see ``include/sparq.h`` and, for the microscaled formats,
-``include/sparq_mx.h``): the names below are the C entry points, taking torch device tensors as plain buffers.
+``include/sparq_mx.h`` and ``include/sparq_mx_experts.h``): the names below are the C entry points, taking torch device tensors as plain buffers.
 """
 from .binding import (  # noqa: F401
     LIB_PATH, SparqConvDesc, SparqError, SparqMode, conv_desc, lib, mode, out_rows, strerror,
@@ -13,6 +13,10 @@ from .binding import (  # noqa: F401
     sparq_mx_act, sparq_mx_act_grad, sparq_mx_norm, sparq_mx_norm_grad, sparq_mx_code_bytes, sparq_mx_scale_bytes,
     sparq_mx_gemm_workspace_bytes, sparq_mx_linear_workspace_bytes, sparq_mx_linear_dx_workspace_bytes,
     sparq_mx_linear_dw_workspace_bytes, sparq_mx_norm_grad_workspace_bytes,
+    sparq_mx_sort, sparq_mx_gather, sparq_mx_combine, sparq_mx_combine_grad, sparq_mx_experts_gemm, sparq_mx_experts_linear,
+    sparq_mx_experts_dx, sparq_mx_experts_dw, sparq_mx_dropout, sparq_mx_sort_workspace_bytes,
+    sparq_mx_experts_gemm_workspace_bytes, sparq_mx_experts_linear_workspace_bytes, sparq_mx_experts_dx_workspace_bytes,
+    sparq_mx_experts_dw_workspace_bytes,
 )
 
 __all__ = ["LIB_PATH", "SparqConvDesc", "SparqError", "SparqMode", "conv_desc", "lib", "mode", "out_rows",
@@ -23,4 +27,8 @@ __all__ = ["LIB_PATH", "SparqConvDesc", "SparqError", "SparqMode", "conv_desc", 
            "sparq_mx_quantize", "sparq_mx_dequantize", "sparq_mx_gemm", "sparq_mx_linear", "sparq_mx_linear_dx",
            "sparq_mx_linear_dw", "sparq_mx_act", "sparq_mx_act_grad", "sparq_mx_norm", "sparq_mx_norm_grad",
            "sparq_mx_code_bytes", "sparq_mx_scale_bytes", "sparq_mx_gemm_workspace_bytes", "sparq_mx_linear_workspace_bytes",
-           "sparq_mx_linear_dx_workspace_bytes", "sparq_mx_linear_dw_workspace_bytes", "sparq_mx_norm_grad_workspace_bytes"]
+           "sparq_mx_linear_dx_workspace_bytes", "sparq_mx_linear_dw_workspace_bytes", "sparq_mx_norm_grad_workspace_bytes",
+           "sparq_mx_sort", "sparq_mx_gather", "sparq_mx_combine", "sparq_mx_combine_grad", "sparq_mx_experts_gemm", "sparq_mx_experts_linear",
+           "sparq_mx_experts_dx", "sparq_mx_experts_dw", "sparq_mx_dropout", "sparq_mx_sort_workspace_bytes",
+           "sparq_mx_experts_gemm_workspace_bytes", "sparq_mx_experts_linear_workspace_bytes", "sparq_mx_experts_dx_workspace_bytes",
+           "sparq_mx_experts_dw_workspace_bytes"]

@@ -90,6 +90,10 @@ def _load() -> ctypes.CDLL:
                        ("linear_dw_workspace_bytes", [i64, i32, i32]), ("norm_grad_workspace_bytes", [i64, i32])):
         f = getattr(L, "sparq_mx_" + name)
         f.argtypes, f.restype = args, sz
+    L.sparq_mx_sort_workspace_bytes.argtypes, L.sparq_mx_sort_workspace_bytes.restype = [i64, i32], sz
+    for name in ("gemm", "linear", "dx", "dw"):
+        f = getattr(L, f"sparq_mx_experts_{name}_workspace_bytes")
+        f.argtypes, f.restype = [i64, i32, i32, i32], sz
     L.sparq_strerror.argtypes = [ctypes.c_int]
     L.sparq_strerror.restype = ctypes.c_char_p
     return L
@@ -108,6 +112,8 @@ def _load_native():
     n.bind(tuple(ctypes.cast(getattr(lib, "sparq_" + k), ctypes.c_void_p).value for k in names), SparqMode, SparqConvDesc, SparqError)
     names = ("quantize", "dequantize", "gemm", "linear", "linear_dx", "linear_dw", "act", "act_grad", "norm", "norm_grad", "code_bytes", "scale_bytes")
     n.bind_mx(tuple(ctypes.cast(getattr(lib, "sparq_mx_" + k), ctypes.c_void_p).value for k in names))
+    names = ("sort", "gather", "combine", "combine_grad", "experts_gemm", "experts_linear", "experts_dx", "experts_dw", "dropout")
+    n.bind_experts(tuple(ctypes.cast(getattr(lib, "sparq_mx_" + k), ctypes.c_void_p).value for k in names))
     return n
 
 
@@ -131,6 +137,15 @@ sparq_mx_act = _native.sparq_mx_act
 sparq_mx_act_grad = _native.sparq_mx_act_grad
 sparq_mx_norm = _native.sparq_mx_norm
 sparq_mx_norm_grad = _native.sparq_mx_norm_grad
+sparq_mx_sort = _native.sparq_mx_sort
+sparq_mx_gather = _native.sparq_mx_gather
+sparq_mx_combine = _native.sparq_mx_combine
+sparq_mx_combine_grad = _native.sparq_mx_combine_grad
+sparq_mx_experts_gemm = _native.sparq_mx_experts_gemm
+sparq_mx_experts_linear = _native.sparq_mx_experts_linear
+sparq_mx_experts_dx = _native.sparq_mx_experts_dx
+sparq_mx_experts_dw = _native.sparq_mx_experts_dw
+sparq_mx_dropout = _native.sparq_mx_dropout
 
 
 def strerror(status: int) -> str:
@@ -283,3 +298,23 @@ def sparq_mx_linear_dw_workspace_bytes(M: int, N: int, K: int) -> int:
 
 def sparq_mx_norm_grad_workspace_bytes(rows: int, K: int) -> int:
     return int(lib.sparq_mx_norm_grad_workspace_bytes(int(rows), int(K)))
+
+
+def sparq_mx_sort_workspace_bytes(slots: int, experts: int) -> int:
+    return int(lib.sparq_mx_sort_workspace_bytes(int(slots), int(experts)))
+
+
+def sparq_mx_experts_gemm_workspace_bytes(M: int, N: int, K: int, experts: int = 1) -> int:
+    return int(lib.sparq_mx_experts_gemm_workspace_bytes(int(M), int(N), int(K), int(experts)))
+
+
+def sparq_mx_experts_linear_workspace_bytes(M: int, N: int, K: int, experts: int = 1) -> int:
+    return int(lib.sparq_mx_experts_linear_workspace_bytes(int(M), int(N), int(K), int(experts)))
+
+
+def sparq_mx_experts_dx_workspace_bytes(M: int, N: int, K: int, experts: int) -> int:
+    return int(lib.sparq_mx_experts_dx_workspace_bytes(int(M), int(N), int(K), int(experts)))
+
+
+def sparq_mx_experts_dw_workspace_bytes(M: int, N: int, K: int, experts: int) -> int:
+    return int(lib.sparq_mx_experts_dw_workspace_bytes(int(M), int(N), int(K), int(experts)))

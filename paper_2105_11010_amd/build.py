@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsparq.so")
 PROBE_SRC = os.path.join(CSRC, "probe", "sparq_probe.hip")
 PROBE_LIB = os.path.join(HERE, "libsparq_probe.so")   # machine-ceiling micro-benchmarks (include/sparq_probe.h)
-NATIVE_SRCS = [os.path.join(CSRC, "binding", f) for f in ("sparq_native.cpp", "sparq_native_mx.cpp")]
+NATIVE_SRCS = [os.path.join(CSRC, "binding", f) for f in ("sparq_native.cpp", "sparq_native_mx.cpp", "sparq_native_experts.cpp")]
 NATIVE_LIB = os.path.join(HERE, "_sparq_native.so")   # argument marshalling of the hot entry points (binding.py)
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

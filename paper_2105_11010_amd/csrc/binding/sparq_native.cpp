@@ -7,6 +7,7 @@
 
 namespace sparq_native {
 bool add_mx_methods(PyObject* module);      // sparq_native_mx.cpp
+bool add_experts_methods(PyObject* module); // sparq_native_experts.cpp
 }
 
 namespace {
@@ -288,6 +289,6 @@ PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_sparq_native", nullptr, -1, m
 
 PyMODINIT_FUNC PyInit__sparq_native() {
     PyObject* module = PyModule_Create(&module_def);
-    if (module && !add_mx_methods(module)) Py_CLEAR(module);
+    if (module && !(add_mx_methods(module) && add_experts_methods(module))) Py_CLEAR(module);
     return module;
 }

@@ -72,12 +72,12 @@ inline const at::Tensor& tensor(PyObject* o, const char* name) {
     return THPVariable_Unpack(o);
 }
 template <class T>
-constexpr at::ScalarType kDtype = std::is_same_v<T, uint8_t> ? at::kByte : std::is_same_v<T, int32_t> ? at::kInt : at::kFloat;
+constexpr at::ScalarType kDtype = std::is_same_v<T, uint8_t> ? at::kByte : std::is_same_v<T, int32_t> ? at::kInt : std::is_same_v<T, int64_t> ? at::kLong : at::kFloat;
 template <class T>
 T* device_pointer(const at::Tensor& t, const char* name) {
     if (!t.is_cuda() || t.scalar_type() != kDtype<T> || !t.is_contiguous()) {
         PyErr_Format(PyExc_TypeError, "%s must be a contiguous device tensor of dtype %s", name,
-                     kDtype<T> == at::kByte ? "torch.uint8" : kDtype<T> == at::kInt ? "torch.int32" : "torch.float32");
+                     kDtype<T> == at::kByte ? "torch.uint8" : kDtype<T> == at::kInt ? "torch.int32" : kDtype<T> == at::kLong ? "torch.int64" : "torch.float32");
         throw PythonError{};
     }
     return static_cast<T*>(t.data_ptr());

@@ -1,0 +1,126 @@
+// The experts' products, backward: entry points and the choice of tiles (include/sparq_mx_experts.h).
+#include "sparq_mx_experts_grad.h"
+
+namespace sparq {
+namespace mx {
+
+// Sums of dy's columns over each expert's rows, 64 columns a workgroup.
+constexpr int kSumThreads = 1024;
+template <class T>
+__global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __restrict__ dy, int64_t lddy, const int32_t* __restrict__ offsets, int64_t rows, int N,
+                                                                  float* __restrict__ db) {
+    typedef ColumnSums<T, kSumThreads> Sums;
+    __shared__ float shared[Sums::kFloats];
+    int first, n;
+    expert_rows(offsets, blockIdx.y, rows, first, n);
+    Sums::run(dy, lddy, first, (int64_t)first + n, N, blockIdx.x * Sums::kColumns, db + (int64_t)blockIdx.y * N, shared);
+}
+
+// Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them, as in sparq_mx_grad.hip.
+static int grad_tile(int dy_type, int64_t tiles256, int64_t tiles128, int64_t steps, bool dw) {
+    const bool bf16 = dy_type == SPARQ_MX_BF16;
+    return bf16 && !(dw && steps <= 4) && 3 * ((tiles256 + 255) / 256) <= 2 * ((tiles128 + 511) / 512) ? 256 : tiles128 >= 192 ? 128 : 64;
+}
+static int dx_tile(int dy_type, int64_t M, int K, int experts) {
+    const auto tiles = [&](int t) { return (M / t + experts / 2 + 1) * ((K + t - 1) / t); };
+    return grad_tile(dy_type, tiles(256), tiles(128), 0, false);
+}
+static int dw_tile(int dy_type, int64_t M, int N, int K, int experts) {
+    const auto tiles = [&](int64_t t) { return experts * ((N + t - 1) / t) * ((K + t - 1) / t); };
+    return grad_tile(dy_type, tiles(256), tiles(128), (M / experts + kGradStep - 1) / kGradStep, true);
+}
+static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K, int64_t experts) {
+    return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40) && experts_ok((int)experts);
+}
+static bool grad_countable(int64_t M, int64_t N, int experts) {
+    return M < 1ll << 31 && experts <= SPARQ_MX_EXPERTS_MOST && experts * N < 1ll << 31;
+}
+static ExpertGradParams grad_params(const void* dy, int64_t lddy, const void* codes, const void* scales, int bits, int64_t ldo, int64_t J, int64_t R, int K,
+                                    const int32_t* offsets, int64_t rows) {
+    ExpertGradParams p = {};
+    p.dy = dy;
+    p.codes = static_cast<const uint8_t*>(codes);
+    p.scales = static_cast<const uint8_t*>(scales);
+    p.lddy = lddy;
+    p.code_pitch = code_pitch(K, bits);
+    p.scale_pitch = scale_pitch(K);
+    p.ldo = ldo;
+    p.J = J;
+    p.R = R;
+    p.K = K;
+    p.K128 = (int)round_up(K, kCodeUnit);
+    p.offsets = offsets;
+    p.rows = rows;
+    return p;
+}
+// Whether steps can be read without checks: the loads' offsets are 32 bits
+static bool reads_fit(int64_t lddy, int64_t pitch) { return lddy < 1 << 21 && pitch < 1 << 24; }
+
+}  // namespace mx
+}  // namespace sparq
+
+using namespace sparq;
+using namespace sparq::mx;
+
+extern "C" size_t sparq_mx_experts_dx_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t experts) {
+    return grad_sizes_ok(M, N, K, experts) && M > 0 ? table_bytes(M, experts) : 0;
+}
+extern "C" size_t sparq_mx_experts_dw_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t experts) {
+    (void)M, (void)N, (void)K, (void)experts;
+    return 0;
+}
+
+extern "C" sparq_status sparq_mx_experts_dx(const void* dy, int32_t dy_type, int64_t lddy, const int32_t* offsets, int32_t experts, const void* w_codes,
+                                            const void* w_scales, void* dx, int32_t dx_type, int64_t lddx, int64_t M, int32_t N, int32_t K, void* workspace,
+                                            size_t workspace_bytes, void* stream) {
+    if (!grad_sizes_ok(M, N, K, experts) || !type_valid(dy_type) || (dx_type != dy_type && dx_type != SPARQ_MX_F32)) return SPARQ_EINVAL;
+    if (!offsets || !aligned(offsets, 4)) return SPARQ_EINVAL;
+    if (M == 0) return SPARQ_OK;
+    if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
+    if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
+    if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
+    if (workspace_bytes < table_bytes(M, experts)) return SPARQ_EWORKSPACE;
+    const int t = dx_tile(dy_type, M, K, experts);
+    const int64_t tiles_j = most_tiles(M, experts, t), tiles_k = (K + t - 1) / t;
+    if (!grad_countable(M, N, experts) || tiles_j * tiles_k * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    const sparq_status tiled = launch_tiles(offsets, experts, M, t, workspace, s);
+    if (tiled != SPARQ_OK) return tiled;
+    ExpertGradParams p = grad_params(dy, lddy, w_codes, w_scales, 4, lddx, M, N, K, offsets, M);
+    p.table = static_cast<const ExpertTile*>(workspace);
+    p.tiles_k = (int)tiles_k;
+    p.s_whole = reads_fit(lddy, p.code_pitch) ? N / kGradStep : 0;
+    p.steps_per_part = (N + kGradStep - 1) / kGradStep;
+    const dim3 grid((unsigned)(tiles_j * tiles_k));
+    return (dy_type == SPARQ_MX_F32 ? launch_experts_dx_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dx_f16 : launch_experts_dx_bf16)(
+        p, grid, t, dx, dx_type == SPARQ_MX_F32, s);
+}
+
+extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int64_t lddy, const int32_t* offsets, int32_t experts, const void* x_codes,
+                                            const void* x_scales, void* dw, int32_t dw_type, int64_t lddw, float* db, int64_t M, int32_t N, int32_t K,
+                                            void* workspace, size_t workspace_bytes, void* stream) {
+    (void)workspace, (void)workspace_bytes;
+    if (!grad_sizes_ok(M, N, K, experts) || !type_valid(dy_type) || (dw_type != dy_type && dw_type != SPARQ_MX_F32)) return SPARQ_EINVAL;
+    if (!offsets || !aligned(offsets, 4)) return SPARQ_EINVAL;
+    if (!tensor_ok(dw, dw_type, lddw, K) || !extent_ok((int64_t)experts * N, lddw) || !aligned(db, 4)) return SPARQ_EINVAL;
+    if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K))) return SPARQ_EINVAL;
+    const int t = dw_tile(dy_type, M, N, K, experts);
+    const int64_t tiles_j = (N + t - 1) / t, tiles_k = (K + t - 1) / t;
+    if (!grad_countable(M, N, experts) || tiles_j * tiles_k * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
+    const hipStream_t s = static_cast<hipStream_t>(stream);
+    ExpertGradParams p = grad_params(dy, M > 0 ? lddy : 0, x_codes, x_scales, 8, lddw, N, 0, K, offsets, M);
+    p.tiles_j = (int)tiles_j;
+    p.tiles_k = (int)tiles_k;
+    // A run that the last column cuts reads on into the next rows: an expert's last rows, which it would leave, are not read in runs.
+    p.s_whole = M > 0 && reads_fit(lddy, p.code_pitch);
+    p.margin = M > 0 ? (int)((round_up(N, 8) - N + lddy - 1) / lddy) : 0;
+    const dim3 grid((unsigned)(tiles_j * tiles_k), (unsigned)experts);
+    const sparq_status done = (dy_type == SPARQ_MX_F32 ? launch_experts_dw_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dw_f16 : launch_experts_dw_bf16)(
+        p, grid, t, dw, dw_type == SPARQ_MX_F32, s);
+    if (done != SPARQ_OK || !db) return done;
+    with_type(dy_type, [&](auto y) {
+        typedef decltype(y) T;
+        expert_sums_kernel<T><<<dim3((unsigned)((N + 63) / 64), (unsigned)experts), kSumThreads, 0, s>>>(static_cast<const T*>(dy), p.lddy, offsets, M, N, db);
+    });
+    return launch_status();
+}

@@ -17,6 +17,7 @@
 #include <utility>
 
 #include "sparq_mx_store.h"
+#include "sparq_mx_tiles.h"
 
 namespace sparq {
 namespace mx {
@@ -40,8 +41,9 @@ template <int TILE> constexpr int kGemmLds = 4 * 2 * TILE * 64 + 2 * 2 * TILE * 
 
 template <int N> using Const = std::integral_constant<int, N>;
 
-template <class O, int TM, int TN>
-__global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, const GemmParams p) {
+// P: GemmParams, or what sparq_mx_experts_gemm.h makes of it -- rows of several experts, each tile of one, and an epilogue of its own.
+template <class O, int TM, int TN, class P = GemmParams>
+__global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, const P p) {
 #if defined(__HIP_DEVICE_COMPILE__)                          // (the host's pass does not know loads of 16 bytes to LDS, and leaves the kernel out)
     constexpr int FM = TM / 64, FN = TN / 64;                // 32 x 32 results a wavefront makes along either side
     constexpr int kBuffer = (TM + TN) * 64, kScaleBuffer = (TM + TN) * 16;
@@ -53,16 +55,39 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
 
     // A tile of results and its share of the reduction.
     struct Item {
-        int64_t m0;
+        int64_t m0, m_end;
         int n0, s_begin, steps;
-        uint32_t part;
+        uint32_t part, expert;
     };
+    constexpr bool kExperts = !std::is_same_v<P, GemmParams>;
+    uint32_t items = p.items, tiles_m = p.tiles_m;
+    if constexpr (kExperts)
+        if (p.table) {
+            tiles_m = (uint32_t)tile_count(p.table);
+            items = tiles_m * p.tiles_n;
+            if (blockIdx.x >= items) return;
+        }
     auto item_of = [&](uint32_t id) __attribute__((always_inline)) {
         Item it;
         uint32_t tm, tn;
+        it.expert = 0;
+        if constexpr (kExperts)
+            if (p.table) {
+                tile_of(id, tiles_m, p.tiles_n, tm, tn);
+                const ExpertTile t = expert_tile(p.table, tm);
+                it.part = 0;
+                it.m0 = t.row;
+                it.m_end = t.row + t.rows;
+                it.n0 = (int)tn * TN;
+                it.s_begin = 0;
+                it.steps = p.steps;
+                it.expert = t.expert;
+                return it;
+            }
         it.part = p.tiles_m * p.tiles_n == p.items ? 0 : id / (p.tiles_m * p.tiles_n);
         tile_of(id - it.part * p.tiles_m * p.tiles_n, p.tiles_m, p.tiles_n, tm, tn);
         it.m0 = (int64_t)tm * TM;
+        it.m_end = p.M;
         it.n0 = (int)tn * TN;
         it.s_begin = it.part * p.steps_per_part;
         it.steps = p.steps - it.s_begin < p.steps_per_part ? p.steps - it.s_begin : p.steps_per_part;
@@ -72,14 +97,15 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
     __amdgpu_buffer_rsrc_t ra, rw, ras, rws;
     int load_step;
     auto open = [&](const Item& it) __attribute__((always_inline)) {
-        const uint32_t rows_m = p.M - it.m0 < TM ? (uint32_t)(p.M - it.m0) : TM, rows_n = p.N - it.n0 < TN ? p.N - it.n0 : TN;
+        const uint32_t rows_m = it.m_end - it.m0 < TM ? (uint32_t)(it.m_end - it.m0) : TM, rows_n = p.N - it.n0 < TN ? p.N - it.n0 : TN;
         const auto buffer = [](const uint8_t* base, uint32_t rows, uint32_t pitch) __attribute__((always_inline)) {
             return __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(base), 0, (int)(rows * pitch), 0x00020000);
         };
         ra = buffer(p.a + it.m0 * p.code_pitch, rows_m, p.code_pitch);
-        rw = buffer(p.w + (int64_t)it.n0 * p.code_pitch, rows_n, p.code_pitch);
+        const int64_t w_row = (kExperts ? (int64_t)it.expert * p.N : 0) + it.n0;
+        rw = buffer(p.w + w_row * p.code_pitch, rows_n, p.code_pitch);
         ras = buffer(p.as + it.m0 * p.scale_pitch, rows_m, p.scale_pitch);
-        rws = buffer(p.ws + (int64_t)it.n0 * p.scale_pitch, rows_n, p.scale_pitch);
+        rws = buffer(p.ws + w_row * p.scale_pitch, rows_n, p.scale_pitch);
         load_step = it.s_begin;
     };
     // One load brings 16 rows: lane l row l / 4 and its 16-byte unit (l % 4) ^ (row / 4 % 4), which lands in place l % 4: the
@@ -176,7 +202,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         if (place == 0 && s + 4 == it.steps) {               // from here on the loads are the next item's (none: the last one's again, unread)
-            if (next_id < p.items) open(item_of(next_id));
+            if (next_id < items) open(item_of(next_id));
             else load_step = it.s_begin;
         }
         multiply(second, scales, Const<1>{}, [&](int i) __attribute__((always_inline)) {
@@ -215,7 +241,7 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         read_scale(scales, 0, 0, i);
         shift_scale(scales, i);
     }
-    for (; id < p.items; id += gridDim.x) {
+    for (; id < items; id += gridDim.x) {
         const Item it = item_of(id);
 #pragma unroll
         for (int i = 0; i < FN; ++i)
@@ -230,9 +256,13 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         groups += it.steps >> 2;
         // The next item's first three steps are there before the results' stores queue up behind them.
         __builtin_amdgcn_s_waitcnt(vmcnt(kLoads / 2));
-        const __amdgpu_buffer_rsrc_t bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.bias), 0, p.bias ? p.N * 4 : 0, 0x00020000);
-        store_results<O, FN, FM, kTurnRow<TM>>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, p.M, it.n0 + wn, p.N, bias,
-                                               lds + 4 * kBuffer + 2 * kScaleBuffer + wave * 32 * kTurnRow<TM>);
+        const float* const its_bias = p.bias ? p.bias + (kExperts ? (int64_t)it.expert * p.N : 0) : nullptr;
+        const __amdgpu_buffer_rsrc_t bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(its_bias), 0, p.bias ? p.N * 4 : 0, 0x00020000);
+        uint8_t* const turn = lds + 4 * kBuffer + 2 * kScaleBuffer + wave * 32 * kTurnRow<TM>;
+        if constexpr (kExperts)
+            p.epilogue.template store<O, FN, FM, kTurnRow<TM> / 4>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, it.m_end, it.n0 + wn, p.N, it.n0 + TN, bias, turn);
+        else
+            store_results<O, FN, FM, kTurnRow<TM>>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, p.M, it.n0 + wn, p.N, bias, turn);
     }
     __builtin_amdgcn_s_waitcnt(vmcnt(0));                    // nothing is on its way to LDS when the wavefront ends
 #endif

@@ -18,6 +18,7 @@
 #include <type_traits>
 
 #include "sparq_mx_grad_kernel.h"
+#include "sparq_mx_tiles.h"
 
 namespace sparq {
 namespace mx {
@@ -26,9 +27,17 @@ template <int TILE> inline constexpr int kWideBytes = kGradStep * TILE * 2;     
 
 template <class T, int TILE> inline constexpr int kWideLds = 2 * (kParts<T> + 1) * kWideBytes<TILE>;
 template <class T, int TILE> inline constexpr int kWidePerCu = kWideLds<T, TILE> < 40 * 1024 ? 4 : 160 * 1024 / kWideLds<T, TILE>;
-template <class T, class O, bool DW, int TILE>
-__global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide_kernel(O* __restrict__ out, const GradParams p) {
+// PARAMS: GradParams, or what sparq_mx_experts_grad.h makes of it -- dx's tiles of one expert's rows each, dw a workgroup's of one expert.
+template <class T, class O, bool DW, int TILE, class PARAMS = GradParams>
+__global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide_kernel(O* __restrict__ out, const PARAMS all) {
 #if defined(__HIP_DEVICE_COMPILE__)
+    constexpr bool kExperts = !std::is_same_v<PARAMS, GradParams>;
+    std::conditional_t<kExperts, GradParams, const GradParams&> p = all;
+    if constexpr (kExperts) {
+        if (!all.template own<T, DW>(p)) return;
+        if constexpr (DW) out += blockIdx.y * p.J * p.ldo;
+    }
+    const uint32_t part = kExperts ? 0 : blockIdx.y;
     constexpr int P = kParts<T>;                             // of dy, a tile each
     constexpr int kF = TILE / 64, kSlots = P * kF * kF;      // 32 x 32 results along a side; matrix instructions a quarter
     constexpr int kRow = TILE * 2;                           // bytes of a tile's row
@@ -40,7 +49,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
     uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * P * kBytes;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
-    if constexpr (DW) {
+    if constexpr (DW && !kExperts) {
         const uint32_t tiles = (uint32_t)p.tiles_j * (uint32_t)p.tiles_k;
         if (blockIdx.x >= tiles) {
             typedef ColumnSums<T, kGradThreads> Sums;
@@ -55,9 +64,12 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     }
     uint32_t tj, tk;
     tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
-    const int64_t j0 = (int64_t)tj * TILE;
+    int64_t j0 = (int64_t)tj * TILE;
+    if constexpr (kExperts && !DW) {
+        j0 = all.rows_of(p, tj);
+    }
     const int k0 = (int)tk * TILE;
-    const int64_t s_begin = (int64_t)blockIdx.y * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
+    const int64_t s_begin = (int64_t)part * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;
     const int64_t s_end = s_begin + p.steps_per_part < s_all ? s_begin + p.steps_per_part : s_all, s_fast = p.s_whole < s_end ? p.s_whole : s_end;
     Products<P, TILE, TILE> products;
     const int wj = products.wj, wk = products.wk;
@@ -262,7 +274,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
-    store_results<O, kF, kF, kF == 1 ? 64 : 128>(products.acc, out + blockIdx.y * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
+    store_results<O, kF, kF, kF == 1 ? 64 : 128>(products.acc, out + part * p.part_stride, p.ldo, j0 + wj, p.J, k0 + wk, p.K, none, lds8 + wave * 4096);
 #endif
 }
 
