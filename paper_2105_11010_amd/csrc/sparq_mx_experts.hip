@@ -67,7 +67,15 @@ struct ExpertsPlan {
     int64_t pieces;          // few rows: workgroups along them
     size_t table_bytes, partial_bytes;
 };
-static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offsets, bool kept) {
+// What a round of tiles takes (us): one of 256 x 256 a CU, or two of 128 x 128, by the length of the reduction and what comes behind it.  One wavefront a SIMD
+// has nobody to multiply while it makes its results; of two workgroups a CU one does.  (bf16, measured: 8192 x 4096 x 4096, 256 -> 128: 85 -> 97, with gelu 114 -> 105,
+// kept 102 -> 109, both 127 -> 121; 16384 x 4096 x 2048 104 -> 107, 163 -> 121, 136 -> 124, 187 -> 145, residual 140 -> 130; of 1024 76 -> 61.)
+static double round_of(int tile, int K, int function, bool residual, bool kept) {
+    const bool gelu = function == SPARQ_MX_GELU, silu = function == SPARQ_MX_SILU;
+    if (tile == 256) return 11.0 + 7.6 * K / 1024 + (gelu ? 14.7 : silu ? 8.0 : 0.0) + (residual ? 5.0 : 0.0) + (kept ? 8.0 : 0.0);
+    return 1.9 + 5.7 * K / 1024 + (gelu ? 1.8 : silu ? 1.0 : 0.0) + (residual ? 2.8 : 0.0) + (kept ? 2.0 : 0.0);
+}
+static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offsets, int function, bool residual, bool kept) {
     ExpertsPlan p = {};
     p.parts = 1;
     // What an expert has of the rows on average; how they are divided is not known here.
@@ -77,8 +85,11 @@ static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
         p.pieces = offsets ? most_tiles(M, experts, 16 * p.fragments) : 1;
         return p;
     }
-    const auto tiles = [&](int t) { return (M / t + (offsets ? experts / 2 : 0) + 1) * ((N + t - 1) / t); };
-    p.tile = tiles(256) >= 192 ? 256 : tiles(128) >= 112 ? 128 : 64;
+    // (of experts' rows about half of an expert's last tile is empty)
+    const auto tiles = [&](int t) { return (offsets ? M / t + (experts + 1) / 2 : (M + t - 1) / t) * ((N + t - 1) / t); };
+    const int64_t rounds256 = (tiles(256) + 255) / 256, rounds128 = (tiles(128) + 511) / 512;
+    if (tiles(128) < 112) p.tile = 64;
+    else p.tile = rounds256 * round_of(256, K, function, residual, kept) < rounds128 * round_of(128, K, function, residual, kept) ? 256 : 128;
     if (offsets) {
         p.table_bytes = table_bytes(M, experts);
         return p;
@@ -88,16 +99,18 @@ static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
     p.partial_bytes = p.parts > 1 ? (size_t)round_up(p.parts * M * N * 4, 256) : 0;
     return p;
 }
-// Whether offsets or the kept form are given does not change what the query names: the most of all.
+// What the epilogue is and whether there are offsets does not change what the query names: the most of all.
 static size_t experts_bytes(int64_t M, int N, int K, int experts) {
     size_t most = 0;
-    for (const bool offsets : {false, true})
-        for (const bool kept : {false, true}) {
-            if (!offsets && experts > 1) continue;
-            const ExpertsPlan p = experts_plan(M, N, K, experts, offsets, kept);
+    for (int form = 0; form < 8; ++form) {
+        const bool offsets = form & 1, residual = form & 2, kept = form & 4;
+        if (!offsets && experts > 1) continue;
+        for (const int function : {(int)SPARQ_MX_NONE, (int)SPARQ_MX_SILU, (int)SPARQ_MX_GELU}) {
+            const ExpertsPlan p = experts_plan(M, N, K, experts, offsets, function, residual, kept);
             const size_t bytes = p.table_bytes + p.partial_bytes;
             most = bytes > most ? bytes : most;
         }
+    }
     return most;
 }
 
@@ -222,7 +235,7 @@ extern "C" sparq_status sparq_mx_experts_gemm(const void* a_codes, const void* a
     if (!coded_ok(a_codes, a_scales) || !coded_ok(w_codes, w_scales) || !aligned(bias, 4)) return SPARQ_EINVAL;
     if (!tensor_ok(y, type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K) || !epilogue_ok(function, residual, ldr, type, kept_codes, kept_scales, M, N))
         return SPARQ_EINVAL;
-    const ExpertsPlan plan = experts_plan(M, N, K, experts, offsets != nullptr, kept_codes != nullptr);
+    const ExpertsPlan plan = experts_plan(M, N, K, experts, offsets != nullptr, function, residual != nullptr, kept_codes != nullptr);
     const size_t bytes = plan.table_bytes + plan.partial_bytes;
     if (bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < bytes) return SPARQ_EWORKSPACE;
@@ -247,7 +260,7 @@ extern "C" sparq_status sparq_mx_experts_linear(const void* x, int32_t x_type, i
     if (!tensor_ok(x, x_type, ldx, K) || !extent_ok(M, ldx) || !coded_ok(w_codes, w_scales) || !aligned(bias, 4)) return SPARQ_EINVAL;
     if (!tensor_ok(y, y_type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K) || !epilogue_ok(function, residual, ldr, y_type, kept_codes, kept_scales, M, N))
         return SPARQ_EINVAL;
-    const ExpertsPlan plan = experts_plan(M, N, K, experts, offsets != nullptr, kept_codes != nullptr);
+    const ExpertsPlan plan = experts_plan(M, N, K, experts, offsets != nullptr, function, residual != nullptr, kept_codes != nullptr);
     const bool on_the_way = quantised_on_the_way(plan, M, N, K, experts);
     const size_t coded = on_the_way ? 0 : coded_bytes(M, K), bytes = coded + plan.table_bytes + plan.partial_bytes;
     if (bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;

@@ -12,6 +12,11 @@ struct ExpertGemmParams : GemmParams {
     const ExpertTile* table;             // NULL: one expert, all rows
     Epilogue epilogue;
 };
+// ... of one function: a kernel each, or a tile's end would hold all of them
+template <int F>
+struct ExpertGemmParamsOf : ExpertGemmParams {
+    static constexpr int kFunction = F;
+};
 
 struct ExpertFewParams : FewParams {
     const int32_t* offsets;              // NULL: one expert, all rows (M)
@@ -59,9 +64,10 @@ SPARQ_MX_EXPERTS_DECLARE(f32)
 SPARQ_MX_EXPERTS_DECLARE(f16)
 SPARQ_MX_EXPERTS_DECLARE(bf16)
 
-template <class O, int TILE>
-sparq_status launch_experts_tile(const ExpertGemmParams& p, void* y, hipStream_t stream) {
-    const auto kernel = gemm_kernel<O, TILE, TILE, ExpertGemmParams>;
+template <class O, int TILE, int F>
+sparq_status launch_experts_function(const ExpertGemmParams& all, void* y, hipStream_t stream) {
+    const ExpertGemmParamsOf<F> p = {all};
+    const auto kernel = gemm_kernel<O, TILE, TILE, ExpertGemmParamsOf<F>>;
     constexpr int lds_bytes = kGemmLds<TILE>, per_cu = 160 * 1024 / lds_bytes;
     static std::atomic<bool> allowed[kMaxDevices];           // the attribute is set once per device (twice at worst)
     const int slot = current_device_slot();
@@ -73,6 +79,12 @@ sparq_status launch_experts_tile(const ExpertGemmParams& p, void* y, hipStream_t
     const uint32_t places = (uint32_t)(device_cu_count() * per_cu);
     kernel<<<p.items < places ? p.items : places, kGemmThreads, lds_bytes, stream>>>(static_cast<O*>(y), p);
     return launch_status();
+}
+template <class O, int TILE>
+sparq_status launch_experts_tile(const ExpertGemmParams& p, void* y, hipStream_t stream) {
+    return p.epilogue.function == SPARQ_MX_SILU   ? launch_experts_function<O, TILE, SPARQ_MX_SILU>(p, y, stream)
+           : p.epilogue.function == SPARQ_MX_GELU ? launch_experts_function<O, TILE, SPARQ_MX_GELU>(p, y, stream)
+                                                  : launch_experts_function<O, TILE, SPARQ_MX_NONE>(p, y, stream);
 }
 template <class O>
 sparq_status launch_experts_tiles(const ExpertGemmParams& p, int tile, void* y, hipStream_t stream) {

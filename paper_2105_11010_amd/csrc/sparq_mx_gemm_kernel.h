@@ -256,13 +256,14 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         groups += it.steps >> 2;
         // The next item's first three steps are there before the results' stores queue up behind them.
         __builtin_amdgcn_s_waitcnt(vmcnt(kLoads / 2));
-        const float* const its_bias = p.bias ? p.bias + (kExperts ? (int64_t)it.expert * p.N : 0) : nullptr;
-        const __amdgpu_buffer_rsrc_t bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(its_bias), 0, p.bias ? p.N * 4 : 0, 0x00020000);
         uint8_t* const turn = lds + 4 * kBuffer + 2 * kScaleBuffer + wave * 32 * kTurnRow<TM>;
-        if constexpr (kExperts)
-            p.epilogue.template store<O, FN, FM, kTurnRow<TM> / 4>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, it.m_end, it.n0 + wn, p.N, it.n0 + TN, bias, turn);
-        else
+        if constexpr (kExperts) {
+            p.epilogue.template store<P::kFunction>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, it.m_end, it.n0 + wn, p.N, it.n0 + TN,
+                                                    p.bias ? p.bias + (int64_t)it.expert * p.N : nullptr, turn);
+        } else {
+            const __amdgpu_buffer_rsrc_t bias = __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(p.bias), 0, p.bias ? p.N * 4 : 0, 0x00020000);
             store_results<O, FN, FM, kTurnRow<TM>>(acc, y + it.part * p.part_stride, p.ldy, it.m0 + wm, p.M, it.n0 + wn, p.N, bias, turn);
+        }
     }
     __builtin_amdgcn_s_waitcnt(vmcnt(0));                    // nothing is on its way to LDS when the wavefront ends
 #endif
