@@ -7,6 +7,10 @@ namespace mx {
 constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
+// 16-bit results of what adds up and its gradient go past the caches: the rows these read have the caches to themselves, and what is written is not written back
+// while the next kernel runs (8192 tokens of 4096, two rows each, one after the other: 42 and 60 us -> 36 and 54).
+template <class T> inline constexpr bool kPast = sizeof(T) == 2;
+
 struct RouteParams {
     const int32_t* place;
     const float* weights;
@@ -65,20 +69,19 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const T* __restrict__ 
     }
 }
 
-// A wavefront makes 512 values of a token's row; the rows of four slots are on their way at a time.  (A slot without a row reads row 0 and leaves it out: a
-// branch would have one row wait for another.)
-template <class T, int STREAMING>
+// A wavefront makes 512 values of a token's row, or 1024, and the rows of four slots are on their way at a time.  (A slot without a row reads row 0 and leaves it
+// out: a branch would have one row wait for another.)
+template <class T, int CHUNKS, bool NT>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__ x, const T* __restrict__ residual, T* __restrict__ y, const RouteParams p) {
     const int lane = threadIdx.x & 63;
     const uint32_t item = blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     if (item >= p.items) return;
     const uint32_t token = fastdiv(item, p.div_chunks);
-    const int col = (int)(item - token * p.chunks) * kScaleUnit + 8 * lane, n = p.K - col;
-    if (n <= 0) return;
+    const int col = (int)(item - token * p.chunks) * (CHUNKS * kScaleUnit) + 8 * lane, n = p.K - col;
     const int64_t slot = (int64_t)token * p.per;
-    float sum[8] = {};
+    float sum[CHUNKS][8] = {};
     for (int j0 = 0; j0 < p.per && p.rows > 0; j0 += 4) {
-        Raw8<T> raw[4];
+        Raw8<T> raw[4][CHUNKS];
         float w[4];
         bool there[4];
 #pragma unroll
@@ -87,34 +90,47 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__
             const int64_t row = p.place[slot + j];
             there[i] = j0 + i < p.per && row >= 0 && row < p.rows;
             w[i] = p.weights ? p.weights[slot + j] : 1.0f;
-            if (j0 + i < p.per) load_raw_upto8<STREAMING == kAll>(x + (there[i] ? row : 0) * p.ldx + col, n, raw[i]);
+            if (j0 + i < p.per) {
+#pragma unroll
+                for (int h = 0; h < CHUNKS; ++h) load_raw_upto8<false>(x + (there[i] ? row : 0) * p.ldx + col + h * kScaleUnit, n - h * kScaleUnit, raw[i][h]);
+            }
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            float v[8];
-            values_of(raw[i], v);
             if (there[i]) {
 #pragma unroll
-                for (int e = 0; e < 8; ++e) sum[e] = __builtin_fmaf(w[i], v[e], sum[e]);
+                for (int h = 0; h < CHUNKS; ++h) {
+                    float v[8];
+                    values_of(raw[i][h], v);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) sum[h][e] = __builtin_fmaf(w[i], v[e], sum[h][e]);
+                }
             }
         }
     }
-    if (residual) {
-        float r[8];
-        load_upto8<STREAMING == kAll>(residual + token * p.ldr + col, n, r);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sum[e] += r[e];
+    for (int h = 0; h < CHUNKS; ++h) {
+        const int left = n - h * kScaleUnit;
+        if (left <= 0) return;
+        if (residual) {
+            float r[8];
+            load_upto8(residual + token * p.ldr + col + h * kScaleUnit, left, r);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) sum[h][e] += r[e];
+        }
+        store_upto8<NT>(y + token * p.ldy + col + h * kScaleUnit, left, sum[h]);
     }
-    store_upto8<STREAMING != kKept>(y + token * p.ldy + col, n, sum);
 }
 
-// A workgroup takes a token, its wavefronts every fourth 512 values of the row and four slots at a time; dweights are sums within a lane, within a
-// wavefront and over the wavefronts in their order.
-template <class T, bool DX, bool DW, int STREAMING>
+// W wavefronts take a token, every W-th 512 values of its row each and four slots at a time; dweights are sums within a lane, within a wavefront and over the
+// wavefronts in their order.
+template <class T, bool DX, bool DW, int W, bool NT>
 __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ x, T* __restrict__ dx, const RouteParams p) {
     __shared__ float sums[kWaves][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int64_t token = blockIdx.x, slot = token * p.per;
+    const uint32_t at = blockIdx.x * (kWaves / W) + wave / W;
+    const bool working = at < p.items;                       // (the others pass the barriers)
+    const int64_t token = working ? at : p.items - 1, slot = token * p.per;
     for (int j0 = 0; j0 < p.per; j0 += 4) {
         int64_t row[4];
         bool there[4];
@@ -123,19 +139,19 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restr
         for (int i = 0; i < 4; ++i) {
             const int j = j0 + i < p.per ? j0 + i : p.per - 1;
             row[i] = p.place[slot + j];
-            there[i] = j0 + i < p.per && row[i] >= 0 && row[i] < p.rows;
+            there[i] = working && j0 + i < p.per && row[i] >= 0 && row[i] < p.rows;
             row[i] = there[i] ? row[i] : 0;
             if constexpr (DX) w[i] = p.weights[slot + j];
         }
-        for (int chunk = wave; chunk < (int)p.chunks && p.rows > 0; chunk += kWaves) {
+        for (int chunk = wave % W; chunk < (int)p.chunks && p.rows > 0; chunk += W) {
             const int col = chunk * kScaleUnit + 8 * lane, n = p.K - col;
             Raw8<T> raw[4];
             float d[8];
-            load_upto8<STREAMING == kAll>(dy + token * p.ldr + col, n, d);
+            load_upto8(dy + token * p.ldr + col, n, d);
             if constexpr (DW) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (j0 + i < p.per) load_raw_upto8<STREAMING == kAll>(x + row[i] * p.ldx + col, n, raw[i]);
+                    if (j0 + i < p.per) load_raw_upto8<false>(x + row[i] * p.ldx + col, n, raw[i]);
             }
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
@@ -144,7 +160,7 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restr
                     float o[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) o[e] = w[i] * d[e];
-                    if (n > 0) store_upto8<STREAMING != kKept>(dx + row[i] * p.ldy + col, n, o);
+                    if (n > 0) store_upto8<NT>(dx + row[i] * p.ldy + col, n, o);
                 }
                 if constexpr (DW) {
                     float v[8];
@@ -159,17 +175,16 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restr
             for (int i = 0; i < 4; ++i) {
 #pragma unroll
                 for (int m = 1; m < 64; m <<= 1) dot[i] += __shfl_xor(dot[i], m);
-                if (lane == 0) sums[wave][i] = dot[i];
+                if (W > 1 && lane == 0) sums[wave][i] = dot[i];
             }
-            __syncthreads();
-            const int t = threadIdx.x;
-            if (t < 4 && j0 + t < p.per) {
-                float s = sums[0][t];
+            if constexpr (W > 1) __syncthreads();
+            if (working && wave % W == 0 && lane < 4 && j0 + lane < p.per) {
+                float s = lane == 0 ? dot[0] : lane == 1 ? dot[1] : lane == 2 ? dot[2] : dot[3];
 #pragma unroll
-                for (int v = 1; v < kWaves; ++v) s += sums[v][t];
-                p.dweights[slot + j0 + t] = s;
+                for (int v = 1; v < W; ++v) s += sums[wave + v][lane];
+                p.dweights[slot + j0 + lane] = s;
             }
-            __syncthreads();
+            if constexpr (W > 1) __syncthreads();
         }
     }
 }
@@ -267,14 +282,19 @@ extern "C" sparq_status sparq_mx_combine(const void* x, int64_t ldx, int64_t row
     sparq_status s = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const int64_t result = tokens * K * (int64_t)sizeof(T), slots = tokens * per, read = slots < rows ? slots : rows;
-        with_streaming<T>((residual ? 2 : 1) * result + read * K * (int64_t)sizeof(T), result, [&](auto streaming) {
-            constexpr int S = decltype(streaming)::value;
-            s = in_route_launches(tokens, p, [&](const RouteParams& q, uint32_t grid, int64_t first) {
-                combine_kernel<T, S><<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+        const auto launch = [&](auto chunks) {
+            constexpr int C = decltype(chunks)::value;
+            RouteParams all = p;
+            all.chunks = (p.chunks + C - 1) / C;
+            all.div_chunks = make_fastdiv(all.chunks);
+            s = in_route_launches(tokens, all, [&](const RouteParams& q, uint32_t grid, int64_t first) {
+                combine_kernel<T, C, kPast<T>><<<grid, kThreads, 0, static_cast<hipStream_t>(stream)>>>(
                     static_cast<const T*>(x), residual ? static_cast<const T*>(residual) + first * ldr : nullptr, static_cast<T*>(y) + first * ldy, q);
             });
-        });
+        };
+        // (more on its way at a time, where there is work for all CUs)
+        if (p.chunks > 1 && p.items >= 8192) launch(std::integral_constant<int, 2>{});
+        else launch(std::integral_constant<int, 1>{});
     });
     return s;
 }
@@ -297,20 +317,25 @@ extern "C" sparq_status sparq_mx_combine_grad(const void* dy, int64_t lddy, cons
     sparq_status s = SPARQ_OK;
     with_type(type, [&](auto t) {
         typedef decltype(t) T;
-        const int64_t row = K * (int64_t)sizeof(T), slots = tokens * per, used = slots < rows ? slots : rows;
-        with_streaming<T>(row * (tokens + used * ((dx ? 1 : 0) + (dweights ? 1 : 0))), row * used, [&](auto streaming) {
-            constexpr int S = decltype(streaming)::value;
-            const auto kernel = dx && dweights ? combine_grad_kernel<T, true, true, S> : dx ? combine_grad_kernel<T, true, false, S> : combine_grad_kernel<T, false, true, S>;
-            s = in_launches(tokens, kThreads, [&](int64_t first, int64_t n) {
+        const auto launch = [&](auto wavefronts) {
+            constexpr int W = decltype(wavefronts)::value, kTokens = kWaves / W;
+            constexpr bool NT = kPast<T>;
+            const auto kernel = dx && dweights ? combine_grad_kernel<T, true, true, W, NT> : dx ? combine_grad_kernel<T, true, false, W, NT> : combine_grad_kernel<T, false, true, W, NT>;
+            s = in_launches(tokens, kThreads / kTokens, [&](int64_t first, int64_t n) {
                 RouteParams q = p;
+                q.items = (uint32_t)n;
                 q.place += first * per;
                 if (q.weights) q.weights += first * per;
                 q.dweights = dweights ? dweights + first * per : nullptr;
-                kernel<<<(unsigned)n, kThreads, 0, static_cast<hipStream_t>(stream)>>>(static_cast<const T*>(dy) + first * lddy, static_cast<const T*>(x),
-                                                                                       static_cast<T*>(dx), q);
+                kernel<<<(unsigned)((n + kTokens - 1) / kTokens), kThreads, 0, static_cast<hipStream_t>(stream)>>>(
+                    static_cast<const T*>(dy) + first * lddy, static_cast<const T*>(x), static_cast<T*>(dx), q);
                 return launch_status();
             });
-        });
+        };
+        // (two pieces of 512 a wavefront, while there are tokens for all CUs: 8192 tokens of 1003, two rows each, four wavefronts 32 us)
+        if (p.chunks <= 2 && tokens >= 2048) launch(std::integral_constant<int, 1>{});
+        else if (p.chunks <= 4 && tokens >= 2048) launch(std::integral_constant<int, 2>{});
+        else launch(std::integral_constant<int, 4>{});
     });
     return s;
 }
