@@ -4,22 +4,33 @@
 namespace sparq {
 namespace mx {
 
-// A counting sort that keeps the order of equal keys.  A wavefront has a range of slots: it counts them by expert in LDS, and once the counts of
-// all ranges before its own are known, for each expert, it takes 64 slots at a time; a slot's rank among the lanes with the same expert is the number of
-// such lanes below, found by one ballot a bit of the expert's number.  Slots refused are those of one expert more, the last.
+// A counting sort that keeps the order of equal keys.  A wavefront has a range of slots, kAhead times 64 of them in registers at a time: it counts them by expert
+// in LDS, and once the counts of all ranges before its own are known, for each expert, it takes 64 slots at a time; a slot's rank among the lanes with the
+// same expert is the number of such lanes below, found by one ballot a bit of the expert's number.  Slots refused are those of one expert more, the last.
+// Bound by waiting: for the slots, the other workgroups' counts, and as many rounds of ballots as a range has 64s.
 struct SortParams {
     const int32_t* expert;
     int32_t *offsets, *place, *order;
     int32_t* counts;             // [workgroups][experts + 1], of more workgroups than one
-    int32_t slots, experts, range, ranges;       // slots of a wavefront (whole 64s), and all wavefronts
+    int32_t slots, experts, range;               // slots of a wavefront (whole kAhead 64s)
 };
+constexpr int kAhead = 8;
 
-template <int WAVES>
-__device__ __forceinline__ void count_own(const SortParams& p, int32_t* mine, int first, int last) {
+// Lanes' buckets of kAhead times 64 slots from s on (-1: past the end)
+__device__ __forceinline__ void buckets_of(const SortParams& p, int64_t s, int (&key)[kAhead]) {
     const int lane = threadIdx.x & 63;
-    for (int s = first + lane; s < last; s += 64) {
-        const int e = p.expert[s];
-        atomicAdd(&mine[(unsigned)e < (unsigned)p.experts ? e : p.experts], 1);
+    int e[kAhead];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) e[i] = p.expert[s + 64 * i + lane < p.slots ? s + 64 * i + lane : p.slots - 1];
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) key[i] = s + 64 * i + lane >= p.slots ? -1 : (unsigned)e[i] < (unsigned)p.experts ? e[i] : p.experts;
+}
+__device__ __forceinline__ void count_range(const SortParams& p, int64_t first, int32_t* counts, int (&key)[kAhead]) {
+    for (int64_t s = first; s < first + p.range && s < p.slots; s += 64 * kAhead) {
+        buckets_of(p, s, key);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i)
+            if (key[i] >= 0) atomicAdd(&counts[key[i]], 1);
     }
 }
 
@@ -30,8 +41,8 @@ __global__ __launch_bounds__(WAVES * 64) void sort_count_kernel(const SortParams
     const int buckets = p.experts + 1;
     for (int i = threadIdx.x; i < buckets; i += WAVES * 64) counts[i] = 0;
     __syncthreads();
-    const int64_t first = (int64_t)(blockIdx.x * WAVES + (threadIdx.x >> 6)) * p.range, last = first + p.range;
-    count_own<WAVES>(p, counts, (int)(first < p.slots ? first : p.slots), (int)(last < p.slots ? last : p.slots));
+    int key[kAhead];
+    count_range(p, (int64_t)(blockIdx.x * WAVES + (threadIdx.x >> 6)) * p.range, counts, key);
     __syncthreads();
     for (int i = threadIdx.x; i < buckets; i += WAVES * 64) p.counts[(int64_t)blockIdx.x * buckets + i] = counts[i];
 }
@@ -44,24 +55,33 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(const SortParams p) {
     int32_t *const mine = lds + wave * buckets, *const all = lds + WAVES * buckets, *const sums = all + buckets;
     for (int i = threadIdx.x; i < WAVES * buckets; i += THREADS) lds[i] = 0;
     __syncthreads();
-    const int64_t begin = (int64_t)(blockIdx.x * WAVES + wave) * p.range, end = begin + p.range;
-    const int first = (int)(begin < p.slots ? begin : p.slots), last = (int)(end < p.slots ? end : p.slots);
-    count_own<WAVES>(p, mine, first, last);
+    const int64_t first = (int64_t)(blockIdx.x * WAVES + wave) * p.range;
+    int key[kAhead];                             // of a range no longer than these, for good
+    count_range(p, first, mine, key);
     __syncthreads();
     // Counts before each wavefront, and all of them
     for (int e = threadIdx.x; e < buckets; e += THREADS) {
-        int before = 0;
-        if constexpr (MANY)
-            for (int b = 0; b < (int)blockIdx.x; ++b) before += p.counts[(int64_t)b * buckets + e];
+        int before = 0, total = 0;
+        if constexpr (MANY) {
+            // (32 workgroups' counts on their way at a time)
+            for (int b0 = 0; b0 < (int)gridDim.x; b0 += 32) {
+                int n[32];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) n[i] = p.counts[(int64_t)(b0 + i < (int)gridDim.x ? b0 + i : 0) * buckets + e];
+#pragma unroll
+                for (int i = 0; i < 32; ++i) {
+                    if (b0 + i < (int)gridDim.x) total += n[i];
+                    if (b0 + i < (int)blockIdx.x) before += n[i];
+                }
+            }
+        }
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const int n = lds[w * buckets + e];
             lds[w * buckets + e] = before;
             before += n;
         }
-        if constexpr (MANY)
-            for (int b = blockIdx.x + 1; b < (int)gridDim.x; ++b) before += p.counts[(int64_t)b * buckets + e];
-        all[e] = before;
+        all[e] = MANY ? total : before;
     }
     __syncthreads();
     // The experts' first rows: sums of the counts below, THREADS experts at a time
@@ -92,43 +112,64 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(const SortParams p) {
         __syncthreads();
     }
     const int bits = 32 - __builtin_clz(p.experts);
-    for (int s0 = first; s0 < last; s0 += 64) {
-        const int s = s0 + lane, e = s < last ? p.expert[s] : -1, key = (unsigned)e < (unsigned)p.experts ? e : p.experts;
-        uint64_t same = __ballot(s < last);
-        for (int b = 0; b < bits; ++b) {
-            const uint64_t set = __ballot(key >> b & 1);
-            same &= key >> b & 1 ? set : ~set;
+    for (int64_t s0 = first; s0 < first + p.range && s0 < p.slots; s0 += 64 * kAhead) {
+        if (p.range > 64 * kAhead) buckets_of(p, s0, key);
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) {
+            if (s0 + 64 * i >= p.slots) break;
+            const int64_t s = s0 + 64 * i + lane;
+            const bool there = key[i] >= 0;
+            uint64_t same = __ballot(there);
+            for (int b = 0; b < bits; ++b) {
+                const uint64_t set = __ballot(key[i] >> b & 1);
+                same &= key[i] >> b & 1 ? set : ~set;
+            }
+            const int rank = __popcll(same & ((1ull << lane) - 1));
+            if (there) {
+                const int row = mine[key[i]] + rank;
+                p.place[s] = key[i] < p.experts ? row : -1;
+                if (p.order) p.order[row] = key[i] < p.experts ? (int)s : -1;
+            }
+            wavefront_lds_fence();
+            if (there && rank == 0) mine[key[i]] += __popcll(same);
+            wavefront_lds_fence();
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        if (s < last) {
-            const int row = mine[key] + rank;
-            p.place[s] = key < p.experts ? row : -1;
-            if (p.order) p.order[row] = key < p.experts ? s : -1;
-        }
-        wavefront_lds_fence();
-        if (s < last && rank == 0) mine[key] += __popcll(same);
-        wavefront_lds_fence();
     }
 }
 
-constexpr int kSortWaves = 8;
-// One workgroup up to this many slots; more take two launches, the first of which counts.
+// One workgroup while its sixteen wavefronts hold all slots; more take two launches, the first of which counts: as few slots a workgroup as leave no more than
+// 256 of them, whose counts each adds up.
 struct SortPlan {
     int waves, range, blocks;
     size_t bytes;
 };
 static SortPlan sort_plan(int64_t slots, int experts) {
     SortPlan p = {};
-    p.waves = slots <= 128 ? 1 : kSortWaves;
-    const int64_t wanted = slots <= 8192 ? p.waves : (slots + 511) / 512;
-    const int64_t ranges = wanted < 1024 ? wanted : 1024;
-    p.range = (int)round_up((slots + ranges - 1) / ranges, 64);
+    constexpr int least = 64 * kAhead;
+    const int most = experts <= 512 ? 16 : 8;                // (LDS)
+    p.waves = slots <= 256 ? 1 : slots <= least * most ? most : 8;
+    const int64_t ranges = (slots + least - 1) / least;
+    p.range = p.waves == 8 && ranges > 8 * 256 ? (int)round_up((slots + 8 * 256 - 1) / (8 * 256), least) : least;
     p.blocks = slots == 0 ? 1 : (int)((slots + (int64_t)p.range * p.waves - 1) / ((int64_t)p.range * p.waves));
     p.bytes = p.blocks > 1 ? (size_t)round_up((int64_t)p.blocks * (experts + 1) * 4, 256) : 0;
     return p;
 }
 static bool sort_sizes_ok(int64_t slots, int experts) { return slots >= 0 && experts >= 1; }
 static bool sort_countable(int64_t slots, int experts) { return slots <= 1 << 30 && experts <= SPARQ_MX_EXPERTS_MOST; }
+
+template <int WAVES>
+static sparq_status launch_sort(const SortParams& p, int blocks, hipStream_t stream) {
+    const int buckets = p.experts + 1, lds_bytes = ((WAVES + 1) * buckets + WAVES) * 4;
+    if (blocks == 1) {
+        sort_kernel<WAVES, false><<<1, WAVES * 64, lds_bytes, stream>>>(p);
+        return launch_status();
+    }
+    sort_count_kernel<WAVES><<<blocks, WAVES * 64, buckets * 4, stream>>>(p);
+    const sparq_status counted = launch_status();
+    if (counted != SPARQ_OK) return counted;
+    sort_kernel<WAVES, true><<<blocks, WAVES * 64, lds_bytes, stream>>>(p);
+    return launch_status();
+}
 
 }  // namespace mx
 }  // namespace sparq
@@ -149,21 +190,7 @@ extern "C" sparq_status sparq_mx_sort(const int32_t* expert, int64_t slots, int3
     const SortPlan plan = sort_plan(slots, experts);
     if (plan.bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < plan.bytes) return SPARQ_EWORKSPACE;
-    const SortParams p = {expert, offsets, place, order, static_cast<int32_t*>(workspace), (int32_t)slots, experts, plan.range, 0};
+    const SortParams p = {expert, offsets, place, order, static_cast<int32_t*>(workspace), (int32_t)slots, experts, plan.range};
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const int buckets = experts + 1;
-    if (plan.waves == 1) {
-        sort_kernel<1, false><<<1, 64, (2 * buckets + 1) * 4, s>>>(p);
-        return launch_status();
-    }
-    const int lds_bytes = ((kSortWaves + 1) * buckets + kSortWaves) * 4;
-    if (plan.blocks == 1) {
-        sort_kernel<kSortWaves, false><<<1, kSortWaves * 64, lds_bytes, s>>>(p);
-        return launch_status();
-    }
-    sort_count_kernel<kSortWaves><<<plan.blocks, kSortWaves * 64, buckets * 4, s>>>(p);
-    const sparq_status counted = launch_status();
-    if (counted != SPARQ_OK) return counted;
-    sort_kernel<kSortWaves, true><<<plan.blocks, kSortWaves * 64, lds_bytes, s>>>(p);
-    return launch_status();
+    return plan.waves == 1 ? launch_sort<1>(p, plan.blocks, s) : plan.waves == 8 ? launch_sort<8>(p, plan.blocks, s) : launch_sort<16>(p, plan.blocks, s);
 }
