@@ -1,5 +1,6 @@
 // The experts' products and a layer with an epilogue: entry points, the choice of kernels, tiles of rows (include/sparq_mx_experts.h).
 #include "sparq_mx_experts_gemm.h"
+#include <math.h>
 
 namespace sparq {
 namespace mx {
@@ -64,7 +65,8 @@ struct ExpertsPlan {
     int tile;                // 256, 128 or 64: results a workgroup makes along either side; 0: few rows, 16 `fragments` of them a workgroup
     int fragments;
     int parts;               // of the reduction (one expert without offsets alone)
-    int64_t pieces;          // few rows: workgroups along them
+    int64_t pieces;          // few rows: as many as any division of the rows can make
+    int blocks;              // ... and blocks of 16 columns a workgroup makes
     size_t table_bytes, partial_bytes;
 };
 // What a round of tiles takes (us): one of 256 x 256 a CU, or two of 128 x 128, by the length of the reduction and what comes behind it.  One wavefront a SIMD
@@ -80,9 +82,15 @@ static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
     p.parts = 1;
     // What an expert has of the rows on average; how they are divided is not known here.
     const int64_t each = (M + experts - 1) / experts;
-    if (!kept && (each <= 16 || (each <= kFewMost && each * N * K <= 5ll << 27))) {
+    if (!kept && (each <= 16 || (each <= 64 && each * N * K <= 5ll << 27))) {
         p.fragments = (int)((each + 15) / 16);
         p.pieces = offsets ? most_tiles(M, experts, 16 * p.fragments) : 1;
+        // Two workgroups of eight wavefronts a CU, or three of four, by the number of pieces to be expected of rows that go to any expert alike (us, by blocks a
+        // workgroup makes: 16 rows, 16 experts of 2048 x 4096: one 16.7, two 15.8, three 13.9, four 14.8, six 14.5; 64 rows, the same: 27, 21, 23, 17.8, 21).
+        const double part = offsets ? (double)M / (16 * p.fragments) - 0.5 * experts : 0.0;
+        const double expected = offsets ? experts * (1.0 - pow(1.0 - 1.0 / experts, (double)M)) + (part > 0.0 ? part : 0.0) : 1.0;
+        const double wanted = expected * ((N + kFewColumns - 1ll) / kFewColumns) / (K <= 4 * kScaleUnit ? 690 : 460);
+        p.blocks = wanted < 1.5 ? 1 : wanted > 8.0 ? 8 : (int)(wanted + 0.5);
         return p;
     }
     // (of experts' rows about half of an expert's last tile is empty)
@@ -137,12 +145,24 @@ static sparq_status launch_tiles_of(const ExpertGemmParams& p, int tile, void* y
 static sparq_status product(const Call& c, const ExpertsPlan& plan, void* workspace, hipStream_t stream) {
     if (plan.tile == 0) {
         ExpertFewParams f = {};
-        static_cast<FewParams&>(f) = {c.x, static_cast<const uint8_t*>(c.a), static_cast<const uint8_t*>(c.as), static_cast<const uint8_t*>(c.w),
-                                      static_cast<const uint8_t*>(c.ws), c.bias, c.ldx, c.ldy, code_pitch(c.K, 4), scale_pitch(c.K), (int)c.M, c.N, c.K,
-                                      (c.K + kScaleUnit - 1) / kScaleUnit, (c.K + kCodeUnit - 1) / kCodeUnit - 1};
+        f.x = c.x;
+        f.a = static_cast<const uint8_t*>(c.a);
+        f.as = static_cast<const uint8_t*>(c.as);
+        f.w = static_cast<const uint8_t*>(c.w);
+        f.ws = static_cast<const uint8_t*>(c.ws);
+        f.bias = c.bias;
         f.offsets = c.offsets;
-        f.rows = c.M;
+        f.ldx = c.ldx;
+        f.ldy = c.ldy;
+        f.code_pitch = code_pitch(c.K, 4);
+        f.scale_pitch = scale_pitch(c.K);
+        f.M = c.M;
+        f.N = c.N;
+        f.K = c.K;
+        f.groups = (c.K + kScaleUnit - 1) / kScaleUnit;
+        f.last_step = (c.K + kCodeUnit - 1) / kCodeUnit - 1;
         f.experts = c.experts;
+        f.blocks = plan.blocks;
         f.epilogue = c.epilogue;
         return (c.type == SPARQ_MX_F32 ? launch_experts_few_f32 : c.type == SPARQ_MX_F16 ? launch_experts_few_f16 : launch_experts_few_bf16)(
             f, c.x_type, plan.fragments, plan.pieces, c.y, stream);
@@ -190,7 +210,7 @@ static sparq_status product(const Call& c, const ExpertsPlan& plan, void* worksp
 // As many tiles, with their parts, as the kernels count
 static bool countable(const ExpertsPlan& p, int64_t M, int64_t N, int experts) {
     if (M >= 1ll << 31 || experts > SPARQ_MX_EXPERTS_MOST || (int64_t)experts * N >= 1ll << 31) return false;
-    if (p.tile == 0) return p.pieces < 65536 && (N + kFewRows - 1) / kFewRows < 1ll << 22;
+    if (p.tile == 0) return p.pieces < 65536 && (N + kFewColumns - 1) / kFewColumns < 1ll << 22;
     const int t = p.tile;
     return (M / t + 1 + experts) * ((N + t - 1) / t) * p.parts < (1ll << 31);
 }
@@ -208,11 +228,9 @@ static Epilogue epilogue_of(int function, const void* residual, int64_t ldr, voi
             (int)round_up(N, kCodeUnit)};
 }
 
-// Whether the product quantises its rows itself
-static bool quantised_on_the_way(const ExpertsPlan& plan, int64_t M, int N, int K, int experts) {
-    const int64_t each = (M + experts - 1) / experts;
-    return plan.tile == 0 && plan.fragments == 1 && each * N * K <= 1 << 27;
-}
+// Whether the product quantises its rows itself, each wavefront the group that it multiplies, once a workgroup: what that saves is a launch (us, itself -> before it,
+// 16 experts of 2048 x 4096, 16 rows 13.9 -> 16.2, 64 rows 17.8 -> 19.4; 128 rows among 8 of 4096 x 2048, 16 each, 14.2 -> 14.4).
+static bool quantised_on_the_way(const ExpertsPlan& plan, int K) { return plan.tile == 0 && plan.fragments == 1 && K <= 8 * kScaleUnit; }
 static size_t coded_bytes(int64_t M, int K) { return (size_t)(round_up(M * code_pitch(K, 4), 256) + round_up(M * scale_pitch(K), 256)); }
 
 }  // namespace mx
@@ -261,7 +279,7 @@ extern "C" sparq_status sparq_mx_experts_linear(const void* x, int32_t x_type, i
     if (!tensor_ok(y, y_type, ldy, N) || !extent_ok(M, ldy) || !extent_ok(M, K) || !epilogue_ok(function, residual, ldr, y_type, kept_codes, kept_scales, M, N))
         return SPARQ_EINVAL;
     const ExpertsPlan plan = experts_plan(M, N, K, experts, offsets != nullptr, function, residual != nullptr, kept_codes != nullptr);
-    const bool on_the_way = quantised_on_the_way(plan, M, N, K, experts);
+    const bool on_the_way = quantised_on_the_way(plan, K);
     const size_t coded = on_the_way ? 0 : coded_bytes(M, K), bytes = coded + plan.table_bytes + plan.partial_bytes;
     if (bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < bytes) return SPARQ_EWORKSPACE;

@@ -1,7 +1,7 @@
-// The experts' products: the kernels of sparq_mx_gemm_kernel.h and sparq_mx_few_kernel.h with rows of several experts and an epilogue.
+// The experts' products: the kernel of sparq_mx_gemm_kernel.h with rows of several experts and an epilogue, and the one for few rows.
 #pragma once
 #include "sparq_mx_epilogue.h"
-#include "sparq_mx_few.h"
+#include "sparq_mx_experts_few_kernel.h"
 #include "sparq_mx_gemm_kernel.h"
 #include "sparq_mx_tiles.h"
 
@@ -16,44 +16,6 @@ struct ExpertGemmParams : GemmParams {
 template <int F>
 struct ExpertGemmParamsOf : ExpertGemmParams {
     static constexpr int kFunction = F;
-};
-
-struct ExpertFewParams : FewParams {
-    const int32_t* offsets;              // NULL: one expert, all rows (M)
-    int64_t rows;
-    int32_t experts;
-    Epilogue epilogue;
-
-#if defined(__HIPCC__)
-    // The rows of piece `index` of the pieces of at most `most` rows that the experts' rows are divided into; false: there are fewer.  A lane an expert.
-    __device__ __forceinline__ bool find(int most, uint32_t index, int& row0, int& count, int& expert) const {
-        const int lane = threadIdx.x & 63;
-        uint32_t before = 0;
-        for (int e0 = 0; e0 < experts; e0 += 64) {
-            int first = 0, n = 0;
-            if (e0 + lane < experts) expert_rows(offsets, e0 + lane, rows, first, n);
-            const uint32_t pieces = (uint32_t)(n + most - 1) / (uint32_t)most;
-            uint32_t sum = pieces;
-#pragma unroll
-            for (int d = 1; d < 64; d <<= 1) {
-                const uint32_t v = __shfl_up(sum, d);
-                if (lane >= d) sum += v;
-            }
-            const uint64_t past = __ballot(before + sum > index);
-            if (past) {
-                const int at = __builtin_ctzll(past);
-                const int in = (int)(index - before - (uint32_t)__builtin_amdgcn_readlane((int)(sum - pieces), at)) * most;
-                row0 = __builtin_amdgcn_readlane(first, at) + in;
-                count = __builtin_amdgcn_readlane(n, at) - in;
-                count = count < most ? count : most;
-                expert = e0 + at;
-                return true;
-            }
-            before += (uint32_t)__builtin_amdgcn_readlane((int)sum, 63);
-        }
-        return false;
-    }
-#endif
 };
 
 // Implemented in sparq_mx_experts_{gemm,few}_{f32,f16,bf16}.hip, by the results' type.
@@ -91,16 +53,19 @@ sparq_status launch_experts_tiles(const ExpertGemmParams& p, int tile, void* y, 
     return tile == 256 ? launch_experts_tile<O, 256>(p, y, stream) : tile == 128 ? launch_experts_tile<O, 128>(p, y, stream) : launch_experts_tile<O, 64>(p, y, stream);
 }
 
-template <class O, class X, int MT, int WAVES>
+template <class O, class X, int MT, int WAVES, bool SINGLE>
 sparq_status launch_experts_few_kernel(const ExpertFewParams& p, int64_t pieces, void* y, hipStream_t stream) {
-    const int rows = p.offsets ? 16 * MT : p.M;
-    few_rows_kernel<O, X, MT, WAVES, ExpertFewParams><<<dim3((unsigned)((p.N + kFewRows - 1ll) / kFewRows), (unsigned)pieces), WAVES * 64,
-                                                        few_lds_bytes<WAVES, MT>(rows, p.x != nullptr), stream>>>(static_cast<O*>(y), p);
+    const int rows = p.offsets ? 16 * MT : (int)p.M, blocks = (p.N + kFewColumns - 1) / kFewColumns;
+    experts_few_kernel<O, X, MT, WAVES, SINGLE><<<dim3((unsigned)((blocks + p.blocks - 1) / p.blocks), (unsigned)pieces), WAVES * 64,
+                                                  experts_few_lds_bytes<WAVES, MT>(rows, p.x != nullptr), stream>>>(static_cast<O*>(y), p);
     return launch_status();
 }
 template <class O, class X, int MT>
 sparq_status launch_experts_waves(const ExpertFewParams& p, int64_t pieces, void* y, hipStream_t stream) {
-    return p.groups <= 4 ? launch_experts_few_kernel<O, X, MT, 4>(p, pieces, y, stream) : launch_experts_few_kernel<O, X, MT, 8>(p, pieces, y, stream);
+    if (p.groups <= 4) return launch_experts_few_kernel<O, X, MT, 4, true>(p, pieces, y, stream);
+    if (p.groups <= 8) return launch_experts_few_kernel<O, X, MT, 8, true>(p, pieces, y, stream);
+    if constexpr (std::is_void_v<X>) return launch_experts_few_kernel<O, X, MT, 8, false>(p, pieces, y, stream);
+    return SPARQ_EINVAL;                                     // (nobody asks for it: sparq_mx_experts.hip)
 }
 // fragments: of 16 rows a workgroup takes
 template <class O>

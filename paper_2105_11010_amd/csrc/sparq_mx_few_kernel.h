@@ -30,18 +30,13 @@ constexpr int kFewRows = 16;             // of W and of A an instruction takes
 constexpr int kGroupRow = 256 + 16;      // bytes of a group of a row in LDS, and what keeps rows out of each other's banks
 constexpr int kFewQuantised = kGroupRow + 16;       // with its scales
 
-// P: FewParams, or what sparq_mx_experts_gemm.h makes of it -- rows of several experts, a workgroup's of one, and an epilogue of its own.
-template <class O, class X, int MT, int WAVES, class P = FewParams>
-__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y, const P p) {
-    constexpr bool kQuantise = !std::is_void_v<X>, kExperts = !std::is_same_v<P, FewParams>;
-    int M = p.M, row0 = 0, expert = 0;
-    if constexpr (kExperts)
-        if (p.offsets && !p.find(16 * MT, blockIdx.y, row0, M, expert)) return;
+template <class O, class X, int MT, int WAVES>
+__global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y, const FewParams p) {
+    constexpr bool kQuantise = !std::is_void_v<X>;
     extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), r = lane & 15, g = lane >> 4;
     const int n0 = blockIdx.x * kFewRows, nw = n0 + r < p.N ? n0 + r : p.N - 1;
-    const int64_t w_row = (kExperts ? (int64_t)expert * p.N : 0) + nw;
-    const uint8_t *w = p.w + w_row * p.code_pitch + 16 * g, *ws = p.ws + w_row * p.scale_pitch;
+    const uint8_t *w = p.w + nw * p.code_pitch + 16 * g, *ws = p.ws + nw * p.scale_pitch;
 
     struct Group {
         v4i w[4], a[kQuantise ? 1 : MT][4];
@@ -56,8 +51,8 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
             if constexpr (!kQuantise) {
 #pragma unroll
                 for (int i = 0; i < MT; ++i) {
-                    const int m = 16 * i + r < M ? 16 * i + r : M - 1;
-                    o.a[i][s] = *reinterpret_cast<const v4i*>(p.a + (row0 + m) * p.code_pitch + 16 * g + (int64_t)step * 64);
+                    const int m = 16 * i + r < p.M ? 16 * i + r : p.M - 1;
+                    o.a[i][s] = *reinterpret_cast<const v4i*>(p.a + m * p.code_pitch + 16 * g + (int64_t)step * 64);
                 }
             }
         }
@@ -65,16 +60,16 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
         if constexpr (!kQuantise) {
 #pragma unroll
             for (int i = 0; i < MT; ++i) {
-                const int m = 16 * i + r < M ? 16 * i + r : M - 1;
-                o.as[i] = *reinterpret_cast<const v4u*>(p.as + (row0 + m) * p.scale_pitch + (int64_t)group * 16);
+                const int m = 16 * i + r < p.M ? 16 * i + r : p.M - 1;
+                o.as[i] = *reinterpret_cast<const v4u*>(p.as + m * p.scale_pitch + (int64_t)group * 16);
             }
         }
     };
     v4f acc[MT];
 #pragma unroll
     for (int i = 0; i < MT; ++i) acc[i] = v4f{};
-    uint8_t* const mine = lds + wave * M * kFewQuantised;  // the wavefront's quantised rows
-    const int ma = r < M ? r : 0;                          // (rows past the last one make results that are not stored)
+    uint8_t* const mine = lds + wave * p.M * kFewQuantised;  // the wavefront's quantised rows
+    const int ma = r < p.M ? r : 0;                          // (rows past the last one make results that are not stored)
 
     Group held;
     fetch(held, wave);
@@ -84,21 +79,21 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
             // (Four rows' loads at once, none in a branch that would have one wait for another: lanes past a row's whole runs read its first.)
             const int col = group * kScaleUnit + 8 * lane, n = p.K - col;
             const X* const x = static_cast<const X*>(p.x);
-            for (int m0 = 0; m0 < M; m0 += 4) {
+            for (int m0 = 0; m0 < p.M; m0 += 4) {
                 float v[4][8];
                 const X* row[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) row[i] = x + (row0 + (m0 + i < M ? m0 + i : M - 1)) * p.ldx;
+                for (int i = 0; i < 4; ++i) row[i] = x + (m0 + i < p.M ? m0 + i : p.M - 1) * p.ldx;
                 if (p.K >= 8) {
                     Raw8<X> raw[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         raw[i] = Raw8<X>{};
-                        if (m0 + i < M) load_raw<false>(row[i] + (n >= 8 ? col : 0), raw[i]);
+                        if (m0 + i < p.M) load_raw<false>(row[i] + (n >= 8 ? col : 0), raw[i]);
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        if (m0 + i >= M) break;
+                        if (m0 + i >= p.M) break;
                         values_of(raw[i], v[i]);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) v[i][e] = n >= 8 ? v[i][e] : 0.0f;
@@ -122,7 +117,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    if (m0 + i >= M) break;
+                    if (m0 + i >= p.M) break;
                     const uint32_t byte = scale4_of(block_top(v[i]));
                     uint8_t* to = mine + (m0 + i) * kFewQuantised;
                     *reinterpret_cast<uint32_t*>(to + 4 * lane) = codes4_of(v[i], byte);
@@ -163,15 +158,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(O* __restrict__ y,
         float s = 0.0f;
 #pragma unroll
         for (int k = 0; k < WAVES; ++k) s += reinterpret_cast<const float*>(sums)[((k * MT + i) * 64 + from) * 4 + e];
-        if constexpr (kExperts) {
-            if (m < M && n < p.N) {
-                s = p.epilogue.template apply<O>(s + (p.bias ? p.bias[(int64_t)expert * p.N + n] : 0.0f));
-                const int64_t row = row0 + m;
-                y[row * p.ldy + n] = (O)(p.epilogue.residual ? s + (float)static_cast<const O*>(p.epilogue.residual)[row * p.epilogue.ldr + n] : s);
-            }
-        } else if (m < M && n < p.N) {
-            y[m * p.ldy + n] = (O)(s + (p.bias ? p.bias[n] : 0.0f));
-        }
+        if (m < p.M && n < p.N) y[m * p.ldy + n] = (O)(s + (p.bias ? p.bias[n] : 0.0f));
     }
 }
 
