@@ -82,7 +82,9 @@ static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
     p.parts = 1;
     // What an expert has of the rows on average; how they are divided is not known here.
     const int64_t each = (M + experts - 1) / experts;
-    if (!kept && (each <= 16 || (each <= 64 && each * N * K <= 5ll << 27))) {
+    // (us, a gemm, this kernel -> tiles: 8 experts of 2048 x 4096 with 8 rows each 10.4 -> 12.3, 16 13.0 -> 12.5, 32 17.8 -> 12.7; 64 of 1024 x 1024 11.0 -> 14.9,
+    // 13.2 -> 15.2, 18.8 -> 16.4; one expert: as the product without an epilogue, sparq_mx_gemm.hip)
+    if (!kept && (offsets ? each <= 12 : each <= 16 || (each <= 64 && each * N * K <= 5ll << 27))) {
         p.fragments = (int)((each + 15) / 16);
         p.pieces = offsets ? most_tiles(M, experts, 16 * p.fragments) : 1;
         // Two workgroups of eight wavefronts a CU, or three of four, by the number of pieces to be expected of rows that go to any expert alike (us, by blocks a
@@ -94,12 +96,15 @@ static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
         return p;
     }
     // (of experts' rows about half of an expert's last tile is empty)
-    const auto tiles = [&](int t) { return (offsets ? M / t + (experts + 1) / 2 : (M + t - 1) / t) * ((N + t - 1) / t); };
+    const auto tiles_m = [&](int t) { return !offsets ? (M + t - 1) / t : M / t + (experts + 1) / 2 > experts ? M / t + (experts + 1) / 2 : (int64_t)experts; };
+    const auto tiles = [&](int t) { return tiles_m(t) * ((N + t - 1) / t); };
     const int64_t rounds256 = (tiles(256) + 255) / 256, rounds128 = (tiles(128) + 511) / 512;
+    // (experts of a few hundred rows leave much of their tiles of 256 empty: 16 of 4096 x 2048 with 96 rows each 36 us, in tiles of 128 31)
     if (tiles(128) < 112) p.tile = 64;
+    else if (offsets && each < 512) p.tile = 128;
     else p.tile = rounds256 * round_of(256, K, function, residual, kept) < rounds128 * round_of(128, K, function, residual, kept) ? 256 : 128;
     if (offsets) {
-        p.table_bytes = table_bytes(M, experts);
+        p.table_bytes = p.tile == 256 || experts > kExpertsOfLanes ? table_bytes(M, experts) : 0;
         return p;
     }
     const int64_t n = ((M + p.tile - 1) / p.tile) * ((N + p.tile - 1) / p.tile), steps = (K + kCodeUnit - 1) / kCodeUnit, most = steps / 16;
@@ -190,7 +195,9 @@ static sparq_status product(const Call& c, const ExpertsPlan& plan, void* worksp
     p.items = (uint32_t)(tiles_m * tiles_n * parts);
     if (parted) p.epilogue.function = SPARQ_MX_NONE;
     else p.epilogue = c.epilogue;
-    if (c.offsets) {
+    p.offsets = c.offsets;
+    p.experts = c.experts;
+    if (plan.table_bytes) {
         p.table = static_cast<const ExpertTile*>(workspace);
         const sparq_status s = launch_tiles(c.offsets, c.experts, c.M, t, workspace, stream);
         if (s != SPARQ_OK) return s;

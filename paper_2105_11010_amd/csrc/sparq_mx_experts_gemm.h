@@ -9,7 +9,9 @@ namespace sparq {
 namespace mx {
 
 struct ExpertGemmParams : GemmParams {
-    const ExpertTile* table;             // NULL: one expert, all rows
+    const ExpertTile* table;             // of the rows' tiles, or NULL and the offsets (at most 64 experts and tiles of 128), or both NULL: one expert, all rows
+    const int32_t* offsets;
+    int32_t experts;
     Epilogue epilogue;
 };
 // ... of one function: a kernel each, or a tile's end would hold all of them

@@ -6,39 +6,41 @@ namespace sparq {
 namespace mx {
 
 struct ExpertGradParams : GradParams {
-    const ExpertTile* table;             // dx: tiles of rows
-    const int32_t* offsets;              // dw
+    const ExpertTile* table;             // dx: tiles of rows (NULL: by the offsets, at most 64 experts)
+    const int32_t* offsets;
+    int32_t experts;
     int64_t rows;                        // of dy and of X or dx
     int32_t margin;                      // dw: an expert's last rows that are not read in whole runs
 
 #if defined(__HIP_DEVICE_COMPILE__)
-    // What is the workgroup's own of the call: its expert's rows (dw), the number of tiles (dx).  false: there is nothing for it.
-    template <class T, bool DW>
-    __device__ __forceinline__ bool own(GradParams& p) const {
-        if constexpr (DW) {
-            const int expert = blockIdx.y;
-            ConstantInt* const at = (ConstantInt*)(offsets + expert);
-            const int most = (int)rows, a = at[0], b = at[1], first = a < 0 ? 0 : a > most ? most : a, end = b > most ? most : b;
-            p.R = end > first ? end - first : 0;
-            p.dy = static_cast<const T*>(dy) + first * lddy;
-            p.codes = codes + first * code_pitch;
-            p.scales = scales + first * scale_pitch;
-            p.steps_per_part = (int)((p.R + kGradStep - 1) / kGradStep);
-            const int64_t whole = p.R - margin;
-            p.s_whole = whole > 0 && s_whole > 0 ? whole / kGradStep : 0;
-            return true;
-        } else {
-            p.tiles_j = tile_count(table);
-            return blockIdx.x < (uint32_t)p.tiles_j * (uint32_t)tiles_k;
-        }
+    // dw: what is the workgroup's own of the call, its expert's rows.
+    template <class T>
+    __device__ __forceinline__ void own_rows(GradParams& p) const {
+        ConstantInt* const at = (ConstantInt*)(offsets + blockIdx.y);
+        const int most = (int)rows, a = at[0], b = at[1], first = a < 0 ? 0 : a > most ? most : a, end = b > most ? most : b;
+        p.R = end > first ? end - first : 0;
+        p.dy = static_cast<const T*>(dy) + first * lddy;
+        p.codes = codes + first * code_pitch;
+        p.scales = scales + first * scale_pitch;
+        p.steps_per_part = (int)((p.R + kGradStep - 1) / kGradStep);
+        const int64_t whole = p.R - margin;
+        p.s_whole = whole > 0 && s_whole > 0 ? whole / kGradStep : 0;
     }
-    // dx: the first row of tile tj; p's rows end with the tile's.
-    __device__ __forceinline__ int64_t rows_of(GradParams& p, uint32_t tj) const {
-        const ExpertTile t = expert_tile(table, tj);
+    // dx: the workgroup's tile, its first row and column (in tiles); false: there are fewer tiles.
+    template <int TILE>
+    __device__ __forceinline__ bool own_tile(GradParams& p, int64_t& j0, uint32_t& tk) const {
+        LaneTiles lanes = {};
+        if (!table) lanes = tiles_of_lanes(offsets, experts, rows, TILE);
+        const uint32_t tiles = (uint32_t)(table ? tile_count(table) : tile_count(lanes));
+        if (blockIdx.x >= tiles * (uint32_t)tiles_k) return false;
+        uint32_t tj;
+        tile_of(blockIdx.x, tiles, tiles_k, tj, tk);
+        const ExpertTile t = table ? expert_tile(table, tj) : expert_tile(lanes, TILE, tj);
+        j0 = t.row;
         p.J = t.row + t.rows;
         p.codes = codes + (int64_t)t.expert * R * code_pitch;
         p.scales = scales + (int64_t)t.expert * R * scale_pitch;
-        return t.row;
+        return true;
     }
 #endif
 };

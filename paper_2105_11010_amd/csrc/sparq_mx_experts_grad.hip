@@ -29,6 +29,7 @@ static int dw_tile(int dy_type, int64_t M, int N, int K, int experts) {
     const auto tiles = [&](int64_t t) { return experts * ((N + t - 1) / t) * ((K + t - 1) / t); };
     return grad_tile(dy_type, tiles(256), tiles(128), (M / experts + kGradStep - 1) / kGradStep, true);
 }
+static size_t dx_bytes(int64_t M, int experts) { return experts > kExpertsOfLanes ? table_bytes(M, experts) : 0; }
 static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K, int64_t experts) {
     return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40) && experts_ok((int)experts);
 }
@@ -63,7 +64,7 @@ using namespace sparq;
 using namespace sparq::mx;
 
 extern "C" size_t sparq_mx_experts_dx_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t experts) {
-    return grad_sizes_ok(M, N, K, experts) && M > 0 ? table_bytes(M, experts) : 0;
+    return grad_sizes_ok(M, N, K, experts) && M > 0 ? dx_bytes(M, experts) : 0;
 }
 extern "C" size_t sparq_mx_experts_dw_workspace_bytes(int64_t M, int32_t N, int32_t K, int32_t experts) {
     (void)M, (void)N, (void)K, (void)experts;
@@ -78,16 +79,20 @@ extern "C" sparq_status sparq_mx_experts_dx(const void* dy, int32_t dy_type, int
     if (M == 0) return SPARQ_OK;
     if (!coded_ok(w_codes, w_scales) || !tensor_ok(dy, dy_type, lddy, N) || !tensor_ok(dx, dx_type, lddx, K)) return SPARQ_EINVAL;
     if (!extent_ok(M, lddy) || !extent_ok(M, lddx) || !extent_ok(M, K)) return SPARQ_EINVAL;
-    if (!workspace || !aligned(workspace, 256)) return SPARQ_EINVAL;
-    if (workspace_bytes < table_bytes(M, experts)) return SPARQ_EWORKSPACE;
+    const size_t bytes = dx_bytes(M, experts);
+    if (bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
+    if (workspace_bytes < bytes) return SPARQ_EWORKSPACE;
     const int t = dx_tile(dy_type, M, K, experts);
     const int64_t tiles_j = most_tiles(M, experts, t), tiles_k = (K + t - 1) / t;
     if (!grad_countable(M, N, experts) || tiles_j * tiles_k * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
     const hipStream_t s = static_cast<hipStream_t>(stream);
-    const sparq_status tiled = launch_tiles(offsets, experts, M, t, workspace, s);
-    if (tiled != SPARQ_OK) return tiled;
+    if (bytes) {
+        const sparq_status tiled = launch_tiles(offsets, experts, M, t, workspace, s);
+        if (tiled != SPARQ_OK) return tiled;
+    }
     ExpertGradParams p = grad_params(dy, lddy, w_codes, w_scales, 4, lddx, M, N, K, offsets, M);
-    p.table = static_cast<const ExpertTile*>(workspace);
+    p.table = bytes ? static_cast<const ExpertTile*>(workspace) : nullptr;
+    p.experts = experts;
     p.tiles_k = (int)tiles_k;
     p.s_whole = reads_fit(lddy, p.code_pitch) ? N / kGradStep : 0;
     p.steps_per_part = (N + kGradStep - 1) / kGradStep;

@@ -61,9 +61,16 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
     };
     constexpr bool kExperts = !std::is_same_v<P, GemmParams>;
     uint32_t items = p.items, tiles_m = p.tiles_m;
+    constexpr bool kLanes = kExperts && TM <= 128;           // (256 x 256 results leave no registers: a table)
+    std::conditional_t<kLanes, LaneTiles, char> lane_tiles = {};
     if constexpr (kExperts)
-        if (p.table) {
-            tiles_m = (uint32_t)tile_count(p.table);
+        if ((kLanes ? p.offsets != nullptr : p.table != nullptr)) {
+            if constexpr (kLanes) {
+                if (!p.table) lane_tiles = tiles_of_lanes(p.offsets, p.experts, p.M, TM);
+                tiles_m = (uint32_t)(p.table ? tile_count(p.table) : tile_count(lane_tiles));
+            } else {
+                tiles_m = (uint32_t)tile_count(p.table);
+            }
             items = tiles_m * p.tiles_n;
             if (blockIdx.x >= items) return;
         }
@@ -72,9 +79,11 @@ __global__ __launch_bounds__(kGemmThreads) void gemm_kernel(O* __restrict__ y, c
         uint32_t tm, tn;
         it.expert = 0;
         if constexpr (kExperts)
-            if (p.table) {
+            if ((kLanes ? p.offsets != nullptr : p.table != nullptr)) {
                 tile_of(id, tiles_m, p.tiles_n, tm, tn);
-                const ExpertTile t = expert_tile(p.table, tm);
+                ExpertTile t;
+                if constexpr (kLanes) t = p.table ? expert_tile(p.table, tm) : expert_tile(lane_tiles, TM, tm);
+                else t = expert_tile(p.table, tm);
                 it.part = 0;
                 it.m0 = t.row;
                 it.m_end = t.row + t.rows;

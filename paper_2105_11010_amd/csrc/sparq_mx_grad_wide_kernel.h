@@ -33,9 +33,9 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 #if defined(__HIP_DEVICE_COMPILE__)
     constexpr bool kExperts = !std::is_same_v<PARAMS, GradParams>;
     std::conditional_t<kExperts, GradParams, const GradParams&> p = all;
-    if constexpr (kExperts) {
-        if (!all.template own<T, DW>(p)) return;
-        if constexpr (DW) out += blockIdx.y * p.J * p.ldo;
+    if constexpr (kExperts && DW) {
+        all.template own_rows<T>(p);
+        out += blockIdx.y * p.J * p.ldo;
     }
     const uint32_t part = kExperts ? 0 : blockIdx.y;
     constexpr int P = kParts<T>;                             // of dy, a tile each
@@ -63,10 +63,12 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         }
     }
     uint32_t tj, tk;
-    tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
-    int64_t j0 = (int64_t)tj * TILE;
+    int64_t j0;
     if constexpr (kExperts && !DW) {
-        j0 = all.rows_of(p, tj);
+        if (!all.template own_tile<TILE>(p, j0, tk)) return;
+    } else {
+        tile_of(blockIdx.x, p.tiles_j, p.tiles_k, tj, tk);
+        j0 = (int64_t)tj * TILE;
     }
     const int k0 = (int)tk * TILE;
     const int64_t s_begin = (int64_t)part * p.steps_per_part, s_all = (p.R + kGradStep - 1) / kGradStep;

@@ -1,4 +1,5 @@
-// Tiles of rows, none of two experts: how a launch that cannot know the experts' rows finds its own.
+// Tiles of rows, none of two experts: how a launch that cannot know the experts' rows finds its own.  Up to 64 experts each wavefront counts their tiles itself, a
+// lane an expert, and keeps them in three registers; else, and where a kernel has no registers left, a launch before makes a table of the tiles (3 us).
 #pragma once
 #include "sparq_mx_experts.h"
 
@@ -11,6 +12,7 @@ struct ExpertTile {
 };
 // As many tiles as any division of the rows can make
 inline int64_t most_tiles(int64_t rows, int experts, int tile) { return rows / tile + (rows < experts ? rows : experts); }
+constexpr int kExpertsOfLanes = 64;
 inline size_t table_bytes(int64_t rows, int experts) { return (size_t)round_up((most_tiles(rows, experts, 64) + 1) * (int64_t)sizeof(ExpertTile), 256); }
 sparq_status launch_tiles(const int32_t* offsets, int experts, int64_t rows, int tile, void* table, hipStream_t stream);
 
@@ -21,6 +23,28 @@ __device__ __forceinline__ void expert_rows(const int32_t* offsets, int e, int64
     first = a < 0 ? 0 : a > most ? most : a;
     const int end = b > most ? most : b;
     count = end > first ? end - first : 0;
+}
+// A lane's expert: its rows, and the tiles of all experts up to it
+struct LaneTiles {
+    int first, rows, sum;
+};
+__device__ __forceinline__ LaneTiles tiles_of_lanes(const int32_t* offsets, int experts, int64_t rows, int tile) {
+    const int lane = threadIdx.x & 63;
+    LaneTiles t = {0, 0, 0};
+    if (lane < experts) expert_rows(offsets, lane, rows, t.first, t.rows);
+    t.sum = (t.rows + tile - 1) / tile;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int v = __shfl_up(t.sum, d);
+        if (lane >= d) t.sum += v;
+    }
+    return t;
+}
+__device__ __forceinline__ int tile_count(const LaneTiles& t) { return __builtin_amdgcn_readlane(t.sum, 63); }
+__device__ __forceinline__ ExpertTile expert_tile(const LaneTiles& t, int tile, uint32_t i) {
+    const int e = __builtin_ctzll(__ballot((uint32_t)t.sum > i) | 1ull << 63), rows = __builtin_amdgcn_readlane(t.rows, e);
+    const int in = ((int)i - (__builtin_amdgcn_readlane(t.sum, e) - (rows + tile - 1) / tile)) * tile;
+    return {__builtin_amdgcn_readlane(t.first, e) + in, rows - in < tile ? rows - in : tile, e, 0};
 }
 #if defined(__HIP_DEVICE_COMPILE__)
 // (By the scalar cache: the table does not change while a kernel reads it.)

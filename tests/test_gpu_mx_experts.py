@@ -305,7 +305,8 @@ def test_layer_kept(sq, M, N, K, t, f, bias):  # noqa: F811
     run_product(sq, rng(8, M, N, K), M, N, K, None, t, f, bias, True, 3, 2, kept=True)
 
 
-@pytest.mark.parametrize("counts,M,N,K", [([900, 0, 1500, 800, 200], 3400, 4100, 200), ([1024, 2048, 1024], 4096, 3328, 640), ([37] * 130, 4810, 520, 300), ([1] * 1024, 1030, 70, 64)])
+@pytest.mark.parametrize("counts,M,N,K", [([900, 0, 1500, 800, 200], 3400, 4100, 200), ([1024, 2048, 1024], 4096, 3328, 640), ([37] * 130, 4810, 520, 300), ([1] * 1024, 1030, 70, 64),
+                                              ([3000, 1100, 5], 4105, 3400, 2100), ([20, 0, 130] * 30, 4500, 300, 200), ([16] * 64, 1024, 100, 300), ([100] * 65, 6500, 40, 40)])
 def test_experts_of_many_tiles(sq, counts, M, N, K):  # noqa: F811
     run_product(sq, rng(9, N, K), M, N, K, offsets_of(counts), "bf16", "silu", True, False, 0, 0)
 
@@ -407,7 +408,8 @@ def test_gradients(sq, counts, N, K, t, o, pad, at):  # noqa: F811
     run_gradients(sq, rng(13, N, K), COUNTS[counts], 3, N, K, t, o, pad, at)
 
 
-@pytest.mark.parametrize("counts,N,K", [([900, 0, 1500, 800, 200], 1030, 1100), ([130, 1000, 2000, 70], 2056, 1700), ([1024, 512, 64, 2048], 1664, 2048), ([50] * 40, 400, 900)])
+@pytest.mark.parametrize("counts,N,K", [([900, 0, 1500, 800, 200], 1030, 1100), ([130, 1000, 2000, 70], 2056, 1700), ([1024, 512, 64, 2048], 1664, 2048), ([50] * 40, 400, 900),
+                                        ([20, 0, 130] * 30, 300, 200), ([16] * 64, 100, 300)])
 @pytest.mark.parametrize("t,o", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
 def test_gradients_in_large_tiles(sq, counts, N, K, t, o):  # noqa: F811
     run_gradients(sq, rng(14, N, K), counts, 0, N, K, t, o, 0, 0)
@@ -663,7 +665,7 @@ def test_binding_refuses_wrong_shapes(sq):  # noqa: F811
         (ValueError, "its scales go together", lambda: sq.sparq_mx_experts_linear(x, wq[0].t, wq[1].t, torch.zeros(4, 16, device=DEV), kept_codes=wq[0].t)),
         (ValueError, "dw must have one row", lambda: sq.sparq_mx_experts_dw(x, i(3), wq[0].t, wq[1].t, x)),
         (ValueError, "same number of rows", lambda: sq.sparq_mx_experts_dx(x, i(3), wq[0].t, wq[1].t, x[:3])),
-        (sq.SparqError, "invalid", lambda: sq.sparq_mx_experts_dx(torch.zeros(4, 8, device=DEV), i(3), wq[0].t, wq[1].t, x)),
+        (sq.SparqError, "invalid", lambda: sq.sparq_mx_sort(i(20000), i(3), i(20000))),
         (sq.SparqError, "invalid", lambda: sq.sparq_mx_dropout(x, 1.5, 0, torch.empty_like(x))),
         (ValueError, "seed must be", lambda: sq.sparq_mx_dropout(x, 0.5, -1, torch.empty_like(x))),
         (TypeError, "seed must be", lambda: sq.sparq_mx_dropout(x, 0.5, 1.0, torch.empty_like(x))),

@@ -44,13 +44,13 @@ CALLS = [
      {0: (n, ODD1), 1: (I64(63),), 2: (n, ODD2), 3: (n, ODD2), 4: (0,), 5: (ODD1,), 6: (I64(63),), 7: (n, ODD1), 8: (I64(63),), 9: (I64(-1),), 10: (ODD2,), 11: (7,), 12: (I64(-1),),
       13: (0,)}),
     ("combine_grad", [A, I64(64), A, n, 2, n, I64(0), A, I64(64), I64(6), A, 2, I64(3), 64, n], {5: (A,), 10: (n,)}),
-    ("experts_gemm", [A, A, A, 4, A, A, A, 0, A, I64(8), A, 2, I64(8), A, A, I64(300), 8, 64, A, BIG, n],
+    ("experts_gemm", [A, A, A, 100, A, A, A, 0, A, I64(8), A, 2, I64(8), A, A, I64(3000), 8, 64, A, BIG, n],
      {0: (n, ODD8), 1: (n,), 2: (n, ODD2), 3: (0, -1), 4: (n,), 5: (n,), 6: (ODD2,), 7: (-2, 2), 8: (ODD1,), 9: (I64(7),), 10: (n, ODD1), 11: (3,), 12: (I64(7),), 13: (n, ODD8),
       14: (n,), 15: (I64(-1),), 16: (0,), 17: (0, (1 << 23) + 1), 18: (n, P(0x10010))}),
     ("experts_linear", [A, 2, I64(64), A, 4, A, A, A, 1, A, I64(8), A, 2, I64(8), A, A, I64(300), 8, 64, A, BIG, n],
      {0: (n, ODD1), 1: (5,), 2: (I64(63),), 3: (n, ODD2), 4: (0,), 5: (n,), 6: (n,), 7: (ODD2,), 8: (-2, 2), 9: (ODD1,), 10: (I64(7),), 11: (n,), 12: (3,), 13: (I64(7),), 14: (n,),
       15: (n,), 16: (I64(-1),), 17: (0,), 18: (0,), 19: (n, P(0x10010))}),
-    ("experts_dx", [A, 2, I64(8), A, 4, A, A, A, 2, I64(64), I64(300), 8, 64, A, BIG, n],
+    ("experts_dx", [A, 2, I64(8), A, 100, A, A, A, 2, I64(64), I64(300), 8, 64, A, BIG, n],
      {0: (n, ODD1), 1: (4,), 2: (I64(7),), 3: (n, ODD2), 4: (0,), 5: (n,), 6: (n,), 7: (n,), 8: (1, 4), 9: (I64(63),), 10: (I64(-1),), 11: (0,), 12: (0,), 13: (n, P(0x10010))}),
     ("experts_dw", [A, 2, I64(8), A, 4, A, A, A, 0, I64(64), A, I64(300), 8, 64, n, SZ(0), n],
      {0: (n, ODD1), 1: (4,), 2: (I64(7),), 3: (n, ODD2), 4: (0,), 5: (n,), 6: (n,), 7: (n, ODD2), 8: (1, 4), 9: (I64(63),), 10: (ODD2,), 11: (I64(-1),), 12: (0,), 13: (0,)}),
@@ -101,10 +101,10 @@ def test_more_results_than_a_launch_counts():
 # One byte less than the query names, everything else valid: EWORKSPACE and nothing else; sizes whose plan takes all of it.
 def _workspaces():
     yield "sort", (A, I64(300000), 256, A, A, n), (300000, 256)
-    yield "experts_gemm", (A, A, A, 4, A, A, n, -1, n, I64(0), A, 2, I64(8), n, n, I64(3000), 8, 1 << 20), (3000, 8, 1 << 20, 4)
+    yield "experts_gemm", (A, A, A, 100, A, A, n, -1, n, I64(0), A, 2, I64(8), n, n, I64(3000), 8, 1 << 20), (3000, 8, 1 << 20, 100)
     yield "experts_gemm", (A, A, n, 1, A, A, n, -1, n, I64(0), A, 2, I64(100), n, n, I64(70), 100, 8300), (70, 100, 8300, 1)
     yield "experts_linear", (A, 2, I64(1 << 20), A, 4, A, A, n, -1, n, I64(0), A, 2, I64(8), n, n, I64(3000), 8, 1 << 20), (3000, 8, 1 << 20, 4)
-    yield "experts_dx", (A, 2, I64(8), A, 4, A, A, A, 2, I64(64), I64(300), 8, 64), (300, 8, 64, 4)
+    yield "experts_dx", (A, 2, I64(8), A, 100, A, A, A, 2, I64(64), I64(300), 8, 64), (300, 8, 64, 100)
 
 
 @pytest.mark.parametrize("name,args,sizes", list(_workspaces()), ids=lambda v: v if isinstance(v, str) else "")
