@@ -5,26 +5,62 @@
 namespace sparq {
 namespace mx {
 
+// (of 64 finding them costs what it gains: 16384 rows to 512 x 512 each 35 -> 40 us; 16384 to 8 of 2048 x 2048, uneven, 163 -> 146)
+constexpr int kLongestFirst = 16;
+
 struct ExpertGradParams : GradParams {
     const ExpertTile* table;             // dx: tiles of rows (NULL: by the offsets, at most 64 experts)
     const int32_t* offsets;
     int32_t experts;
     int64_t rows;                        // of dy and of X or dx
-    int32_t margin;                      // dw: an expert's last rows that are not read in whole runs
+    int32_t margin;                      // dw: dy's last rows, which are not read in whole runs (or all of them)
 
 #if defined(__HIP_DEVICE_COMPILE__)
-    // dw: what is the workgroup's own of the call, its expert's rows.
-    template <class T>
-    __device__ __forceinline__ void own_rows(GradParams& p) const {
-        ConstantInt* const at = (ConstantInt*)(offsets + blockIdx.y);
+    // dw: what is the workgroup's own of the call, the rows and results of an expert.  Of a few experts those with the most rows come first: the tiles of a
+    // launch's last round are its shortest ones then.
+    template <class T, class O>
+    __device__ __forceinline__ O* own_rows(GradParams& p, O* out) const {
+        uint32_t expert = blockIdx.y;
+        if (experts <= kLongestFirst) {
+            const int lane = threadIdx.x & 63;
+            int first = 0, n = -1;
+            if (lane < experts) expert_rows(offsets, lane, rows, first, n);
+            uint32_t before = 0;
+            for (int e = 0; e < experts; ++e) {
+                const int other = __builtin_amdgcn_readlane(n, e);
+                before += other > n || (other == n && e < lane) ? 1 : 0;
+            }
+            expert = (uint32_t)__builtin_ctzll(__ballot(lane < experts && before == blockIdx.y) | 1ull << 63);
+        }
+        ConstantInt* const at = (ConstantInt*)(offsets + expert);
         const int most = (int)rows, a = at[0], b = at[1], first = a < 0 ? 0 : a > most ? most : a, end = b > most ? most : b;
         p.R = end > first ? end - first : 0;
         p.dy = static_cast<const T*>(dy) + first * lddy;
         p.codes = codes + first * code_pitch;
         p.scales = scales + first * scale_pitch;
         p.steps_per_part = (int)((p.R + kGradStep - 1) / kGradStep);
-        const int64_t whole = p.R - margin;
-        p.s_whole = whole > 0 && s_whole > 0 ? whole / kGradStep : 0;
+        const int64_t most_fast = rows - margin - first;
+        p.slab = p.R < most_fast ? p.R : most_fast > 0 ? most_fast : 0;
+        if (kParts<T> > 1) p.slab = p.slab / kGradStep * kGradStep;          // (the others' last step may have fewer rows)
+        p.s_whole = (p.slab + kGradStep - 1) / kGradStep;
+        if (column_sums) p.column_sums = column_sums + (int64_t)expert * J;
+        return out + (int64_t)expert * J * ldo;
+    }
+    // dw: as many of the expert's rows as are read in whole runs, those whose runs end inside dy (own_rows); the end of dy's last row; and what is left
+    // behind them.
+    __device__ __forceinline__ int fast_rows(const GradParams& p) const { return (int)p.slab; }
+    template <class T>
+    __device__ __forceinline__ const uint8_t* dy_end(T) const {
+        return reinterpret_cast<const uint8_t*>(static_cast<const T*>(dy) + (rows - 1) * lddy + J);
+    }
+    template <class T>
+    __device__ __forceinline__ void leave_fast(GradParams& p) const {
+        const int64_t n = p.slab;
+        p.dy = static_cast<const T*>(p.dy) + n * lddy;
+        p.codes += n * code_pitch;
+        p.scales += n * scale_pitch;
+        p.R -= n;
+        p.steps_per_part = (int)((p.R + kGradStep - 1) / kGradStep);
     }
     // dx: the workgroup's tile, its first row and column (in tiles); false: there are fewer tiles.
     template <int TILE>

@@ -16,18 +16,26 @@ __global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __res
     Sums::run(dy, lddy, first, (int64_t)first + n, N, blockIdx.x * Sums::kColumns, db + (int64_t)blockIdx.y * N, shared);
 }
 
-// Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them, as in sparq_mx_grad.hip.
-static int grad_tile(int dy_type, int64_t tiles256, int64_t tiles128, int64_t steps, bool dw) {
-    const bool bf16 = dy_type == SPARQ_MX_BF16;
-    return bf16 && !(dw && steps <= 4) && 3 * ((tiles256 + 255) / 256) <= 2 * ((tiles128 + 511) / 512) ? 256 : tiles128 >= 192 ? 128 : 64;
+// Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them.  bf16: as in sparq_mx_grad.hip.  The others, whose
+// parts of dy leave LDS for one tile of 128 a CU, and three (fp16) or two of 64: a round of the smaller makes 0.86 or 0.6 of the time of one of the larger (us, 128 -> 64, fp16:
+// dx 2048 x 2048 x 2048 to 4 experts 85 -> 64, 8192 x 1024 x 1024 to 8 67 -> 61, 16384 x 2048 x 2048 to 8 372 -> 401; dw of 4275 x 777 x 520 to 20 40 -> 34, 2048 x 2048 x 2048
+// to 4 71 -> 80); dw's tiles, many and short, come without rounds.
+static int grad_tile(int dy_type, int64_t tiles256, int64_t tiles128, int64_t tiles64, int64_t steps, bool dw) {
+    if (tiles128 < 192) return 64;
+    if (dy_type == SPARQ_MX_BF16) return !(dw && steps <= 4) && 3 * ((tiles256 + 255) / 256) <= 2 * ((tiles128 + 511) / 512) ? 256 : 128;
+    const int places64 = dy_type == SPARQ_MX_F16 ? 768 : 512;
+    const double round64 = dy_type == SPARQ_MX_F16 ? 0.86 : 0.6;
+    const double rounds128 = dw ? tiles128 / 256.0 : (double)((tiles128 + 255) / 256);
+    const double rounds64 = dw ? (double)tiles64 / places64 : (double)((tiles64 + places64 - 1) / places64);
+    return rounds64 * round64 < rounds128 ? 64 : 128;
 }
 static int dx_tile(int dy_type, int64_t M, int K, int experts) {
     const auto tiles = [&](int t) { return (M / t + experts / 2 + 1) * ((K + t - 1) / t); };
-    return grad_tile(dy_type, tiles(256), tiles(128), 0, false);
+    return grad_tile(dy_type, tiles(256), tiles(128), tiles(64), 0, false);
 }
 static int dw_tile(int dy_type, int64_t M, int N, int K, int experts) {
     const auto tiles = [&](int64_t t) { return experts * ((N + t - 1) / t) * ((K + t - 1) / t); };
-    return grad_tile(dy_type, tiles(256), tiles(128), (M / experts + kGradStep - 1) / kGradStep, true);
+    return grad_tile(dy_type, tiles(256), tiles(128), tiles(64), (M / experts + kGradStep - 1) / kGradStep, true);
 }
 static size_t dx_bytes(int64_t M, int experts) { return experts > kExpertsOfLanes ? table_bytes(M, experts) : 0; }
 static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K, int64_t experts) {
@@ -111,18 +119,24 @@ extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K))) return SPARQ_EINVAL;
     const int t = dw_tile(dy_type, M, N, K, experts);
     const int64_t tiles_j = (N + t - 1) / t, tiles_k = (K + t - 1) / t;
-    if (!grad_countable(M, N, experts) || tiles_j * tiles_k * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
+    if (!grad_countable(M, N, experts) || (tiles_j * tiles_k + N) * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     ExpertGradParams p = grad_params(dy, M > 0 ? lddy : 0, x_codes, x_scales, 8, lddw, N, 0, K, offsets, M);
     p.tiles_j = (int)tiles_j;
     p.tiles_k = (int)tiles_k;
-    // A run that the last column cuts reads on into the next rows: an expert's last rows, which it would leave, are not read in runs.
-    p.s_whole = M > 0 && reads_fit(lddy, p.code_pitch);
-    p.margin = M > 0 ? (int)((round_up(N, 8) - N + lddy - 1) / lddy) : 0;
-    const dim3 grid((unsigned)(tiles_j * tiles_k), (unsigned)experts);
+    // A run that the last column cuts reads on into the next rows: the last rows, which it would leave, are not read in runs; none are if rows' distances do not
+    // fit the loads' 32-bit offsets.
+    p.margin = M == 0 ? 0 : reads_fit(lddy, p.code_pitch) ? (int)((round_up(N, 8) - N + lddy - 1) / lddy) : (int)M;
+    p.experts = experts;
+    // The column sums: by workgroups of the product's launch, which saves a launch, unless dy is so large that these would come last (as in
+    // sparq_mx_grad.hip), or a workgroup of the tiles takes a CU for itself.
+    constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
+    const bool beside = db && M * N <= 1 << 21 && (dy_type == SPARQ_MX_BF16 || t == 64);
+    p.column_sums = beside ? db : nullptr;
+    const dim3 grid((unsigned)(tiles_j * tiles_k + (beside ? (N + kColumns - 1) / kColumns : 0)), (unsigned)experts);
     const sparq_status done = (dy_type == SPARQ_MX_F32 ? launch_experts_dw_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dw_f16 : launch_experts_dw_bf16)(
         p, grid, t, dw, dw_type == SPARQ_MX_F32, s);
-    if (done != SPARQ_OK || !db) return done;
+    if (done != SPARQ_OK || !db || beside) return done;
     with_type(dy_type, [&](auto y) {
         typedef decltype(y) T;
         expert_sums_kernel<T><<<dim3((unsigned)((N + 63) / 64), (unsigned)experts), kSumThreads, 0, s>>>(static_cast<const T*>(dy), p.lddy, offsets, M, N, db);

@@ -34,11 +34,11 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     constexpr bool kExperts = !std::is_same_v<PARAMS, GradParams>;
     std::conditional_t<kExperts, GradParams, const GradParams&> p = all;
     if constexpr (kExperts && DW) {
-        all.template own_rows<T>(p);
-        out += blockIdx.y * p.J * p.ldo;
+        out = all.template own_rows<T, O>(p, out);
     }
     const uint32_t part = kExperts ? 0 : blockIdx.y;
     constexpr int P = kParts<T>;                             // of dy, a tile each
+    constexpr bool kCut = kExperts && DW && P == 1;          // dw's last step is cut off (of more parts, checking costs what it saves)
     constexpr int kF = TILE / 64, kSlots = P * kF * kF;      // 32 x 32 results along a side; matrix instructions a quarter
     constexpr int kRow = TILE * 2;                           // bytes of a tile's row
     constexpr int kRun = TILE == 64 ? 16 : 32, kRuns = TILE * kGradStep / kGradThreads / kRun;      // a thread's runs of V's values
@@ -49,11 +49,15 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
     uint8_t *const lds_dy = lds8, *const lds_v = lds8 + 2 * P * kBytes;
     const int t = threadIdx.x, lane = t & 63, wave = __builtin_amdgcn_readfirstlane(t >> 6), c = lane & 31, g = lane >> 5;
-    if constexpr (DW && !kExperts) {
+    if constexpr (DW) {
         const uint32_t tiles = (uint32_t)p.tiles_j * (uint32_t)p.tiles_k;
         if (blockIdx.x >= tiles) {
             typedef ColumnSums<T, kGradThreads> Sums;
             static_assert(Sums::kFloats * 4 <= kWideLds<T, TILE>);
+            if constexpr (kExperts) {                        // (one slab, the expert's rows)
+                Sums::run(static_cast<const T*>(p.dy), p.lddy, 0, p.R, (int)p.J, (int)(blockIdx.x - tiles) * Sums::kColumns, p.column_sums, reinterpret_cast<float*>(lds8));
+                return;
+            }
             const uint32_t n = blockIdx.x - tiles, across = (uint32_t)((p.J + Sums::kColumns - 1) / Sums::kColumns), slab = n / across;
             const int64_t begin = slab * p.slab, end = begin + p.slab < p.R ? begin + p.slab : p.R;
             if (blockIdx.y == 0)
@@ -110,42 +114,64 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * kSize) : kGradStep * kSize, codes_step = (uint32_t)(kGradStep * p.code_pitch);
         const uint32_t scales_step = (uint32_t)(kGradStep * p.scale_pitch);
         int left = (int)(s_fast - s_begin) - 1;
+        // (kCut) A step's rows may be fewer than 64: the next expert's rows behind them, or what lies past the buffers' ends and comes as zeros, are made
+        // zeros as they are written to LDS -- of the step that is written, and of the one that is asked for.
+        int rows_written = 0, rows_asked = 0;
+        if constexpr (kCut) rows_asked = all.fast_rows(p);
         auto advance = [&]() __attribute__((always_inline)) {
             dy_from += left > 0 ? dy_step : 0;
             codes_from += left > 0 ? codes_step : 0;
             scales_from += left > 0 ? scales_step : 0;
             --left;
+            rows_written = rows_asked;
+            rows_asked -= kGradStep;
         };
         const auto buffer = [](const uint8_t* from) __attribute__((always_inline)) { return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, 0x7FFFFFFF, 0x00020000); };
-        auto load_dy = [&](int i) __attribute__((always_inline)) {
+        // ... that ends with the call's rows, where a step may not
+        const auto buffer_to = [&](const uint8_t* from, const uint8_t* end, auto checked) __attribute__((always_inline)) {
+            const int64_t bytes = end - from;
+            return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, decltype(checked)::value && bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF, 0x00020000);
+        };
+        const uint8_t *dy_end = nullptr, *codes_end = nullptr, *scales_end = nullptr;
+        if constexpr (kCut) {
+            dy_end = all.dy_end(T{});
+            codes_end = all.codes + all.rows * p.code_pitch;
+            scales_end = all.scales + all.rows * p.scale_pitch;
+        }
+        auto load_dy = [&](int i, auto checked) __attribute__((always_inline)) {
 #pragma unroll
             for (int h = 0; h < kKept / 4; ++h) {
-                const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), dy_at[DW ? 0 : i], (DW ? (int)(kRowsAtOnce * i * p.lddy * kSize) : 0) + 16 * h, 0);
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(dy_from, dy_end, checked) : buffer(dy_from)), dy_at[DW ? 0 : i], (DW ? (int)(kRowsAtOnce * i * p.lddy * kSize) : 0) + 16 * h, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) kept[i][4 * h + e] = w[e];
             }
         };
-        auto load_v = [&](int run) __attribute__((always_inline)) {
+        auto load_v = [&](int run, auto checked) __attribute__((always_inline)) {
             if constexpr (kWords == 2) {
-                const v2u w = __builtin_amdgcn_raw_buffer_load_b64(buffer(codes_from), v_at, 0, 0);
+                const v2u w = __builtin_amdgcn_raw_buffer_load_b64((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, 0, 0);
                 raw[run][0] = w[0];
                 raw[run][1] = w[1];
             }
 #pragma unroll
             for (int h = 0; h < kWords / 4; ++h) {
-                const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(codes_from), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) raw[run][4 * h + e] = w[e];
             }
-            scale[run] = __builtin_amdgcn_raw_buffer_load_b8(buffer(scales_from), scale_at, (int)(32 * run * p.scale_pitch), 0);
+            scale[run] = __builtin_amdgcn_raw_buffer_load_b8((kCut ? buffer_to(scales_from, scales_end, checked) : buffer(scales_from)), scale_at, (int)(32 * run * p.scale_pitch), 0);
         };
         // A tile's row is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
         const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
             if constexpr (TILE == 64) return row * kRow + ((chunk ^ (row & 2 ? 5 : 0)) << 4);
             else return row * kRow + ((chunk ^ (chunk >> 4 & 1) ^ ((row & 3) << 2 | (row >> 2 & 3))) << 4);
         };
-        auto write_dy = [&](uint8_t* tile, int i) __attribute__((always_inline)) {
+        auto write_dy = [&](uint8_t* tile, int i, auto checked) __attribute__((always_inline)) {
             uint8_t* const to = tile + (DW ? permuted(kRowsAtOnce * i + t / kAcross, t % kAcross) : 16 * unit_at(32 * i + (t >> 3), t & 7));
+            if constexpr (kCut && decltype(checked)::value) {
+                const bool there = kRowsAtOnce * i + t / kAcross < rows_written;
+#pragma unroll
+                for (int e = 0; e < kKept; ++e) kept[i][e] = there ? kept[i][e] : 0u;
+            }
             if constexpr (P == 1) *reinterpret_cast<v4u*>(to) = v4u{kept[i][0], kept[i][1], kept[i][2], kept[i][3]};
             else {
                 float part[8][P];
@@ -160,9 +186,12 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // values 2 e and 2 e + 1 of the eight of a piece
         v4u decoded;
         float unit;
-        auto decode = [&](int piece, int e) __attribute__((always_inline)) {
+        auto decode = [&](int piece, int e, auto checked) __attribute__((always_inline)) {
             const int run = piece / kPieces, at = piece % kPieces;
-            if (at == 0 && e == 0) unit = DW ? unit8_of(scale[run]) : scale_operand(scale[run]);
+            if (at == 0 && e == 0) {
+                unit = DW ? unit8_of(scale[run]) : scale_operand(scale[run]);
+                if constexpr (kCut && decltype(checked)::value) unit = v_row + 32 * run < rows_written ? unit : 0.0f;
+            }
             if constexpr (DW) {
                 const uint32_t w = raw[run][2 * at + (e >> 1)] >> (16 * (e & 1));
                 decoded[e] = pack_bf16((float)(int8_t)w * unit, (float)(int8_t)(w >> 8) * unit);
@@ -204,7 +233,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 
         // What is issued after matrix instruction i of quarter q of a step whose tiles are the first or second of each side.  Between two
         // barriers, quarters 3, 0, 1, 2, the tiles of the step after the later one's are written and those after them asked for.
-        auto between = [&](auto now_, int q, int i) __attribute__((always_inline)) {
+        auto between = [&](auto now_, int q, int i, auto checked) __attribute__((always_inline)) {
             constexpr int now = decltype(now_)::value;
             const int part = (q + 1) & 3, first = part * kUnits / 4, parts = 8 * ((part + 1) * kUnits / 4 - first);      // pieces this quarter, eight parts each
             if (q == 3 && i == 0) advance();
@@ -212,14 +241,14 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from * P * kBytes, lds_v + read_from * kBytes, (q + 1) & 3, n);
             for (int u = i * parts / kSlots; u < (i + 1) * parts / kSlots; ++u) {
                 const int piece = first + u / 8;
-                if (u % 2 == 0) decode(piece, u % 8 / 2);
+                if (u % 2 == 0) decode(piece, u % 8 / 2, checked);
                 if (u % 8 == 7) {
                     write_v(lds_v + write_to * kBytes, piece);
-                    if (piece % kPieces == kPieces - 1) load_v(piece / kPieces);
+                    if (piece % kPieces == kPieces - 1) load_v(piece / kPieces, checked);
                 }
                 if (u % 8 == 3) {
-                    write_dy(lds_dy + write_to * P * kBytes, piece);
-                    load_dy(piece);
+                    write_dy(lds_dy + write_to * P * kBytes, piece, checked);
+                    load_dy(piece, checked);
                 }
             }
         };
@@ -229,7 +258,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
         };
-        auto step = [&](auto now) __attribute__((always_inline)) {
+        auto step = [&](auto now, auto checked) __attribute__((always_inline)) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 if (q == 3) barrier();                       // the next step's tiles are written, this step's read
@@ -242,37 +271,49 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
                         for (int y = 0; y < kF; ++y) {
                             products.acc[x][y] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(v8bf, o.v[x]), __builtin_bit_cast(v8bf, o.dy[n][y]),
                                                                                          products.acc[x][y], 0, 0, 0);
-                            between(now, q, (x * P + n) * kF + y);
+                            between(now, q, (x * P + n) * kF + y, checked);
                             __builtin_amdgcn_sched_barrier(0);
                         }
             }
         };
 
 #pragma unroll
-        for (int i = 0; i < kUnits; ++i) load_dy(i);
+        for (int i = 0; i < kUnits; ++i) load_dy(i, std::true_type{});
 #pragma unroll
-        for (int i = 0; i < kRuns; ++i) load_v(i);
+        for (int i = 0; i < kRuns; ++i) load_v(i, std::true_type{});
         advance();
         static_assert(kUnits == kPieces * kRuns, "a unit of dy to a piece of V");
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) decode(i, e);
+            for (int e = 0; e < 4; ++e) decode(i, e, std::true_type{});
             write_v(lds_v, i);
-            if (i % kPieces == kPieces - 1) load_v(i / kPieces);
-            write_dy(lds_dy, i);
-            load_dy(i);
+            if (i % kPieces == kPieces - 1) load_v(i / kPieces, std::true_type{});
+            write_dy(lds_dy, i, std::true_type{});
+            load_dy(i, std::true_type{});
         }
         barrier();
         // as if the last quarter of a step before the first
 #pragma unroll
-        for (int i = 0; i < kSlots; ++i) between(std::integral_constant<int, 1>{}, 3, i);
-        for (int64_t s = s_begin; s < s_fast; s += 2) {
-            step(std::integral_constant<int, 0>{});
-            if (s + 1 < s_fast) step(std::integral_constant<int, 1>{});
+        for (int i = 0; i < kSlots; ++i) between(std::integral_constant<int, 1>{}, 3, i, std::true_type{});
+        int64_t s = s_begin;
+        if constexpr (kCut)
+            for (; s + 5 < s_fast; s += 2) {                 // (what these ask for, up to a quarter of step s + 4, is of whole steps)
+                step(std::integral_constant<int, 0>{}, std::false_type{});
+                step(std::integral_constant<int, 1>{}, std::false_type{});
+            }
+        for (; s < s_fast; s += 2) {
+            step(std::integral_constant<int, 0>{}, std::true_type{});
+            if (s + 1 < s_fast) step(std::integral_constant<int, 1>{}, std::true_type{});
         }
     }
-    multiply_rest<T, DW, TILE, TILE>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_begin < s_fast ? s_fast : s_begin, s_end);
+    int64_t s_rest = s_begin < s_fast ? s_fast : s_begin, s_last = s_end;
+    if constexpr (kExperts && DW) {                          // (the rows behind the fast ones, by themselves)
+        all.template leave_fast<T>(p);
+        s_rest = 0;
+        s_last = p.steps_per_part;
+    }
+    multiply_rest<T, DW, TILE, TILE>(products, p, reinterpret_cast<v4u*>(lds8), j0, k0, s_rest, s_last);
 
     __syncthreads();
     const __amdgpu_buffer_rsrc_t none = __builtin_amdgcn_make_buffer_rsrc((void*)nullptr, 0, 0, 0x00020000);
