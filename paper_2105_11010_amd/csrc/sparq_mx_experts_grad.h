@@ -13,6 +13,7 @@ struct ExpertGradParams : GradParams {
     const int32_t* offsets;
     int32_t experts;
     int64_t rows;                        // of dy and of X or dx
+    int32_t whole;                       // dx, without a table: n > 0: each expert's first whole n rows alone; n < 0: what is left behind whole -n rows; 0: all rows
     int32_t margin;                      // dw: dy's last rows, which are not read in whole runs (or all of them)
 
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -66,7 +67,7 @@ struct ExpertGradParams : GradParams {
     template <int TILE>
     __device__ __forceinline__ bool own_tile(GradParams& p, int64_t& j0, uint32_t& tk) const {
         LaneTiles lanes = {};
-        if (!table) lanes = tiles_of_lanes(offsets, experts, rows, TILE);
+        if (!table) lanes = tiles_of_lanes(offsets, experts, rows, TILE, whole);
         const uint32_t tiles = (uint32_t)(table ? tile_count(table) : tile_count(lanes));
         if (blockIdx.x >= tiles * (uint32_t)tiles_k) return false;
         uint32_t tj;

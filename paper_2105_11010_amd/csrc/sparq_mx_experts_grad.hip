@@ -91,7 +91,7 @@ extern "C" sparq_status sparq_mx_experts_dx(const void* dy, int32_t dy_type, int
     if (bytes && (!workspace || !aligned(workspace, 256))) return SPARQ_EINVAL;
     if (workspace_bytes < bytes) return SPARQ_EWORKSPACE;
     const int t = dx_tile(dy_type, M, K, experts);
-    const int64_t tiles_j = most_tiles(M, experts, t), tiles_k = (K + t - 1) / t;
+    const int64_t tiles_j = most_tiles(M, experts, t), tiles_k = (K + t - 1) / t, rest_k = (K + 63) / 64;
     if (!grad_countable(M, N, experts) || tiles_j * tiles_k * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     if (bytes) {
@@ -101,12 +101,24 @@ extern "C" sparq_status sparq_mx_experts_dx(const void* dy, int32_t dy_type, int
     ExpertGradParams p = grad_params(dy, lddy, w_codes, w_scales, 4, lddx, M, N, K, offsets, M);
     p.table = bytes ? static_cast<const ExpertTile*>(workspace) : nullptr;
     p.experts = experts;
-    p.tiles_k = (int)tiles_k;
     p.s_whole = reads_fit(lddy, p.code_pitch) ? N / kGradStep : 0;
     p.steps_per_part = (N + kGradStep - 1) / kGradStep;
-    const dim3 grid((unsigned)(tiles_j * tiles_k));
-    return (dy_type == SPARQ_MX_F32 ? launch_experts_dx_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dx_f16 : launch_experts_dx_bf16)(
-        p, grid, t, dx, dx_type == SPARQ_MX_F32, s);
+    const auto launch = [&](int tile, int64_t rows, int64_t columns) {
+        p.tiles_k = (int)columns;
+        return (dy_type == SPARQ_MX_F32 ? launch_experts_dx_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dx_f16 : launch_experts_dx_bf16)(
+            p, dim3((unsigned)(rows * columns)), tile, dx, dx_type == SPARQ_MX_F32, s);
+    };
+    // Tiles of 256 x 256, one a CU at a time: where the experts' last ones, which are about half empty, would make a round more, what is left behind whole tiles goes in tiles
+    // of 64, in a launch of its own (us, one launch -> two: 16384 x 2048 x 2048 to 8 experts, uneven, 155 -> 137, 16384 x 4096 x 1024 to 4 178 -> 135; the second takes 22 and 45, a step of
+    // its 32 and 64 after the other).
+    const int64_t half = (experts + 1) / 2, whole = M / 256 > half ? (M / 256 - half) * tiles_k : 0;
+    if (t != 256 || bytes || rest_k * experts * 4 * kGradThreads >= 1ll << 32 || ((M / 256 + half) * tiles_k + 255) / 256 <= (whole + 255) / 256)
+        return launch(t, tiles_j, tiles_k);
+    p.whole = 256;
+    const sparq_status done = launch(256, M / 256 > 0 ? M / 256 : 1, tiles_k);
+    if (done != SPARQ_OK) return done;
+    p.whole = -256;
+    return launch(64, experts * 4ll, rest_k);
 }
 
 extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int64_t lddy, const int32_t* offsets, int32_t experts, const void* x_codes,
@@ -131,7 +143,7 @@ extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int
     // The column sums: by workgroups of the product's launch, which saves a launch, unless dy is so large that these would come last (as in
     // sparq_mx_grad.hip), or a workgroup of the tiles takes a CU for itself.
     constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
-    const bool beside = db && M * N <= 1 << 21 && (dy_type == SPARQ_MX_BF16 || t == 64);
+    const bool beside = db && M * N <= 1 << (t == 64 ? 22 : 21) && (dy_type == SPARQ_MX_BF16 || t == 64);
     p.column_sums = beside ? db : nullptr;
     const dim3 grid((unsigned)(tiles_j * tiles_k + (beside ? (N + kColumns - 1) / kColumns : 0)), (unsigned)experts);
     const sparq_status done = (dy_type == SPARQ_MX_F32 ? launch_experts_dw_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dw_f16 : launch_experts_dw_bf16)(

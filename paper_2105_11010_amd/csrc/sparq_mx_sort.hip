@@ -7,14 +7,15 @@ namespace mx {
 // A counting sort that keeps the order of equal keys.  A wavefront has a range of slots, kAhead times 64 of them in registers at a time: it counts them by expert
 // in LDS, and once the counts of all ranges before its own are known, for each expert, it takes 64 slots at a time; a slot's rank among the lanes with the
 // same expert is the number of such lanes below, found by one ballot a bit of the expert's number.  Slots refused are those of one expert more, the last.
-// Bound by waiting: for the slots, the other workgroups' counts, and as many rounds of ballots as a range has 64s.
+// Bound by waiting: for the slots, the other workgroups' counts, and as many rounds of ballots as a range has 64s.  262144 slots among 256 experts 13.1 us (4 and 11 in
+// its two kernels; 3 MB, 0.5 at memory's pace), 16384 among 8 9.9.
 struct SortParams {
     const int32_t* expert;
     int32_t *offsets, *place, *order;
     int32_t* counts;             // [workgroups][experts + 1], of more workgroups than one
     int32_t slots, experts, range;               // slots of a wavefront (whole kAhead 64s)
 };
-constexpr int kAhead = 8;
+constexpr int kAhead = 4;
 
 // Lanes' buckets of kAhead times 64 slots from s on (-1: past the end)
 __device__ __forceinline__ void buckets_of(const SortParams& p, int64_t s, int (&key)[kAhead]) {
@@ -50,38 +51,47 @@ __global__ __launch_bounds__(WAVES * 64) void sort_count_kernel(const SortParams
 template <int WAVES, bool MANY>
 __global__ __launch_bounds__(WAVES * 64) void sort_kernel(const SortParams p) {
     constexpr int THREADS = WAVES * 64;
-    extern __shared__ int32_t lds[];             // [WAVES][buckets] counts, then the wavefronts' next rows; [buckets] all counts; [WAVES] sums
+    // [WAVES][buckets] counts, then the wavefronts' next rows; [buckets] the counts before the workgroup's (MANY) and all of them; [WAVES] sums
+    extern __shared__ int32_t lds[];
     const int buckets = p.experts + 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int32_t *const mine = lds + wave * buckets, *const all = lds + WAVES * buckets, *const sums = all + buckets;
-    for (int i = threadIdx.x; i < WAVES * buckets; i += THREADS) lds[i] = 0;
+    int32_t *const mine = lds + wave * buckets, *const before = lds + WAVES * buckets, *const all = before + buckets, *const sums = all + buckets;
+    for (int i = threadIdx.x; i < (WAVES + 2) * buckets; i += THREADS) lds[i] = 0;
     __syncthreads();
     const int64_t first = (int64_t)(blockIdx.x * WAVES + wave) * p.range;
     int key[kAhead];                             // of a range no longer than these, for good
     count_range(p, first, mine, key);
     __syncthreads();
-    // Counts before each wavefront, and all of them
-    for (int e = threadIdx.x; e < buckets; e += THREADS) {
-        int before = 0, total = 0;
-        if constexpr (MANY) {
-            // (32 workgroups' counts on their way at a time)
-            for (int b0 = 0; b0 < (int)gridDim.x; b0 += 32) {
-                int n[32];
+    // Counts before each wavefront, and all of them: of other workgroups by as many threads a bucket as there are, 16 workgroups' on their way at a time
+    if constexpr (MANY) {
+        const int parts = THREADS / buckets > 1 ? THREADS / buckets : 1;
+        for (int i = threadIdx.x; i < parts * buckets; i += THREADS) {
+            const int part = i / buckets, e = i - part * buckets;
+            int n_before = 0, total = 0;
+            for (int b0 = part; b0 < (int)gridDim.x; b0 += 16 * parts) {
+                int n[16];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) n[i] = p.counts[(int64_t)(b0 + i < (int)gridDim.x ? b0 + i : 0) * buckets + e];
+                for (int j = 0; j < 16; ++j) n[j] = p.counts[(int64_t)(b0 + j * parts < (int)gridDim.x ? b0 + j * parts : 0) * buckets + e];
 #pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    if (b0 + i < (int)gridDim.x) total += n[i];
-                    if (b0 + i < (int)blockIdx.x) before += n[i];
+                for (int j = 0; j < 16; ++j) {
+                    const int b = b0 + j * parts;
+                    if (b < (int)gridDim.x) total += n[j];
+                    if (b < (int)blockIdx.x) n_before += n[j];
                 }
             }
+            atomicAdd(&before[e], n_before);
+            atomicAdd(&all[e], total);
         }
+        __syncthreads();
+    }
+    for (int e = threadIdx.x; e < buckets; e += THREADS) {
+        int sum = MANY ? before[e] : 0;
 #pragma unroll
         for (int w = 0; w < WAVES; ++w) {
             const int n = lds[w * buckets + e];
-            lds[w * buckets + e] = before;
-            before += n;
+            lds[w * buckets + e] = sum;
+            sum += n;
         }
-        all[e] = MANY ? total : before;
+        if (!MANY) all[e] = sum;
     }
     __syncthreads();
     // The experts' first rows: sums of the counts below, THREADS experts at a time
@@ -137,8 +147,8 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(const SortParams p) {
     }
 }
 
-// One workgroup while its sixteen wavefronts hold all slots; more take two launches, the first of which counts: as few slots a workgroup as leave no more than
-// 256 of them, whose counts each adds up.
+// One workgroup for a few thousand slots (4096 among 8 experts 6.3 us, 300 4.8; 8192 among 64 9.6, in two launches 9.9, among 1024 16.1 and 12.6); more take two launches,
+// the first of which counts: as few slots a workgroup as leave no more than 256 of them, whose counts each adds up.
 struct SortPlan {
     int waves, range, blocks;
     size_t bytes;
@@ -147,9 +157,9 @@ static SortPlan sort_plan(int64_t slots, int experts) {
     SortPlan p = {};
     constexpr int least = 64 * kAhead;
     const int most = experts <= 512 ? 16 : 8;                // (LDS)
-    p.waves = slots <= 256 ? 1 : slots <= least * most ? most : 8;
-    const int64_t ranges = (slots + least - 1) / least;
-    p.range = p.waves == 8 && ranges > 8 * 256 ? (int)round_up((slots + 8 * 256 - 1) / (8 * 256), least) : least;
+    p.waves = slots <= least ? 1 : most;
+    const int64_t ranges = (slots + least - 1) / least, wanted = slots <= 4096 ? p.waves : most * 256;
+    p.range = ranges > wanted ? (int)round_up((slots + wanted - 1) / wanted, least) : least;
     p.blocks = slots == 0 ? 1 : (int)((slots + (int64_t)p.range * p.waves - 1) / ((int64_t)p.range * p.waves));
     p.bytes = p.blocks > 1 ? (size_t)round_up((int64_t)p.blocks * (experts + 1) * 4, 256) : 0;
     return p;
@@ -159,7 +169,7 @@ static bool sort_countable(int64_t slots, int experts) { return slots <= 1 << 30
 
 template <int WAVES>
 static sparq_status launch_sort(const SortParams& p, int blocks, hipStream_t stream) {
-    const int buckets = p.experts + 1, lds_bytes = ((WAVES + 1) * buckets + WAVES) * 4;
+    const int buckets = p.experts + 1, lds_bytes = ((WAVES + 2) * buckets + WAVES) * 4;
     if (blocks == 1) {
         sort_kernel<WAVES, false><<<1, WAVES * 64, lds_bytes, stream>>>(p);
         return launch_status();

@@ -24,14 +24,20 @@ __device__ __forceinline__ void expert_rows(const int32_t* offsets, int e, int64
     const int end = b > most ? most : b;
     count = end > first ? end - first : 0;
 }
-// A lane's expert: its rows, and the tiles of all experts up to it
+// A lane's expert: its rows, and the tiles of all experts up to it.  whole n > 0: of its first whole n rows alone; n < 0: of what is left behind whole -n rows.
 struct LaneTiles {
     int first, rows, sum;
 };
-__device__ __forceinline__ LaneTiles tiles_of_lanes(const int32_t* offsets, int experts, int64_t rows, int tile) {
+__device__ __forceinline__ LaneTiles tiles_of_lanes(const int32_t* offsets, int experts, int64_t rows, int tile, int whole = 0) {
     const int lane = threadIdx.x & 63;
     LaneTiles t = {0, 0, 0};
     if (lane < experts) expert_rows(offsets, lane, rows, t.first, t.rows);
+    if (whole > 0) t.rows = t.rows / whole * whole;
+    if (whole < 0) {
+        const int n = t.rows / -whole * -whole;
+        t.first += n;
+        t.rows -= n;
+    }
     t.sum = (t.rows + tile - 1) / tile;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {

@@ -409,7 +409,8 @@ def test_gradients(sq, counts, N, K, t, o, pad, at):  # noqa: F811
 
 
 @pytest.mark.parametrize("counts,N,K", [([900, 0, 1500, 800, 200], 1030, 1100), ([130, 1000, 2000, 70], 2056, 1700), ([1024, 512, 64, 2048], 1664, 2048), ([50] * 40, 400, 900),
-                                        ([20, 0, 130] * 30, 300, 200), ([16] * 64, 100, 300)])
+                                        ([20, 0, 130] * 30, 300, 200), ([16] * 64, 100, 300), ([4096, 5001, 0, 255, 7032], 72, 1000),
+                                        ([16100, 290], 40, 1024)])
 @pytest.mark.parametrize("t,o", [("bf16", "bf16"), ("bf16", "f32"), ("f16", "f16"), ("f32", "f32")])
 def test_gradients_in_large_tiles(sq, counts, N, K, t, o):  # noqa: F811
     run_gradients(sq, rng(14, N, K), counts, 0, N, K, t, o, 0, 0)
