@@ -75,6 +75,7 @@ PyObject* gather(PyObject* const* args, Py_ssize_t nargs, PyObject* kwnames) {
     parse(sig, args, nargs, kwnames, a);
     const Rows x = rows_of(a[0], "x");
     const Places place = places(a[1], x.rows);
+    if (code_bytes((int32_t)x.length, 4) == 0) raise(PyExc_ValueError, "x must have rows of at most 2^28 values");
     int64_t rows = 0;
     Rows y;
     if (given(a[2])) {

@@ -98,7 +98,7 @@ struct Epilogue {
 #pragma unroll
             for (int i = 0; i < FI; ++i) {
                 const Piece now = next;
-                if (residual && whole && i * FJ + j + 1 < FI * FJ) fetch((i + 1) % FI, j + (i + 1) / FI, next);
+                if (residual && whole && j * FI + i + 1 < FI * FJ) fetch((i + 1) % FI, j + (i + 1) / FI, next);
                 float z[16];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)

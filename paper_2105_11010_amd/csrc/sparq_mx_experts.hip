@@ -217,7 +217,7 @@ static sparq_status product(const Call& c, const ExpertsPlan& plan, void* worksp
 // As many tiles, with their parts, as the kernels count
 static bool countable(const ExpertsPlan& p, int64_t M, int64_t N, int experts) {
     if (M >= 1ll << 31 || experts > SPARQ_MX_EXPERTS_MOST || (int64_t)experts * N >= 1ll << 31) return false;
-    if (p.tile == 0) return p.pieces < 65536 && (N + kFewColumns - 1) / kFewColumns < 1ll << 22;
+    if (p.tile == 0) return true;                            // (at most 1792 pieces, and 8 blocks a workgroup of many)
     const int t = p.tile;
     return (M / t + 1 + experts) * ((N + t - 1) / t) * p.parts < (1ll << 31);
 }

@@ -509,6 +509,87 @@ def test_dropout_keeps_its_share(sq):  # noqa: F811
         assert abs(both - m[:, 1:].numel() * (1 - p) ** 2) <= 9 * (n * p * (1 - p)) ** 0.5 + 1
 
 
+# ---- far apart, elsewhere, twice -----------------------------------------------------------------------------------------------------------
+def test_rows_more_than_32_bits_apart(sq):  # noqa: F811
+    """Rows 2^31 + 8 elements apart: offsets beyond 32 bits, of elements and of bytes, give what rows side by side give."""
+    g = rng(17)
+    T, K, N, ld = 3, 200, 72, (1 << 31) + 8
+    far = torch.empty(2 * ld + 8192, dtype=torch.bfloat16, device=DEV)
+    view = lambda n, at: far.as_strided((T, n), (ld, 1), at)      # noqa: E731
+    place = ints(np.array([[2], [0], [1]]))
+    w, offsets = floats(g.standard_normal((T, 1))), ints([0, 1, 3])
+    near_x, near_dy = matrix(values(g, T, K, "bf16"), "bf16"), matrix(values(g, T, N, "bf16"), "bf16")
+    far_x, far_dy = view(K, 0), view(N, 512)
+    far_x.copy_(near_x)
+    far_dy.copy_(near_dy)
+    wq, x8 = stored(sq, values(g, 2 * N, K, "f32"), 4), coded_buffers(sq, T, K, 8)
+    sq.sparq_mx_quantize(near_x, codes8=x8[0].t, scales8=x8[1].t)
+    ws = torch.empty(1 << 16, dtype=torch.uint8, device=DEV)
+
+    def run(x, dy, out):
+        o = [out(K) for _ in range(5)] + [out(N) for _ in range(3)]
+        sq.sparq_mx_gather(x, place, y=o[0])
+        c = coded_buffers(sq, T, K, 4)
+        sq.sparq_mx_gather(x, place, codes4=c[0].t, scales4=c[1].t)
+        sq.sparq_mx_combine(x, place, o[1], weights=w, residual=x)
+        dw = torch.empty(T, 1, device=DEV)
+        sq.sparq_mx_combine_grad(x, place, w, dx=o[2], x=x, dweights=dw)
+        sq.sparq_mx_dropout(x, 0.5, 3, o[3], residual=x)
+        sq.sparq_mx_experts_dx(dy, offsets, *wq, o[4], workspace=ws)
+        sq.sparq_mx_experts_linear(x, *wq, o[5], offsets=offsets, function="silu", residual=dy, workspace=ws)
+        kept = coded_buffers(sq, T, N, 8)
+        sq.sparq_mx_experts_linear(x, *wq, o[6], offsets=offsets, function="gelu", residual=dy, kept_codes=kept[0].t, kept_scales=kept[1].t, workspace=ws)
+        sq.sparq_mx_experts_linear(x, wq[0][:N], wq[1][:N], o[7], residual=dy, workspace=ws)
+        grad, db = torch.empty(2 * N, K, device=DEV), torch.empty(2, N, device=DEV)
+        sq.sparq_mx_experts_dw(dy, offsets, x8[0].t, x8[1].t, grad, db=db)
+        return [v.contiguous() for v in o] + [c[0].t, c[1].t, dw, kept[0].t, kept[1].t, grad, db]
+
+    places_ = iter(range(1024, 8192, 512))
+    got = run(far_x, far_dy, lambda n: view(n, next(places_)))
+    want = run(near_x, near_dy, lambda n: torch.empty(T, n, dtype=torch.bfloat16, device=DEV))
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(got) == len(want)
+
+
+def test_on_another_stream_and_twice(sq):  # noqa: F811
+    """The same calls on a stream of their own, at work beside the default one, and again: the same bits."""
+    tokens, per, experts = 700, 3, 9
+    chosen, weights = choices(2, tokens, per, experts)
+    x = torch.randn(tokens, 192, device=DEV).bfloat16()
+    dy = torch.randn(tokens, 192, device=DEV).bfloat16()
+    torch.cuda.synchronize()
+
+    def run():
+        block = Block(sq, tokens, per, experts, 192, 136)
+        block.forward(x, chosen, weights, 0.3, None)
+        block.backward(dy, weights, 0.3, None)
+        return block.results()
+
+    first = run()
+    stream = torch.cuda.Stream()
+    with torch.cuda.stream(stream):
+        second = run()
+    third = run()
+    torch.cuda.synchronize()
+    for k, v in first.items():
+        assert torch.equal(v, second[k]) and torch.equal(v, third[k]), k
+
+
+def test_the_same_rows_in_any_company(sq):  # noqa: F811
+    """A row's result does not depend on which rows are beside it as long as the kernel is the same: rows of one expert among others' and alone."""
+    g = rng(18)
+    N, K = 96, 256
+    x, W = values(g, 60, K, "bf16"), values(g, 3 * N, K, "f32")
+    w = stored(sq, W, 4)
+    ws = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+    a, b = torch.empty(60, N, device=DEV), torch.empty(30, N, device=DEV)
+    sq.sparq_mx_experts_linear(matrix(x, "bf16"), *w, a, offsets=ints([0, 10, 40, 60]), workspace=ws)
+    sq.sparq_mx_experts_linear(matrix(x[10:40], "bf16"), *w, b, offsets=ints([0, 0, 30, 30]), workspace=ws)
+    z, size, _ = E.product(R.quantised(x, 4), R.quantised(W, 4).reshape(3, N, K), [0, 10, 40, 60])
+    off = 2 * (K + 2) * u * size
+    close(a.double().cpu().numpy(), z, off, "f32")
+    close(b.double().cpu().numpy(), z[10:40], off[10:40], "f32")
+
+
 # ---- together --------------------------------------------------------------------------------------------------------------------------
 class Block:
     """y = x + dropout(sum_j w_j W2[e_j] gelu(W1[e_j] x + b1[e_j])) over each token's chosen experts e_j, forward and backward, on the entry points alone."""
