@@ -7,15 +7,15 @@ namespace mx {
 // A counting sort that keeps the order of equal keys.  A wavefront has a range of slots, kAhead times 64 of them in registers at a time: it counts them by expert
 // in LDS, and once the counts of all ranges before its own are known, for each expert, it takes 64 slots at a time; a slot's rank among the lanes with the
 // same expert is the number of such lanes below, found by one ballot a bit of the expert's number.  Slots refused are those of one expert more, the last.
-// Bound by waiting: for the slots, the other workgroups' counts, and as many rounds of ballots as a range has 64s.  262144 slots among 256 experts 13.1 us (4 and 11 in
-// its two kernels; 3 MB, 0.5 at memory's pace), 16384 among 8 9.9.
+// Bound by waiting: for the slots, the other workgroups' counts, and as many rounds of ballots as a range has 64s.  262144 slots among 256 experts 13.2 us (4 and 11 in
+// its two kernels; 3 MB, 0.5 at memory's pace), 16384 among 8 8.6.
 struct SortParams {
     const int32_t* expert;
     int32_t *offsets, *place, *order;
     int32_t* counts;             // [workgroups][experts + 1], of more workgroups than one
     int32_t slots, experts, range;               // slots of a wavefront (whole kAhead 64s)
 };
-constexpr int kAhead = 4;
+constexpr int kAhead = 2;                    // (us, one -> two -> four: 16384 slots among 8 experts 7.8, 8.6, 9.9; 262144 among 256 16.8, 13.2, 13.1)
 
 // Lanes' buckets of kAhead times 64 slots from s on (-1: past the end)
 __device__ __forceinline__ void buckets_of(const SortParams& p, int64_t s, int (&key)[kAhead]) {
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(WAVES * 64) void sort_kernel(const SortParams p) {
     }
 }
 
-// One workgroup for a few thousand slots (4096 among 8 experts 6.3 us, 300 4.8; 8192 among 64 9.6, in two launches 9.9, among 1024 16.1 and 12.6); more take two launches,
+// One workgroup for a few thousand slots (4096 among 8 experts 6.5 us, 300 4.4; 8192 among 1024 in one 16.1, in two 11.8); more take two launches,
 // the first of which counts: as few slots a workgroup as leave no more than 256 of them, whose counts each adds up.
 struct SortPlan {
     int waves, range, blocks;
