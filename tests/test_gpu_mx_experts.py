@@ -8,6 +8,9 @@ Tolerances, fixed before any run.  u = 2^-24 is fp32's unit roundoff, U the resu
   epilogue      f's slope is at most 1.13 in magnitude; f itself is off by what test_gpu_mx.test_act allows; the residual's addition u (|f| + |r|)
   kept form     half a step of the block's power of two, a whole one where 127 is the last code, and z's own error
 """
+import os
+import sys
+
 import numpy as np
 import pytest
 import torch
@@ -17,6 +20,14 @@ import mx_reference as R
 from test_gpu_mx import DEV, TYPES, Bytes, Result, close, coded_buffers, guard, matrix, rng, sq, stored, u, values, workspace  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def Block():
+    """The example's block, which runs the operators together."""
+    sys.path.insert(0, os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples"))
+    import experts
+    return experts.Block
 
 
 class Whole:
@@ -550,7 +561,7 @@ def test_rows_more_than_32_bits_apart(sq):  # noqa: F811
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and len(got) == len(want)
 
 
-def test_on_another_stream_and_twice(sq):  # noqa: F811
+def test_on_another_stream_and_twice(sq, Block):  # noqa: F811
     """The same calls on a stream of their own, at work beside the default one, and again: the same bits."""
     tokens, per, experts = 700, 3, 9
     chosen, weights = choices(2, tokens, per, experts)
@@ -559,7 +570,7 @@ def test_on_another_stream_and_twice(sq):  # noqa: F811
     torch.cuda.synchronize()
 
     def run():
-        block = Block(sq, tokens, per, experts, 192, 136)
+        block = Block(tokens, per, experts, 192, 136)
         block.forward(x, chosen, weights, 0.3, None)
         block.backward(dy, weights, 0.3, None)
         return block.results()
@@ -591,61 +602,6 @@ def test_the_same_rows_in_any_company(sq):  # noqa: F811
 
 
 # ---- together --------------------------------------------------------------------------------------------------------------------------
-class Block:
-    """y = x + dropout(sum_j w_j W2[e_j] gelu(W1[e_j] x + b1[e_j])) over each token's chosen experts e_j, forward and backward, on the entry points alone."""
-
-    def __init__(self, sq, tokens, per, experts, width, hidden):  # noqa: F811
-        g = torch.Generator(device=DEV).manual_seed(3)
-        self.sq, self.sizes = sq, (tokens, per, experts, width, hidden)
-        rows = tokens * per
-        f32 = lambda *s: torch.empty(*s, device=DEV)      # noqa: E731
-        bf16 = lambda *s: torch.empty(*s, dtype=torch.bfloat16, device=DEV)      # noqa: E731
-        i32 = lambda *s: torch.empty(*s, dtype=torch.int32, device=DEV)      # noqa: E731
-        coded = lambda r, K, bits: tuple(b.t for b in coded_buffers(sq, r, K, bits))      # noqa: E731
-        self.w1 = torch.randn(experts * hidden, width, generator=g, device=DEV) * width ** -0.5
-        self.w2 = torch.randn(experts * width, hidden, generator=g, device=DEV) * hidden ** -0.5
-        self.b1 = torch.randn(experts, hidden, generator=g, device=DEV)
-        self.w1q, self.w2q = coded(experts * hidden, width, 4), coded(experts * width, hidden, 4)
-        sq.sparq_mx_quantize(self.w1, *self.w1q)
-        sq.sparq_mx_quantize(self.w2, *self.w2q)
-        self.offsets, self.place = i32(experts + 1), i32(tokens, per)
-        self.x4, self.x8, self.a4, self.a8, self.z8 = coded(rows, width, 4), coded(rows, width, 8), coded(rows, hidden, 4), coded(rows, hidden, 8), coded(rows, hidden, 8)
-        self.a, self.o, self.c, self.y = bf16(rows, hidden), bf16(rows, width), bf16(tokens, width), bf16(tokens, width)
-        self.dc, self.do, self.da, self.dz, self.dr, self.dx = bf16(tokens, width), bf16(rows, width), bf16(rows, hidden), bf16(rows, hidden), bf16(rows, width), bf16(tokens, width)
-        self.dweights, self.dw1, self.dw2, self.db1 = f32(tokens, per), torch.empty_like(self.w1), torch.empty_like(self.w2), f32(experts, hidden)
-        need = [sq.sparq_mx_sort_workspace_bytes(rows, experts)]
-        for n, k in ((hidden, width), (width, hidden)):
-            need += [getattr(sq, f"sparq_mx_experts_{f}_workspace_bytes")(rows, n, k, experts) for f in ("gemm", "dx", "dw")]
-        self.ws = torch.empty(max(need), dtype=torch.uint8, device=DEV)
-        for v in vars(self).values():                                            # rows that nobody has are read by the codec alone
-            if isinstance(v, torch.Tensor) and v.dtype == torch.bfloat16:
-                v.zero_()
-
-    def forward(self, x, chosen, weights, p, step):
-        sq, ws, width, hidden = self.sq, self.ws, *self.sizes[3:]  # noqa: F811
-        sq.sparq_mx_sort(chosen, self.offsets, self.place, workspace=ws)
-        sq.sparq_mx_gather(x, self.place, codes4=self.x4[0], scales4=self.x4[1], codes8=self.x8[0], scales8=self.x8[1])
-        sq.sparq_mx_experts_gemm(*self.x4, *self.w1q, width, self.a, offsets=self.offsets, bias=self.b1, function="gelu", kept_codes=self.z8[0], kept_scales=self.z8[1], workspace=ws)
-        sq.sparq_mx_quantize(self.a, *self.a4, *self.a8)
-        sq.sparq_mx_experts_gemm(*self.a4, *self.w2q, hidden, self.o, offsets=self.offsets, workspace=ws)
-        sq.sparq_mx_combine(self.o, self.place, self.c, weights=weights)
-        sq.sparq_mx_dropout(self.c, p, 17, self.y, residual=x, step=step)
-
-    def backward(self, dy, weights, p, step):
-        sq, ws = self.sq, self.ws  # noqa: F811
-        sq.sparq_mx_dropout(dy, p, 17, self.dc, step=step)
-        sq.sparq_mx_combine_grad(self.dc, self.place, weights, dx=self.do, x=self.o, dweights=self.dweights)
-        sq.sparq_mx_experts_dx(self.do, self.offsets, *self.w2q, self.da, workspace=ws)
-        sq.sparq_mx_experts_dw(self.do, self.offsets, *self.a8, self.dw2, workspace=ws)
-        sq.sparq_mx_act_grad("gelu", self.da, *self.z8, self.dz)
-        sq.sparq_mx_experts_dx(self.dz, self.offsets, *self.w1q, self.dr, workspace=ws)
-        sq.sparq_mx_experts_dw(self.dz, self.offsets, *self.x8, self.dw1, db=self.db1, workspace=ws)
-        sq.sparq_mx_combine(self.dr, self.place, self.dx, residual=dy)
-
-    def results(self):
-        return {k: getattr(self, k) for k in ("offsets", "place", "y", "dx", "dweights", "dw1", "dw2", "db1")}
-
-
 def choices(seed, tokens, per, experts):
     g = torch.Generator(device=DEV).manual_seed(seed)
     top, chosen = torch.topk(torch.randn(tokens, experts, generator=g, device=DEV), per, dim=1)
@@ -653,11 +609,11 @@ def choices(seed, tokens, per, experts):
     return chosen.contiguous(), torch.softmax(top, 1).contiguous()
 
 
-def test_a_block_with_experts(sq):  # noqa: F811
+def test_a_block_with_experts(sq, Block):  # noqa: F811
     """Outputs and gradients beside those of the same block in fp32 by autograd, whose operands are not quantised: they point the same way (a cosine of 0.99 a product of
     4-bit operands, up to three of them on the way)."""
     tokens, per, experts, width, hidden, p = 600, 2, 6, 256, 320, 0.1
-    block = Block(sq, tokens, per, experts, width, hidden)
+    block = Block(tokens, per, experts, width, hidden)
     g = torch.Generator(device=DEV).manual_seed(4)
     x = torch.randn(tokens, width, generator=g, device=DEV).bfloat16()
     dy = (torch.randn(tokens, width, generator=g, device=DEV) / tokens).bfloat16()
@@ -683,10 +639,10 @@ def test_a_block_with_experts(sq):  # noqa: F811
         assert cosine > 0.95, (name, cosine)
 
 
-def test_a_block_in_a_graph(sq):  # noqa: F811
+def test_a_block_in_a_graph(sq, Block):  # noqa: F811
     """Captured once and replayed on other choices and another step, beside the same calls made one by one, on a stream of its own."""
     tokens, per, experts = 300, 2, 5
-    block = Block(sq, tokens, per, experts, 128, 192)
+    block = Block(tokens, per, experts, 128, 192)
     x = torch.randn(tokens, 128, device=DEV).bfloat16()
     dy = torch.randn(tokens, 128, device=DEV).bfloat16()
     chosen, weights = choices(1, tokens, per, experts)
