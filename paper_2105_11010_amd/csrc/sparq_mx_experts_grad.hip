@@ -4,16 +4,16 @@
 namespace sparq {
 namespace mx {
 
-// Sums of dy's columns over each expert's rows, 64 columns a workgroup.
+// Sums of dy's columns over each expert's rows, 64 columns (from column `from` on) a workgroup.  16384 x 2048 bf16 among 8 experts 11-15 us (67 MB, 10 at memory's pace).
 constexpr int kSumThreads = 1024;
 template <class T>
-__global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __restrict__ dy, int64_t lddy, const int32_t* __restrict__ offsets, int64_t rows, int N,
+__global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __restrict__ dy, int64_t lddy, const int32_t* __restrict__ offsets, int64_t rows, int N, int from,
                                                                   float* __restrict__ db) {
     typedef ColumnSums<T, kSumThreads> Sums;
     __shared__ float shared[Sums::kFloats];
     int first, n;
     expert_rows(offsets, blockIdx.y, rows, first, n);
-    Sums::run(dy, lddy, first, (int64_t)first + n, N, blockIdx.x * Sums::kColumns, db + (int64_t)blockIdx.y * N, shared);
+    Sums::run(dy, lddy, first, (int64_t)first + n, N, from + blockIdx.x * Sums::kColumns, db + (int64_t)blockIdx.y * N, shared);
 }
 
 // Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them.  bf16: as in sparq_mx_grad.hip.  The others, whose
@@ -131,7 +131,12 @@ extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int
     if (M > 0 && (!coded_ok(x_codes, x_scales) || !tensor_ok(dy, dy_type, lddy, N) || !extent_ok(M, lddy) || !extent_ok(M, K))) return SPARQ_EINVAL;
     const int t = dw_tile(dy_type, M, N, K, experts);
     const int64_t tiles_j = (N + t - 1) / t, tiles_k = (K + t - 1) / t;
-    if (!grad_countable(M, N, experts) || (tiles_j * tiles_k + N) * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
+    // The column sums: by workgroups of the product's launch, which saves a launch, unless dy is so large that these would come last (as in
+    // sparq_mx_grad.hip), or a workgroup of the tiles takes a CU for itself.
+    constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
+    const bool beside = db && M * N <= 1 << (t == 64 ? 22 : 21) && (dy_type == SPARQ_MX_BF16 || t == 64);
+    const int64_t workgroups = tiles_j * tiles_k + (beside ? (N + kColumns - 1) / kColumns : 0);
+    if (!grad_countable(M, N, experts) || workgroups * kGradThreads >= 1ll << 32) return SPARQ_EUNSUPPORTED;
     const hipStream_t s = static_cast<hipStream_t>(stream);
     ExpertGradParams p = grad_params(dy, M > 0 ? lddy : 0, x_codes, x_scales, 8, lddw, N, 0, K, offsets, M);
     p.tiles_j = (int)tiles_j;
@@ -140,18 +145,16 @@ extern "C" sparq_status sparq_mx_experts_dw(const void* dy, int32_t dy_type, int
     // fit the loads' 32-bit offsets.
     p.margin = M == 0 ? 0 : reads_fit(lddy, p.code_pitch) ? (int)((round_up(N, 8) - N + lddy - 1) / lddy) : (int)M;
     p.experts = experts;
-    // The column sums: by workgroups of the product's launch, which saves a launch, unless dy is so large that these would come last (as in
-    // sparq_mx_grad.hip), or a workgroup of the tiles takes a CU for itself.
-    constexpr int kColumns = ColumnSums<float, kGradThreads>::kColumns;
-    const bool beside = db && M * N <= 1 << (t == 64 ? 22 : 21) && (dy_type == SPARQ_MX_BF16 || t == 64);
     p.column_sums = beside ? db : nullptr;
-    const dim3 grid((unsigned)(tiles_j * tiles_k + (beside ? (N + kColumns - 1) / kColumns : 0)), (unsigned)experts);
+    const dim3 grid((unsigned)workgroups, (unsigned)experts);
     const sparq_status done = (dy_type == SPARQ_MX_F32 ? launch_experts_dw_f32 : dy_type == SPARQ_MX_F16 ? launch_experts_dw_f16 : launch_experts_dw_bf16)(
         p, grid, t, dw, dw_type == SPARQ_MX_F32, s);
     if (done != SPARQ_OK || !db || beside) return done;
-    with_type(dy_type, [&](auto y) {
-        typedef decltype(y) T;
-        expert_sums_kernel<T><<<dim3((unsigned)((N + 63) / 64), (unsigned)experts), kSumThreads, 0, s>>>(static_cast<const T*>(dy), p.lddy, offsets, M, N, db);
+    return in_launches((N + 63ll) / 64, kSumThreads, [&](int64_t first, int64_t n) {
+        with_type(dy_type, [&](auto y) {
+            typedef decltype(y) T;
+            expert_sums_kernel<T><<<dim3((unsigned)n, (unsigned)experts), kSumThreads, 0, s>>>(static_cast<const T*>(dy), p.lddy, offsets, M, N, (int)(64 * first), db);
+        });
+        return launch_status();
     });
-    return launch_status();
 }
