@@ -44,6 +44,8 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
     constexpr int kRun = TILE == 64 ? 16 : 32, kRuns = TILE * kGradStep / kGradThreads / kRun;      // a thread's runs of V's values
     constexpr int kUnits = TILE / 32;                        // and of eight values of dy, as many as V's pieces of eight
     constexpr int kPieces = kRun / 8;                        // a run
+    constexpr bool kDeep = kExperts && TILE <= 128;          // V is asked for two steps ahead: a thread's one run of it is written in pieces all over a step
+    constexpr int kSets = kDeep ? 2 : 1;
     constexpr int kBytes = kWideBytes<TILE>;
     typedef short v4s __attribute__((ext_vector_type(4)));
     extern __shared__ __attribute__((aligned(16))) uint8_t lds8[];
@@ -101,7 +103,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // ---- V: a thread has two runs of 32 values, one block each, of rows 4 (lane / 8) + wave and that + 32; or one of row 4 (lane / 4) + wave;
         // or one of 16 values of row lane / 4 + 16 wave
         constexpr int kWords = kRun / (DW ? 4 : 8);
-        uint32_t raw[kRuns][kWords], scale[kRuns];
+        uint32_t raw[kSets][kRuns][kWords], scale[kSets][kRuns];
         constexpr int kAlong = TILE / kRun;
         const int v_row = TILE == 64 ? lane / kAlong + 16 * wave : 4 * (lane / kAlong) + wave;
         int k = k0 + kRun * (lane % kAlong);
@@ -118,10 +120,20 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // zeros as they are written to LDS -- of the step that is written, and of the one that is asked for.
         int rows_written = 0, rows_asked = 0;
         if constexpr (kCut) rows_asked = all.fast_rows(p);
+        int left_v = left;
+        auto advance_v = [&]() __attribute__((always_inline)) {
+            codes_from += left_v > 0 ? codes_step : 0;
+            scales_from += left_v > 0 ? scales_step : 0;
+            --left_v;
+        };
         auto advance = [&]() __attribute__((always_inline)) {
             dy_from += left > 0 ? dy_step : 0;
-            codes_from += left > 0 ? codes_step : 0;
-            scales_from += left > 0 ? scales_step : 0;
+            if constexpr (kDeep) {
+                advance_v();
+            } else {
+                codes_from += left > 0 ? codes_step : 0;
+                scales_from += left > 0 ? scales_step : 0;
+            }
             --left;
             rows_written = rows_asked;
             rows_asked -= kGradStep;
@@ -146,19 +158,19 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
                 for (int e = 0; e < 4; ++e) kept[i][4 * h + e] = w[e];
             }
         };
-        auto load_v = [&](int run, auto checked) __attribute__((always_inline)) {
+        auto load_v = [&](int set, int run, auto checked) __attribute__((always_inline)) {
             if constexpr (kWords == 2) {
                 const v2u w = __builtin_amdgcn_raw_buffer_load_b64((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, 0, 0);
-                raw[run][0] = w[0];
-                raw[run][1] = w[1];
+                raw[kDeep ? set : 0][run][0] = w[0];
+                raw[kDeep ? set : 0][run][1] = w[1];
             }
 #pragma unroll
             for (int h = 0; h < kWords / 4; ++h) {
                 const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) raw[run][4 * h + e] = w[e];
+                for (int e = 0; e < 4; ++e) raw[kDeep ? set : 0][run][4 * h + e] = w[e];
             }
-            scale[run] = __builtin_amdgcn_raw_buffer_load_b8((kCut ? buffer_to(scales_from, scales_end, checked) : buffer(scales_from)), scale_at, (int)(32 * run * p.scale_pitch), 0);
+            scale[kDeep ? set : 0][run] = __builtin_amdgcn_raw_buffer_load_b8((kCut ? buffer_to(scales_from, scales_end, checked) : buffer(scales_from)), scale_at, (int)(32 * run * p.scale_pitch), 0);
         };
         // A tile's row is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
         const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
@@ -186,17 +198,17 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         // values 2 e and 2 e + 1 of the eight of a piece
         v4u decoded;
         float unit;
-        auto decode = [&](int piece, int e, auto checked) __attribute__((always_inline)) {
+        auto decode = [&](int set, int piece, int e, auto checked) __attribute__((always_inline)) {
             const int run = piece / kPieces, at = piece % kPieces;
             if (at == 0 && e == 0) {
-                unit = DW ? unit8_of(scale[run]) : scale_operand(scale[run]);
+                unit = DW ? unit8_of(scale[kDeep ? set : 0][run]) : scale_operand(scale[kDeep ? set : 0][run]);
                 if constexpr (kCut && decltype(checked)::value) unit = v_row + 32 * run < rows_written ? unit : 0.0f;
             }
             if constexpr (DW) {
-                const uint32_t w = raw[run][2 * at + (e >> 1)] >> (16 * (e & 1));
+                const uint32_t w = raw[kDeep ? set : 0][run][2 * at + (e >> 1)] >> (16 * (e & 1));
                 decoded[e] = pack_bf16((float)(int8_t)w * unit, (float)(int8_t)(w >> 8) * unit);
             } else {
-                decoded[e] = pair4_of(raw[run][at], unit, e);
+                decoded[e] = pair4_of(raw[kDeep ? set : 0][run][at], unit, e);
             }
         };
         auto write_v = [&](uint8_t* tile, int piece) __attribute__((always_inline)) {
@@ -241,10 +253,10 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             for (int n = i * kReads / kSlots; n < (i + 1) * kReads / kSlots; ++n) read(set[(q + 1) & 1], lds_dy + read_from * P * kBytes, lds_v + read_from * kBytes, (q + 1) & 3, n);
             for (int u = i * parts / kSlots; u < (i + 1) * parts / kSlots; ++u) {
                 const int piece = first + u / 8;
-                if (u % 2 == 0) decode(piece, u % 8 / 2, checked);
+                if (u % 2 == 0) decode(write_to, piece, u % 8 / 2, checked);
                 if (u % 8 == 7) {
                     write_v(lds_v + write_to * kBytes, piece);
-                    if (piece % kPieces == kPieces - 1) load_v(piece / kPieces, checked);
+                    if (piece % kPieces == kPieces - 1) load_v(write_to, piece / kPieces, checked);
                 }
                 if (u % 8 == 3) {
                     write_dy(lds_dy + write_to * P * kBytes, piece, checked);
@@ -280,15 +292,20 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) load_dy(i, std::true_type{});
 #pragma unroll
-        for (int i = 0; i < kRuns; ++i) load_v(i, std::true_type{});
+        for (int i = 0; i < kRuns; ++i) load_v(0, i, std::true_type{});
+        if constexpr (kDeep) {
+            advance_v();
+#pragma unroll
+            for (int i = 0; i < kRuns; ++i) load_v(1, i, std::true_type{});
+        }
         advance();
         static_assert(kUnits == kPieces * kRuns, "a unit of dy to a piece of V");
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) decode(i, e, std::true_type{});
+            for (int e = 0; e < 4; ++e) decode(0, i, e, std::true_type{});
             write_v(lds_v, i);
-            if (i % kPieces == kPieces - 1) load_v(i / kPieces, std::true_type{});
+            if (i % kPieces == kPieces - 1) load_v(0, i / kPieces, std::true_type{});
             write_dy(lds_dy, i, std::true_type{});
             load_dy(i, std::true_type{});
         }
@@ -298,7 +315,7 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         for (int i = 0; i < kSlots; ++i) between(std::integral_constant<int, 1>{}, 3, i, std::true_type{});
         int64_t s = s_begin;
         if constexpr (kCut)
-            for (; s + 5 < s_fast; s += 2) {                 // (what these ask for, up to a quarter of step s + 4, is of whole steps)
+            for (; s + (kDeep ? 6 : 5) < s_fast; s += 2) {   // (what these ask for, up to a quarter of step s + 4 -- of V s + 5 --, is of whole steps)
                 step(std::integral_constant<int, 0>{}, std::false_type{});
                 step(std::integral_constant<int, 1>{}, std::false_type{});
             }
