@@ -118,10 +118,14 @@ struct Epilogue {
                 }
                 const int col = col0 + 32 * i + 16 * g, n = cols - col;
                 if (kept_codes) {
+                    if (!whole) {                            // (columns past N, which are zeros in the kept form and are not stored)
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) z[e] = e < n ? z[e] : 0.0f;
+                    }
                     uint32_t top = 0;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        const uint32_t m = e < n ? __float_as_uint(z[e]) & 0x7FFFFFFFu : 0u;
+                        const uint32_t m = __float_as_uint(z[e]) & 0x7FFFFFFFu;
                         top = m > top ? m : top;
                     }
                     const auto other = __builtin_amdgcn_permlane32_swap(top, top, false, false);
@@ -131,7 +135,7 @@ struct Epilogue {
                     for (int h = 0; h < 2; ++h) {
                         float v[8];
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = 8 * h + e < n ? z[8 * h + e] : 0.0f;
+                        for (int e = 0; e < 8; ++e) v[e] = z[8 * h + e];
                         const v2u half = codes8_of(v, byte);
                         w[2 * h] = half[0];
                         w[2 * h + 1] = half[1];
