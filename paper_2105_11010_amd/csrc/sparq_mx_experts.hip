@@ -71,11 +71,12 @@ struct ExpertsPlan {
 };
 // What a round of tiles takes (us): one of 256 x 256 a CU, or two of 128 x 128, by the length of the reduction and what comes behind it.  One wavefront a SIMD
 // has nobody to multiply while it makes its results; of two workgroups a CU one does.  (bf16, measured: 8192 x 4096 x 4096, 256 -> 128: 85 -> 97, with gelu 114 -> 105,
-// kept 102 -> 109, both 127 -> 121; 16384 x 4096 x 2048 104 -> 107, 163 -> 121, 136 -> 124, 187 -> 145, residual 140 -> 130; of 1024 76 -> 61.)
+// kept 102 -> 109, both 127 -> 118, residual 100 -> 112; 16384 x 4096 x 2048 104 -> 107, 163 -> 121, 136 -> 124, 187 -> 144, residual 153 -> 133; of 1024 76 -> 61,
+// residual 127 -> 90.)
 static double round_of(int tile, int K, int function, bool residual, bool kept) {
     const bool gelu = function == SPARQ_MX_GELU, silu = function == SPARQ_MX_SILU;
-    if (tile == 256) return 11.0 + 7.6 * K / 1024 + (gelu ? 14.7 : silu ? 8.0 : 0.0) + (residual ? 5.0 : 0.0) + (kept ? 8.0 : 0.0);
-    return 1.9 + 5.7 * K / 1024 + (gelu ? 1.8 : silu ? 1.0 : 0.0) + (residual ? 2.8 : 0.0) + (kept ? 2.0 : 0.0);
+    if (tile == 256) return 11.0 + 7.6 * K / 1024 + (gelu ? 14.7 : silu ? 8.0 : 0.0) + (residual ? 10.0 : 0.0) + (kept ? 8.0 : 0.0);
+    return 1.9 + 5.7 * K / 1024 + (gelu ? 1.8 : silu ? 1.0 : 0.0) + (residual ? 3.4 : 0.0) + (kept ? 2.0 : 0.0);
 }
 static ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offsets, int function, bool residual, bool kept) {
     ExpertsPlan p = {};
