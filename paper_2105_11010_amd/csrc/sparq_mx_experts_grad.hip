@@ -18,8 +18,9 @@ __global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __res
 
 // Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them.  bf16: as in sparq_mx_grad.hip.  The others, whose
 // parts of dy leave LDS for one tile of 128 a CU, and three (fp16) or two of 64: a round of the smaller makes 0.86 or 0.6 of the time of one of the larger (us, 128 -> 64, fp16:
-// dx 2048 x 2048 x 2048 to 4 experts 85 -> 64, 8192 x 1024 x 1024 to 8 67 -> 61, 16384 x 2048 x 2048 to 8 372 -> 401; dw of 4275 x 777 x 520 to 20 40 -> 34, 2048 x 2048 x 2048
-// to 4 71 -> 80); dw's tiles, many and short, come without rounds.
+// dx 2048 x 2048 x 2048 to 4 experts 77 -> 62, 8192 x 1024 x 1024 to 8 65 -> 58, 16384 x 2048 x 2048 to 8 347 -> 402; dw of 4275 x 777 x 520 to 20 39 -> 35, 2048 x 2048 x 2048
+// to 4 70 -> 80); dw's tiles, many and short, come without rounds.  What the experts leave empty of their last tiles it takes for half a tile each: fp16 dx of 16384 x 512 x 512
+// to 64 goes in tiles of 128, 39, for 34.5.
 static int grad_tile(int dy_type, int64_t tiles256, int64_t tiles128, int64_t tiles64, int64_t steps, bool dw) {
     if (tiles128 < 192) return 64;
     if (dy_type == SPARQ_MX_BF16) return !(dw && steps <= 4) && 3 * ((tiles256 + 255) / 256) <= 2 * ((tiles128 + 511) / 512) ? 256 : 128;
@@ -109,7 +110,7 @@ extern "C" sparq_status sparq_mx_experts_dx(const void* dy, int32_t dy_type, int
             p, dim3((unsigned)(rows * columns)), tile, dx, dx_type == SPARQ_MX_F32, s);
     };
     // Tiles of 256 x 256, one a CU at a time: where the experts' last ones, which are about half empty, would make a round more, what is left behind whole tiles goes in tiles
-    // of 64, in a launch of its own (us, one launch -> two: 16384 x 2048 x 2048 to 8 experts, uneven, 155 -> 137, 16384 x 4096 x 1024 to 4 178 -> 135; the second takes 22 and 45, a step of
+    // of 64, in a launch of its own (us, one launch -> two: 16384 x 2048 x 2048 to 8 experts, uneven, 149 -> 138, 16384 x 4096 x 1024 to 4 174 -> 130; the second takes 22 and 45, a step of
     // its 32 and 64 after the other).
     const int64_t half = (experts + 1) / 2, whole = M / 256 > half ? (M / 256 - half) * tiles_k : 0;
     if (t != 256 || bytes || rest_k * experts * 4 * kGradThreads >= 1ll << 32 || ((M / 256 + half) * tiles_k + 255) / 256 <= (whole + 255) / 256)
