@@ -48,13 +48,8 @@ struct ExpertGradParams : GradParams {
         if (column_sums) p.column_sums = column_sums + (int64_t)expert * J;
         return out + (int64_t)expert * J * ldo;
     }
-    // dw: as many of the expert's rows as are read in whole runs, those whose runs end inside dy (own_rows); the end of dy's last row; and what is left
-    // behind them.
+    // dw: as many of the expert's rows as are read in whole runs, those whose runs end inside dy (own_rows), and what is left behind them.
     __device__ __forceinline__ int fast_rows(const GradParams& p) const { return (int)p.slab; }
-    template <class T>
-    __device__ __forceinline__ const uint8_t* dy_end(T) const {
-        return reinterpret_cast<const uint8_t*>(static_cast<const T*>(dy) + (rows - 1) * lddy + J);
-    }
     template <class T>
     __device__ __forceinline__ void leave_fast(GradParams& p) const {
         const int64_t n = p.slab;

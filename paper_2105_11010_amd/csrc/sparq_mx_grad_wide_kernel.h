@@ -87,10 +87,11 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         constexpr int kAcross = TILE / 8, kRowsAtOnce = kGradThreads / kAcross;
         constexpr int kSize = sizeof(T), kKept = 2 * kSize;
         uint32_t kept[kUnits][kKept];
-        uint32_t dy_at[DW ? 1 : kUnits];
+        uint32_t dy_at[DW ? 1 : kUnits], dy_column = 0;
         if constexpr (DW) {
             int64_t j = j0 + 8 * (t % kAcross);
             j = j < p.J ? j : j0;                            // (columns past the last one make results that are not stored)
+            dy_column = (uint32_t)((j - j0) * kSize);
             dy_at[0] = (uint32_t)((t / kAcross * p.lddy + (j - j0)) * kSize);
         } else {
             const int64_t last = p.J - 1 - j0;
@@ -116,8 +117,8 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
         const uint32_t dy_step = DW ? (uint32_t)(kGradStep * p.lddy * kSize) : kGradStep * kSize, codes_step = (uint32_t)(kGradStep * p.code_pitch);
         const uint32_t scales_step = (uint32_t)(kGradStep * p.scale_pitch);
         int left = (int)(s_fast - s_begin) - 1;
-        // (kCut) A step's rows may be fewer than 64: the next expert's rows behind them, or what lies past the buffers' ends and comes as zeros, are made
-        // zeros as they are written to LDS -- of the step that is written, and of the one that is asked for.
+        // (kCut) A step's rows may be fewer than 64: what comes for the others -- the next expert's rows of V, or what lies past V's end and comes as zeros -- is made
+        // zeros as it is written to LDS.  Of the step that is written, and of the one that is asked for.
         int rows_written = 0, rows_asked = 0;
         if constexpr (kCut) rows_asked = all.fast_rows(p);
         int left_v = left;
@@ -144,21 +145,29 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             const int64_t bytes = end - from;
             return __builtin_amdgcn_make_buffer_rsrc((void*)from, 0, decltype(checked)::value && bytes < 0x7FFFFFFF ? (int)bytes : 0x7FFFFFFF, 0x00020000);
         };
-        const uint8_t *dy_end = nullptr, *codes_end = nullptr, *scales_end = nullptr;
+        const uint8_t *codes_end = nullptr, *scales_end = nullptr;
         if constexpr (kCut) {
-            dy_end = all.dy_end(T{});
             codes_end = all.codes + all.rows * p.code_pitch;
             scales_end = all.scales + all.rows * p.scale_pitch;
         }
+        // (dy's rows past the fast ones are not asked for: their lanes read the step's first row, which is one.  Its end is no border a load could be held against: rows may
+        // be an odd number of elements, and words lie across it.)
         auto load_dy = [&](int i, auto checked) __attribute__((always_inline)) {
+            constexpr bool kCheck = kCut && decltype(checked)::value;
+            const uint32_t row = DW ? (uint32_t)(kRowsAtOnce * i * p.lddy * kSize) : 0;
+            uint32_t at = dy_at[DW ? 0 : i];
+            if constexpr (kCheck) at = kRowsAtOnce * i + t / kAcross < rows_asked ? at + row : dy_column;
 #pragma unroll
             for (int h = 0; h < kKept / 4; ++h) {
-                const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(dy_from, dy_end, checked) : buffer(dy_from)), dy_at[DW ? 0 : i], (DW ? (int)(kRowsAtOnce * i * p.lddy * kSize) : 0) + 16 * h, 0);
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128(buffer(dy_from), at, (kCheck ? 0 : (int)row) + 16 * h, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) kept[i][4 * h + e] = w[e];
             }
         };
+        // (V's end is one.  A load's offset is the sum of a lane's part and a scalar one, and the lane's alone is held against the buffer's size: the row is in it.)
         auto load_v = [&](int set, int run, auto checked) __attribute__((always_inline)) {
+            const uint32_t row = (uint32_t)(32 * run * p.code_pitch), scale_row = (uint32_t)(32 * run * p.scale_pitch);
+            const uint32_t in_lane = kCut && decltype(checked)::value ? row : 0, scale_in_lane = kCut && decltype(checked)::value ? scale_row : 0;
             if constexpr (kWords == 2) {
                 const v2u w = __builtin_amdgcn_raw_buffer_load_b64((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, 0, 0);
                 raw[kDeep ? set : 0][run][0] = w[0];
@@ -166,11 +175,12 @@ __global__ __launch_bounds__(kGradThreads, (kWidePerCu<T, TILE>)) void grad_wide
             }
 #pragma unroll
             for (int h = 0; h < kWords / 4; ++h) {
-                const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at, (int)(32 * run * p.code_pitch) + 16 * h, 0);
+                const v4u w = __builtin_amdgcn_raw_buffer_load_b128((kCut ? buffer_to(codes_from, codes_end, checked) : buffer(codes_from)), v_at + in_lane, (int)(row - in_lane) + 16 * h, 0);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) raw[kDeep ? set : 0][run][4 * h + e] = w[e];
             }
-            scale[kDeep ? set : 0][run] = __builtin_amdgcn_raw_buffer_load_b8((kCut ? buffer_to(scales_from, scales_end, checked) : buffer(scales_from)), scale_at, (int)(32 * run * p.scale_pitch), 0);
+            scale[kDeep ? set : 0][run] = __builtin_amdgcn_raw_buffer_load_b8((kCut ? buffer_to(scales_from, scales_end, checked) : buffer(scales_from)), scale_at + scale_in_lane,
+                                                                              (int)(scale_row - scale_in_lane), 0);
         };
         // A tile's row is permuted in its 16-byte units, which keeps both the turning reads and the writes apart in the banks.
         const auto permuted = [](int row, int chunk) __attribute__((always_inline)) {
