@@ -81,7 +81,8 @@ __global__ __launch_bounds__(WAVES * 64) void experts_few_kernel(O* __restrict__
         v4i a[MT][4];
         v4u as[MT];
     };
-    // Columns past N, blocks past the last one and groups past the row's lie past the buffer's end: they come as zeros, without a request.
+    // Columns past N, blocks past the last one and groups past the row's lie past the buffer's end: they come as zeros, without a request.  (Of no rows the scalar
+    // part of the offset is 0 too: what it would leave of a size of 0, taken as a number without a sign, is no end.)
     auto fetch = [&](Weights& o, int block, int group) __attribute__((always_inline)) {
         const int n0 = (block0 + block) * kFewColumns, rows = block >= blocks || group >= p.groups ? 0 : p.N - n0 < kFewColumns ? p.N - n0 : kFewColumns;
         const auto buffer = [&](const uint8_t* base, int64_t pitch) __attribute__((always_inline)) {
@@ -91,9 +92,9 @@ __global__ __launch_bounds__(WAVES * 64) void experts_few_kernel(O* __restrict__
 #pragma unroll
         for (int s = 0; s < 4; ++s) {
             const int step = 4 * group + s < p.last_step ? 4 * group + s : p.last_step;          // (a row's scales are zeros past its end)
-            o.w[s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(codes, r * (int)p.code_pitch + 16 * g, step * 64, 0));
+            o.w[s] = __builtin_bit_cast(v4i, __builtin_amdgcn_raw_buffer_load_b128(codes, r * (int)p.code_pitch + 16 * g, rows ? step * 64 : 0, 0));
         }
-        o.ws = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(scales, r * (int)p.scale_pitch, group * 16, 0));
+        o.ws = __builtin_bit_cast(v4u, __builtin_amdgcn_raw_buffer_load_b128(scales, r * (int)p.scale_pitch, rows ? group * 16 : 0, 0));
     };
     auto fetch_rows = [&](Rows& o, int group) __attribute__((always_inline)) {
         group = group < p.groups ? group : p.groups - 1;

@@ -48,3 +48,9 @@ def test_weights_gradient_of_wider_types(checker, t, tile, J, K, lddy, before, r
 @pytest.mark.parametrize("rows,N,K,lddy", [(1, 64, 1, 64), (70, 200, 300, 203), (300, 64, 129, 65), (257, 130, 513, 130), (3, 5, 40, 5)])
 def test_inputs_gradient(checker, t, tile, rows, N, K, lddy):
     check(checker, "dx", t, tile, rows, N, K, lddy)
+
+
+# Blocks of columns past the last one, groups past a row's last one (wavefronts without any, a row of several groups a wavefront), columns past N.
+@pytest.mark.parametrize("N,K,M,blocks", [(40, 600, 5, 2), (40, 600, 5, 1), (17, 64, 16, 1), (65, 2500, 7, 3), (100, 5000, 3, 8), (16, 512, 1, 1), (1, 1, 1, 8), (130, 4096, 2, 4)])
+def test_few_rows(checker, N, K, M, blocks):
+    check(checker, "few", N, K, M, blocks)
