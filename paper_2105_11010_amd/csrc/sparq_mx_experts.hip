@@ -6,28 +6,11 @@ namespace sparq {
 namespace mx {
 
 // ---- tiles of rows ---------------------------------------------------------------------
-// Each expert's rows in tiles of their own, one workgroup, a thread an expert.
-constexpr int kTableThreads = SPARQ_MX_EXPERTS_MOST;
+// Each expert's rows in tiles of their own.
 __global__ __launch_bounds__(kTableThreads) void tiles_kernel(const int32_t* __restrict__ offsets, int experts, int64_t rows, int tile, int most,
                                                               ExpertTile* __restrict__ table) {
-    __shared__ int sums[kTableThreads / 64];
-    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
-    int first = 0, n = 0;
-    if (e < experts) expert_rows(offsets, e, rows, first, n);
-    const int tiles = (n + tile - 1) / tile;
-    int sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-        const int v = __shfl_up(sum, d);
-        if (lane >= d) sum += v;
-    }
-    if (lane == 63) sums[wave] = sum;
-    __syncthreads();
-    int before = sum - tiles;
-    for (int w = 0; w < wave; ++w) before += sums[w];
-    for (int i = 0; i < tiles; ++i)
-        if (before + i < most) table[1 + before + i] = {first + i * tile, n - i * tile < tile ? n - i * tile : tile, e, 0};
-    if (e == kTableThreads - 1) table[0] = {before + tiles < most ? before + tiles : most, 0, 0, 0};
+    __shared__ int64_t sums[kTableThreads / 64];
+    write_tiles(offsets, experts, rows, tile, most, table, sums);
 }
 sparq_status launch_tiles(const int32_t* offsets, int experts, int64_t rows, int tile, void* table, hipStream_t stream) {
     tiles_kernel<<<1, kTableThreads, 0, stream>>>(offsets, experts, rows, tile, (int)most_tiles(rows, experts, tile), static_cast<ExpertTile*>(table));

@@ -10,6 +10,8 @@ namespace mx {
 struct ExpertTile {
     int32_t row, rows, expert, unused;
 };
+// Tiles that n rows make (n + tile need not fit 32 bits)
+inline constexpr int tiles_in(int n, int tile) { return n / tile + (n % tile != 0); }
 // As many tiles as any division of the rows can make
 inline int64_t most_tiles(int64_t rows, int experts, int tile) { return rows / tile + (rows < experts ? rows : experts); }
 constexpr int kExpertsOfLanes = 64;
@@ -38,7 +40,7 @@ __device__ __forceinline__ LaneTiles tiles_of_lanes(const int32_t* offsets, int 
         t.first += n;
         t.rows -= n;
     }
-    t.sum = (t.rows + tile - 1) / tile;
+    t.sum = tiles_in(t.rows, tile);
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const int v = __shfl_up(t.sum, d);
@@ -49,8 +51,29 @@ __device__ __forceinline__ LaneTiles tiles_of_lanes(const int32_t* offsets, int 
 __device__ __forceinline__ int tile_count(const LaneTiles& t) { return __builtin_amdgcn_readlane(t.sum, 63); }
 __device__ __forceinline__ ExpertTile expert_tile(const LaneTiles& t, int tile, uint32_t i) {
     const int e = __builtin_ctzll(__ballot((uint32_t)t.sum > i) | 1ull << 63), rows = __builtin_amdgcn_readlane(t.rows, e);
-    const int in = ((int)i - (__builtin_amdgcn_readlane(t.sum, e) - (rows + tile - 1) / tile)) * tile;
+    const int in = ((int)i - (__builtin_amdgcn_readlane(t.sum, e) - tiles_in(rows, tile))) * tile;
     return {__builtin_amdgcn_readlane(t.first, e) + in, rows - in < tile ? rows - in : tile, e, 0};
+}
+// The table, by one workgroup, a thread an expert; sums: one of each wavefront.  Offsets that fall can make more tiles than fit 32 bits: `most` of them are written.
+constexpr int kTableThreads = SPARQ_MX_EXPERTS_MOST;
+__device__ __forceinline__ void write_tiles(const int32_t* offsets, int experts, int64_t rows, int tile, int most, ExpertTile* table, int64_t* sums) {
+    const int e = threadIdx.x, lane = e & 63, wave = e >> 6;
+    int first = 0, n = 0;
+    if (e < experts) expert_rows(offsets, e, rows, first, n);
+    const int tiles = tiles_in(n, tile);
+    int64_t sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+        const int64_t v = __shfl_up(sum, d);
+        if (lane >= d) sum += v;
+    }
+    if (lane == 63) sums[wave] = sum;
+    __syncthreads();
+    int64_t before = sum - tiles;
+    for (int w = 0; w < wave; ++w) before += sums[w];
+    const int64_t left = most - before;
+    for (int i = 0; i < tiles && i < left; ++i) table[1 + before + i] = {first + i * tile, n - i * tile < tile ? n - i * tile : tile, e, 0};
+    if (e == kTableThreads - 1) table[0] = {tiles < left ? (int)(before + tiles) : most, 0, 0, 0};
 }
 #if defined(__HIP_DEVICE_COMPILE__)
 // (By the scalar cache: the table does not change while a kernel reads it.)
