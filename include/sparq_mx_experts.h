@@ -3,7 +3,7 @@
  * product: the router's choices sorted by expert, rows on their way to their experts and back, the experts' products with
  * bias, activation and residual, their gradients, and dropout.  Formats, storage and conventions are those of sparq_mx.h.
  *
- * A token t has `per` slots, s = t per + j, each with the number of an expert, of a place and of a weight.  Sorted rows lie
+ * A token t has `per` slots (up to 2^30), s = t per + j, each with the number of an expert, of a place and of a weight.  Sorted rows lie
  * expert after expert: expert e has the rows offsets[e] to offsets[e + 1] - 1.  Offsets, places and choices are int32 in
  * device memory and are never read by the host, so that a call can be captured into a graph and replayed on other choices.
  *   - offsets: [experts + 1], rising from 0 to at most the rows of the tensors they divide; what lies outside is cut off at

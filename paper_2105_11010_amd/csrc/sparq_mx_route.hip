@@ -192,10 +192,11 @@ __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restr
     }
 }
 
-// false: more tokens than a call counts
+constexpr int kMostSlots = 1 << 30;              // of a token: four at a time, they are counted in 32 bits
+// false: more tokens or slots than a call counts
 static bool route_params(int64_t tokens, int K, int per, const int32_t* place, int64_t rows, RouteParams* p) {
     const int64_t chunks = (K + kScaleUnit - 1) / kScaleUnit, items = tokens * chunks;
-    if (tokens >= (1ll << 31) || items >= (1ll << 31) || tokens * per >= (1ll << 40)) return false;
+    if (tokens >= (1ll << 31) || items >= (1ll << 31) || per > kMostSlots || tokens * per >= (1ll << 40)) return false;
     *p = {};
     p->place = place;
     p->code4_pitch = code_pitch(K, 4);

@@ -80,6 +80,16 @@ def test_more_than_a_call_counts(call, at, value):
     assert getattr(sq.lib, "sparq_mx_" + name)(*args) == EUNSUPPORTED
 
 
+@pytest.mark.parametrize("call,at", [(1, 6), (2, 6), (3, 5), (4, 4), (5, 4)])
+def test_more_slots_a_token_than_a_call_counts(call, at):
+    """Their number and four more have to fit 32 bits."""
+    name, args, _ = CALLS[call]
+    for per in ((1 << 30) + 1, (1 << 31) - 1):
+        args = list(args)
+        args[at] = per
+        assert getattr(sq.lib, "sparq_mx_" + name)(*args) == EUNSUPPORTED
+
+
 def test_an_expert_without_offsets_is_alone():
     name, args, _ = CALLS[6]
     args = list(args)
