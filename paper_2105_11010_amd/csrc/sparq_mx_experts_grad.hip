@@ -1,5 +1,6 @@
-// The experts' products, backward: entry points and the choice of tiles (include/sparq_mx_experts.h).
+// The experts' products, backward: entry points (include/sparq_mx_experts.h).
 #include "sparq_mx_experts_grad.h"
+#include "sparq_mx_experts_plan.h"
 
 namespace sparq {
 namespace mx {
@@ -16,28 +17,6 @@ __global__ __launch_bounds__(kSumThreads) void expert_sums_kernel(const T* __res
     Sums::run(dy, lddy, first, (int64_t)first + n, N, from + blockIdx.x * Sums::kColumns, db + (int64_t)blockIdx.y * N, shared);
 }
 
-// Tiles of 256 (bf16), 128 or 64 results along either side, by the rounds that 256 CUs make of them.  bf16: as in sparq_mx_grad.hip.  The others, whose
-// parts of dy leave LDS for one tile of 128 a CU, and three (fp16) or two of 64: a round of the smaller makes 0.86 or 0.6 of the time of one of the larger (us, 128 -> 64, fp16:
-// dx 2048 x 2048 x 2048 to 4 experts 77 -> 62, 8192 x 1024 x 1024 to 8 65 -> 58, 16384 x 2048 x 2048 to 8 347 -> 402; dw of 4275 x 777 x 520 to 20 39 -> 35, 2048 x 2048 x 2048
-// to 4 70 -> 80); dw's tiles, many and short, come without rounds.  What the experts leave empty of their last tiles it takes for half a tile each: fp16 dx of 16384 x 512 x 512
-// to 64 goes in tiles of 128, 39, for 34.5.
-static int grad_tile(int dy_type, int64_t tiles256, int64_t tiles128, int64_t tiles64, int64_t steps, bool dw) {
-    if (tiles128 < 192) return 64;
-    if (dy_type == SPARQ_MX_BF16) return !(dw && steps <= 4) && 3 * ((tiles256 + 255) / 256) <= 2 * ((tiles128 + 511) / 512) ? 256 : 128;
-    const int places64 = dy_type == SPARQ_MX_F16 ? 768 : 512;
-    const double round64 = dy_type == SPARQ_MX_F16 ? 0.86 : 0.6;
-    const double rounds128 = dw ? tiles128 / 256.0 : (double)((tiles128 + 255) / 256);
-    const double rounds64 = dw ? (double)tiles64 / places64 : (double)((tiles64 + places64 - 1) / places64);
-    return rounds64 * round64 < rounds128 ? 64 : 128;
-}
-static int dx_tile(int dy_type, int64_t M, int K, int experts) {
-    const auto tiles = [&](int t) { return (M / t + experts / 2 + 1) * ((K + t - 1) / t); };
-    return grad_tile(dy_type, tiles(256), tiles(128), tiles(64), 0, false);
-}
-static int dw_tile(int dy_type, int64_t M, int N, int K, int experts) {
-    const auto tiles = [&](int64_t t) { return experts * ((N + t - 1) / t) * ((K + t - 1) / t); };
-    return grad_tile(dy_type, tiles(256), tiles(128), tiles(64), (M / experts + kGradStep - 1) / kGradStep, true);
-}
 static size_t dx_bytes(int64_t M, int experts) { return experts > kExpertsOfLanes ? table_bytes(M, experts) : 0; }
 static bool grad_sizes_ok(int64_t M, int64_t N, int64_t K, int64_t experts) {
     return sizes_ok(M, K) && N >= 1 && N <= kMaxK && M < (1ll << 40) && experts_ok((int)experts);
