@@ -7,7 +7,8 @@
  * expert after expert: expert e has the rows offsets[e] to offsets[e + 1] - 1.  Offsets, places and choices are int32 in
  * device memory and are never read by the host, so that a call can be captured into a graph and replayed on other choices.
  *   - offsets: [experts + 1], rising from 0 to at most the rows of the tensors they divide; what lies outside is cut off at
- *     these borders by the kernels.  Rows at offsets[experts] and behind belong to nobody: no call reads or writes them.
+ *     these borders by the kernels.  Rows at offsets[experts] and behind belong to nobody: no call writes them and no result
+ *     depends on what they hold, but they may be read, as may be rows that no slot has.
  *   - place: [tokens][per], a slot's sorted row; one outside of [0, rows) is a slot that was refused, which has no row.  No
  *     two slots may have the same row.
  */

@@ -74,6 +74,50 @@ def test_the_same_rows_in_any_company_of_one_kernel(sq, counts, N, K, f):  # noq
     assert torch.equal(y[a:b], z[: b - a]) and bool((z[b - a:] == 7).all())
 
 
+@pytest.mark.parametrize("t", TYPES)
+@pytest.mark.parametrize("counts,N,K", [([3, 0, 7], 40, 130), ([100, 61, 33], 72, 200), ([700, 0, 813], 1030, 300), ([2000, 300, 657], 1672, 1032)])
+def test_what_nobodys_rows_hold(sq, t, counts, N, K):  # noqa: F811
+    """Not numbers, or zeros: the same results to the bit, and what lies there in the results stays."""
+    g = torch.Generator(DEV).manual_seed(K)
+    own, behind, experts = sum(counts), 37, len(counts)
+    M, offsets = own + behind, ints(offsets_of(counts))
+    coded = lambda rows, n, bits: [torch.zeros(rows, p, dtype=torch.uint8, device=DEV) for p in (sq.sparq_mx_code_bytes(n, bits), sq.sparq_mx_scale_bytes(n))]      # noqa: E731
+    x, dy, r = (torch.randn(M, n, generator=g, device=DEV).to(TYPES[t]) for n in (K, N, N))
+    w, x4, x8 = coded(experts * N, K, 4), coded(M, K, 4), coded(M, K, 8)
+    sq.sparq_mx_quantize(torch.randn(experts * N, K, generator=g, device=DEV), *w)
+    sq.sparq_mx_quantize(x, *x4, *x8)
+    place = torch.randperm(own, generator=g, device=DEV).int().view(own, 1)
+    place[::5] = -1
+    place[place == 0] = -1                                   # (refused slots' lanes read row 0, which nobody has here)
+    ws = torch.empty(max(f(M, N, K, experts) for f in (sq.sparq_mx_experts_linear_workspace_bytes, sq.sparq_mx_experts_dx_workspace_bytes)), dtype=torch.uint8, device=DEV)
+    results = []
+    for value, scale, code in ((0.0, 0, 0), (float("nan"), 255, 0x81)):
+        for v in (x, dy, r):
+            v[own:] = value
+        for codes, scales in (x4, x8):
+            codes[own:], scales[own:] = code, scale
+        there = torch.zeros(own, dtype=torch.bool, device=DEV)
+        there[place[place >= 0].long()] = True
+        rows = torch.where(there[:, None], dy[:own], torch.full_like(dy[:own], value))
+        y, z, dx, kept = (torch.full((M, n), 7.0, dtype=TYPES[t], device=DEV) for n in (N, N, K, N))
+        kept8 = [torch.full_like(v, 0xA5) for v in coded(M, N, 8)]
+        dw, db, dweights = (torch.full(s, 7.0, device=DEV) for s in ((experts * N, K), (experts, N), (own, 1)))
+        back = torch.full((own, N), 7.0, dtype=TYPES[t], device=DEV)
+        sq.sparq_mx_experts_linear(x, *w, y, offsets=offsets, function="silu", residual=r, workspace=ws)
+        sq.sparq_mx_experts_gemm(*x4, *w, K, z, offsets=offsets, workspace=ws)
+        sq.sparq_mx_experts_gemm(*x4, *w, K, kept, offsets=offsets, function="gelu", kept_codes=kept8[0], kept_scales=kept8[1], workspace=ws)
+        sq.sparq_mx_experts_dx(dy, offsets, *w, dx, workspace=ws)
+        sq.sparq_mx_experts_dw(dy, offsets, *x8, dw, db=db)
+        sq.sparq_mx_combine(rows, place, back)
+        sq.sparq_mx_combine_grad(dy[:own], place, x=rows, dweights=dweights)
+        for v in (y, z, dx, kept):
+            assert bool((v[own:] == 7).all())
+        assert all(bool((v[own:] == 0xA5).all()) for v in kept8)
+        results.append([y, z, dx, kept, *kept8, dw, db, back, dweights])
+    for i, (a, b) in enumerate(zip(*results)):
+        assert torch.equal(a, b) and (not a.dtype.is_floating_point or bool(a.isfinite().all())), i
+
+
 # ---- sort --------------------------------------------------------------------------------------------------------------------
 # One workgroup whose wavefronts have several ranges' worth; and more slots than 4096 (2048 of more than 512 experts) wavefronts take 128 of.
 @pytest.mark.parametrize("slots,experts", [(2049, 8), (3000, 64), (4095, 300), (4096, 1024), (4097, 5), (524289, 8), (600001, 256), (300001, 1024), (2500003, 37)])
