@@ -81,19 +81,21 @@ inline void with_type(int type, F&& f) {
 
 #if defined(__HIPCC__)
 // ---- eight neighbouring elements, from any address of an element -----------------
-typedef v4u v4u_at4 __attribute__((aligned(4)));
-typedef v4u v4u_at2 __attribute__((aligned(2)));
+// (As members: as a template's argument a type loses its alignment, and the compiler would take such an address for a multiple of 16.)
+template <int BYTES> struct Unaligned;
+template <> struct Unaligned<4> { typedef v4u Word __attribute__((aligned(4))); };
+template <> struct Unaligned<2> { typedef v4u Word __attribute__((aligned(2))); };
 
 // NT: non-temporal, for what is streamed once and is not to stay in the caches (Streaming above).
 template <bool NT, class T>
 __device__ __forceinline__ v4u word_at(const T* p) {
-    typedef std::conditional_t<sizeof(T) == 4, const v4u_at4, const v4u_at2> V;
+    typedef const typename Unaligned<sizeof(T)>::Word V;
     if constexpr (NT) return __builtin_nontemporal_load(reinterpret_cast<V*>(p));
     else return *reinterpret_cast<V*>(p);
 }
 template <bool NT, class T>
 __device__ __forceinline__ void word_to(T* p, v4u w) {
-    typedef std::conditional_t<sizeof(T) == 4, v4u_at4, v4u_at2> V;
+    typedef typename Unaligned<sizeof(T)>::Word V;
     if constexpr (NT) __builtin_nontemporal_store(w, reinterpret_cast<V*>(p));
     else *reinterpret_cast<V*>(p) = w;
 }

@@ -2,6 +2,7 @@
 //   experts_reads_check dw TYPE TILE J K lddy before rows behind      two experts with rows, and rows that nobody has behind them
 //   experts_reads_check dx TYPE TILE rows N K lddy                     one expert
 //   experts_reads_check few N K M blocks                               a layer of few rows
+//   experts_reads_check gemm TILE N K rows rows                        two experts, and the last of the weights' rows
 // Prints "ok <loads>" or what lies outside.  A load's offset has two parts.  Which of them meets the buffer's size is told in two ways: the vector part alone; or the
 // vector part against the size less the scalar part, in 32 bits without a sign.  A load that either of them lets through may reach memory.
 #define __shared__
@@ -10,7 +11,7 @@
 #include <stdlib.h>
 
 #include "../paper_2105_11010_amd/csrc/sparq_mx_experts_grad.h"
-#include "../paper_2105_11010_amd/csrc/sparq_mx_experts_few_kernel.h"
+#include "../paper_2105_11010_amd/csrc/sparq_mx_experts_gemm.h"
 
 using namespace sparq::mx;
 
@@ -140,6 +141,39 @@ static void few(int N, int K, int M, int blocks) {
         gpu::run_threads(WAVES * 64, dim3(block), [&] { experts_few_kernel<float, void, MT, WAVES, SINGLE>(reinterpret_cast<float*>(y.begin), p); });
 }
 
+template <int TILE>
+static void gemm(int N, int K, int first, int second) {
+    const int64_t M = first + second;
+    Tensor a(M * code_pitch(K, 4)), as(M * scale_pitch(K)), w(2 * N * code_pitch(K, 4)), ws(2 * N * scale_pitch(K)), y(M * N * 4);
+    tensors = {a, as, w, ws};
+    std::vector<ExpertTile> table(1);
+    const int32_t offsets[] = {0, first, first + second};
+    for (int e = 0; e < 2; ++e)
+        for (int row = offsets[e]; row < offsets[e + 1]; row += TILE) table.push_back({row, offsets[e + 1] - row < TILE ? offsets[e + 1] - row : TILE, e, 0});
+    table[0].row = (int)table.size() - 1;
+    ExpertGemmParamsOf<SPARQ_MX_NONE> p = {};
+    p.a = a.begin;
+    p.as = as.begin;
+    p.w = w.begin;
+    p.ws = ws.begin;
+    p.M = M;
+    p.N = N;
+    p.ldy = N;
+    p.code_pitch = (uint32_t)code_pitch(K, 4);
+    p.scale_pitch = (uint32_t)scale_pitch(K);
+    p.tiles_m = (uint32_t)most_tiles(M, 2, TILE);
+    p.tiles_n = (uint32_t)((N + TILE - 1) / TILE);
+    p.steps = p.steps_per_part = (int)sparq::round_up((K + kCodeUnit - 1) / kCodeUnit, 4);
+    p.items = p.tiles_m * p.tiles_n;
+    p.table = table.data();
+    p.offsets = offsets;
+    p.experts = 2;
+    p.epilogue.function = SPARQ_MX_NONE;
+    gridDim = dim3(2);                           // (workgroups that take one tile after the other)
+    for (int block = 0; block < 2; ++block)
+        gpu::run_threads(kGemmThreads, dim3(block), [&] { gemm_kernel<float, TILE, TILE, ExpertGemmParamsOf<SPARQ_MX_NONE>>(reinterpret_cast<float*>(y.begin), p); });
+}
+
 int main(int argc, char** argv) {
     std::vector<int> n;
     for (int i = 0; i < argc; ++i) n.push_back(atoi(argv[i]));
@@ -150,6 +184,8 @@ int main(int argc, char** argv) {
     } else if (argc == 6 && !strcmp(argv[1], "few")) {
         const int groups = (n[3] + kScaleUnit - 1) / kScaleUnit;
         (groups <= 4 ? few<1, 4, true> : groups <= 8 ? few<1, 8, true> : few<1, 8, false>)(n[2], n[3], n[4], n[5]);
+    } else if (argc == 7 && !strcmp(argv[1], "gemm")) {
+        (n[2] == 256 ? gemm<256> : n[2] == 128 ? gemm<128> : gemm<64>)(n[3], n[4], n[5], n[6]);
     } else {
         return 2;
     }

@@ -106,6 +106,8 @@ void load(const Buffer& b, uint32_t vector, uint32_t scalar, int bytes);       /
 inline u4 load16(const Buffer& b, uint32_t v, uint32_t s, int) { return load(b, v, s, 16), u4{}; }
 inline u2 load8(const Buffer& b, uint32_t v, uint32_t s, int) { return load(b, v, s, 8), u2{}; }
 inline uint32_t load4(const Buffer& b, uint32_t v, uint32_t s, int) { return load(b, v, s, 4), 0; }
+template <class P>
+inline void load_lds(const Buffer& b, const P&, int bytes, uint32_t v, uint32_t s, int at, int) { load(b, v + at, s, bytes); }
 inline uint8_t load1(const Buffer& b, uint32_t v, uint32_t s, int) { return load(b, v, s, 1), 0; }
 
 struct Nothing {                                 // of any type
@@ -146,6 +148,8 @@ inline float __fmul_rn(float a, float b) { return a * b; }
 #define __builtin_amdgcn_raw_buffer_load_b64 gpu::load8
 #define __builtin_amdgcn_raw_buffer_load_b32 gpu::load4
 #define __builtin_amdgcn_raw_buffer_load_b8 gpu::load1
+#define __builtin_amdgcn_raw_ptr_buffer_load_lds gpu::load_lds
+#define __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4 gpu::third
 #define __builtin_amdgcn_readlane(v, from) ((int)gpu::exchange((uint32_t)(v), from))
 #define __builtin_amdgcn_readfirstlane(v) (v)
 #define __builtin_amdgcn_mfma_f32_32x32x16_bf16 gpu::third

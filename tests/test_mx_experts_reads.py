@@ -54,3 +54,9 @@ def test_inputs_gradient(checker, t, tile, rows, N, K, lddy):
 @pytest.mark.parametrize("N,K,M,blocks", [(40, 600, 5, 2), (40, 600, 5, 1), (17, 64, 16, 1), (65, 2500, 7, 3), (100, 5000, 3, 8), (16, 512, 1, 1), (1, 1, 1, 8), (130, 4096, 2, 4)])
 def test_few_rows(checker, N, K, M, blocks):
     check(checker, "few", N, K, M, blocks)
+
+
+@pytest.mark.parametrize("tile", (64, 128, 256))
+@pytest.mark.parametrize("N,K,first,second", [(40, 100, 3, 70), (300, 520, 257, 1), (1, 1, 1, 1), (130, 2100, 128, 300), (256, 512, 0, 256)])
+def test_product(checker, tile, N, K, first, second):
+    check(checker, "gemm", tile, N, K, first, second)
