@@ -2,7 +2,7 @@
 //   experts_reads_check dw TYPE TILE J K lddy before rows behind      two experts with rows, and rows that nobody has behind them
 //   experts_reads_check dx TYPE TILE rows N K lddy                     one expert
 //   experts_reads_check few N K M blocks                               a layer of few rows
-//   experts_reads_check gemm TILE N K rows rows                        two experts, and the last of the weights' rows
+//   experts_reads_check gemm TILE N K rows rows                        two experts, and the last of the weights' rows; plain, and with a bias, a residual and a kept form
 // Prints "ok <loads>" or what lies outside.  A load's offset has two parts.  Which of them meets the buffer's size is told in two ways: the vector part alone; or the
 // vector part against the size less the scalar part, in 32 bits without a sign.  A load that either of them lets through may reach memory.
 #define __shared__
@@ -141,10 +141,11 @@ static void few(int N, int K, int M, int blocks) {
         gpu::run_threads(WAVES * 64, dim3(block), [&] { experts_few_kernel<float, void, MT, WAVES, SINGLE>(reinterpret_cast<float*>(y.begin), p); });
 }
 
-template <int TILE>
-static void gemm(int N, int K, int first, int second) {
+template <class O, int TILE>
+static void gemm(int N, int K, int first, int second, bool epilogue) {
     const int64_t M = first + second;
-    Tensor a(M * code_pitch(K, 4)), as(M * scale_pitch(K)), w(2 * N * code_pitch(K, 4)), ws(2 * N * scale_pitch(K)), y(M * N * 4);
+    Tensor a(M * code_pitch(K, 4)), as(M * scale_pitch(K)), w(2 * N * code_pitch(K, 4)), ws(2 * N * scale_pitch(K)), y(M * N * sizeof(O));
+    Tensor bias(2 * N * 4), residual(M * N * sizeof(O)), kept(M * code_pitch(N, 8)), kept_scales(M * scale_pitch(N));
     tensors = {a, as, w, ws};
     std::vector<ExpertTile> table(1);
     const int32_t offsets[] = {0, first, first + second};
@@ -168,10 +169,16 @@ static void gemm(int N, int K, int first, int second) {
     p.table = table.data();
     p.offsets = offsets;
     p.experts = 2;
-    p.epilogue.function = SPARQ_MX_NONE;
+    p.epilogue = {nullptr, nullptr, nullptr, N, code_pitch(N, 8), scale_pitch(N), SPARQ_MX_NONE, (int)sparq::round_up(N, kCodeUnit)};
+    if (epilogue) {
+        p.bias = reinterpret_cast<const float*>(bias.begin);
+        p.epilogue.residual = residual.begin;
+        p.epilogue.kept_codes = kept.begin;
+        p.epilogue.kept_scales = kept_scales.begin;
+    }
     gridDim = dim3(2);                           // (workgroups that take one tile after the other)
     for (int block = 0; block < 2; ++block)
-        gpu::run_threads(kGemmThreads, dim3(block), [&] { gemm_kernel<float, TILE, TILE, ExpertGemmParamsOf<SPARQ_MX_NONE>>(reinterpret_cast<float*>(y.begin), p); });
+        gpu::run_threads(kGemmThreads, dim3(block), [&] { gemm_kernel<O, TILE, TILE, ExpertGemmParamsOf<SPARQ_MX_NONE>>(reinterpret_cast<O*>(y.begin), p); });
 }
 
 int main(int argc, char** argv) {
@@ -185,7 +192,10 @@ int main(int argc, char** argv) {
         const int groups = (n[3] + kScaleUnit - 1) / kScaleUnit;
         (groups <= 4 ? few<1, 4, true> : groups <= 8 ? few<1, 8, true> : few<1, 8, false>)(n[2], n[3], n[4], n[5]);
     } else if (argc == 7 && !strcmp(argv[1], "gemm")) {
-        (n[2] == 256 ? gemm<256> : n[2] == 128 ? gemm<128> : gemm<64>)(n[3], n[4], n[5], n[6]);
+        for (const bool epilogue : {false, true}) {
+            (n[2] == 256 ? gemm<float, 256> : n[2] == 128 ? gemm<float, 128> : gemm<float, 64>)(n[3], n[4], n[5], n[6], epilogue);
+            (n[2] == 256 ? gemm<__bf16, 256> : n[2] == 128 ? gemm<__bf16, 128> : gemm<__bf16, 64>)(n[3], n[4], n[5], n[6], epilogue);
+        }
     } else {
         return 2;
     }
