@@ -4,8 +4,8 @@
 // their results after the other, `blocks` times: its wavefronts divide the reduction in groups of 512 values (a row's 16 bytes of scales), and their sums are
 // joined in LDS in the wavefronts' order.  The next two blocks' weights are on their way meanwhile, and where each wavefront has one group, its part of A stays
 // in registers: read, or quantised, once for all blocks.
-// 16 rows, 11 of 16 experts with weights of 2048 x 4096: 13.9 us (47 MB, 7.1 at memory's pace, and what any launch takes), with a block a workgroup 16.7, with one on its way
-// and not two 14.1; two experts 5.0.
+// 16 rows, 11 of 16 experts with weights of 2048 x 4096: 12.2 us (47 MB, 7.1 at memory's pace, and what any launch takes); when it was chosen, side by side, 13.9, with a
+// block a workgroup 16.7, with one on its way and not two 14.1; two experts 5.0.
 #pragma once
 #include <type_traits>
 

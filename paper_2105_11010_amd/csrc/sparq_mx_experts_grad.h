@@ -1,5 +1,6 @@
 // The experts' gradients: the kernel of sparq_mx_grad_wide_kernel.h with rows of several experts; a translation unit for each type of dy and direction.
-// 16384 x 2048 x 2048 to 8 experts, bf16: dx 111-114 us of even ones, 132-138 of uneven ones, dw 137-141 and 141-144 (1.0-1.24 PF; the dense kernels 1.07-1.33).
+// 16384 x 2048 x 2048 to 8 experts, bf16, on the same tensors again and on four sets in turn: dx 112-116 and 118 us of even ones, 137 and 140 of uneven ones (two launches,
+// 114-128 and 28), dw 141-144 and 150, 143 and 154 (0.9-1.24 PF; the dense kernels 1.07-1.33).
 #pragma once
 #include "sparq_mx_grad.h"
 

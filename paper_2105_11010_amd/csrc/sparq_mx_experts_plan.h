@@ -32,13 +32,18 @@ inline ExpertsPlan experts_plan(int64_t M, int N, int K, int experts, bool offse
     p.parts = 1;
     // What an expert has of the rows on average; how they are divided is not known here.
     const int64_t each = (M + experts - 1) / experts;
-    // (us, a gemm, this kernel -> tiles: 8 experts of 2048 x 4096 with 8 rows each 10.4 -> 12.3, 16 13.0 -> 12.5, 32 17.8 -> 12.7; 64 of 1024 x 1024 11.0 -> 14.9,
-    // 13.2 -> 15.2, 18.8 -> 16.4; one expert: as the product without an epilogue, sparq_mx_gemm.hip)
+    // Few rows (us, a gemm on six sets of tensors in turn, as many rows for each expert / rows that go to any, few rows -> tiles.  16 rows a workgroup: 16 experts of
+    // 4096 x 2048 with 13 rows each 18.4 / 21.0 -> 20.5 / 20.8, with 16 18.7 / 21.6 -> 20.8 / 20.6; 8 of 2048 x 4096 with 13 12.7 / 12.8 -> 13.3 / 13.3, with 16 13.1 / 14.8 ->
+    // 13.4 / 13.4; 64 of 1024 x 1024 with 13 11.1 / 13.2 -> 11.3 / 11.3.  32 rows a workgroup: 32 rows each 23.5 / 26.8 -> 22.3 / 22.3, 15.9 / 19.1 -> 13.6 / 13.7, 15.9 / 19.2 ->
+    // 11.7 / 12.1; 64: 29.4 / 44.2 -> 24.2 / 24.2, 24.4 / 26.8 -> 14.2 / 14.5, 24.5 / 38.1 -> 13.8 / 14.4.  One expert: as the product without an epilogue, sparq_mx_gemm.hip.)
+    // A kept form goes in tiles at any number of rows: the 16 columns of a block are half of the 32 values that share a scale, and the other half is made elsewhere.  (What
+    // that costs: 16 of 4096 x 2048 with 4 rows each 20.9, without the kept form 16.4; a layer of 4096 x 4096 with 16 rows 8.5 and 4.9.)
     if (!kept && (offsets ? each <= 12 : each <= 16 || (each <= 64 && each * N * K <= 5ll << 27))) {
         p.fragments = (int)((each + 15) / 16);
         p.pieces = offsets ? most_tiles(M, experts, 16 * p.fragments) : 1;
         // Two workgroups of eight wavefronts a CU, or three of four, by the number of pieces to be expected of rows that go to any expert alike (us, by blocks a
-        // workgroup makes: 16 rows, 16 experts of 2048 x 4096: one 16.7, two 15.8, three 13.9, four 14.8, six 14.5; 64 rows, the same: 27, 21, 23, 17.8, 21).
+        // workgroup makes: 16 rows, 16 experts of 2048 x 4096: one 16.7, two 15.8, three 13.9, four 14.8, six 14.5; 64 rows, the same: 27, 21, 23, 17.8, 21.
+        // Rows that every expert has one of make more pieces than that: 16 rows, one of each, 20).
         const double part = offsets ? (double)M / (16 * p.fragments) - 0.5 * experts : 0.0;
         const double expected = offsets ? experts * (1.0 - pow(1.0 - 1.0 / experts, (double)M)) + (part > 0.0 ? part : 0.0) : 1.0;
         const double wanted = expected * ((N + kFewColumns - 1ll) / kFewColumns) / (K <= 4 * kScaleUnit ? 690 : 460);

@@ -11,7 +11,7 @@
 // Bound by the matrix instructions and, with data as large as this, by the card's power: 8192 x 4096 x 4096 takes 206-248 us for dx and 237-256
 // for dw (1.07-1.33 PF; the same instructions without loads and writes 1.57 PF).  fp16 dy, two instructions a product, 673-728 and 706-722 us, fp32, three,
 // 904-916 and 940.  Tiles of 128 and 64 ask for V at a step's end (a thread has one run of it) and need it where the next
-// begins (experts' a step later, which fp16 dx of 16384 x 2048 x 2048 took from 335 to 307-316): of 128 every step waits for all loads behind its barrier, which bf16 hides in part by a second workgroup on the CU and fp16 and fp32, whose LDS
+// begins (experts' a step later, which fp16 dx of 16384 x 2048 x 2048 took from 335 to 307-320): of 128 every step waits for all loads behind its barrier, which bf16 hides in part by a second workgroup on the CU and fp16 and fp32, whose LDS
 // leaves no room for one, do not; of 64 that wait is what a small layer's time is, 515 x 771 x 577 7.7 and 8.4 us of 12 or 13 steps.  dw in 256 x 256 keeps 105
 // scalar registers in lanes of vector ones, about 110 moves a step between its matrix instructions.
 #pragma once

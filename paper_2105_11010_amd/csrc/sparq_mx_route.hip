@@ -8,7 +8,8 @@ constexpr int kThreads = 256;
 constexpr int kWaves = kThreads / 64;
 
 // 16-bit results of what adds up and its gradient go past the caches: the rows these read have the caches to themselves, and what is written is not written back
-// while the next kernel runs (8192 tokens of 4096, two rows each, one after the other: 42 and 60 us -> 36 and 54).
+// while the next kernel runs (8192 tokens of 4096, two rows each, left -> past, when it was chosen: 42 and 60 us -> 36 and 54).
+// Times below: a call on the same tensors again, part of which the last-level cache still holds, and on four sets of them in turn, from memory.
 template <class T> inline constexpr bool kPast = sizeof(T) == 2;
 
 struct RouteParams {
@@ -24,8 +25,8 @@ struct RouteParams {
 };
 
 // A token's row is read once and stored at each of its places, a wavefront 512 values of it: what is read and written is what the formula names, in
-// whole lines, whatever the order of the places.  Bound by memory: 8192 tokens of 4096, two places each, bf16 30.6 us (6.6 TB/s), to both coded forms of 2048 19;
-// fp32 4096 of 2048, four places, 28.6 (5.9).  (1024 values a wavefront: no change.)
+// whole lines, whatever the order of the places.  Bound by memory: 8192 tokens of 4096, two places each, bf16 31 us and 40 (6.5 and 5.0 TB/s), to both coded forms of 2048
+// 15 and 18.5; fp32 4096 of 2048, four places, 29 and 40.  (1024 values a wavefront: no change.)
 template <class T, bool Y, bool F4, bool I8, int STREAMING>
 __global__ __launch_bounds__(kThreads) void gather_kernel(const T* __restrict__ x, T* __restrict__ y, uint8_t* __restrict__ codes4, uint8_t* __restrict__ scales4,
                                                           uint8_t* __restrict__ codes8, uint8_t* __restrict__ scales8, const RouteParams p) {
@@ -71,8 +72,8 @@ __global__ __launch_bounds__(kThreads) void gather_kernel(const T* __restrict__ 
 }
 
 // A wavefront makes 512 values of a token's row, or 1024, and the rows of four slots are on their way at a time.  (A slot without a row reads row 0 and leaves it
-// out: a branch would have one row wait for another.)  Bound by memory: 8192 tokens of 4096, two rows each, bf16 30.4 us (6.6 TB/s), with a residual 39-41; fp32 4096
-// of 2048, four rows, 25.1 (6.7).
+// out: a branch would have one row wait for another.)  Bound by memory: 8192 tokens of 4096, two rows each, bf16 30 us and 37.5 (6.7 and 5.4 TB/s), with a residual 39.5
+// and 49; fp32 4096 of 2048, four rows, 25 and 36.
 template <class T, int CHUNKS, bool NT>
 __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__ x, const T* __restrict__ residual, T* __restrict__ y, const RouteParams p) {
     const int lane = threadIdx.x & 63;
@@ -125,8 +126,8 @@ __global__ __launch_bounds__(kThreads) void combine_kernel(const T* __restrict__
 }
 
 // W wavefronts take a token, every W-th 512 values of its row each and four slots at a time; dweights are sums within a lane, within a wavefront and over the
-// wavefronts in their order.  Bound by memory: 8192 tokens of 4096, two rows each, bf16 50.5 us (6.65 TB/s); fp32 4096 of 2048, four rows, 58 (5.2): a lane's 32 bytes
-// leave as two stores, each half of every line.
+// wavefronts in their order.  Bound by memory: 8192 tokens of 4096, two rows each, bf16 50.5 us and 68 (6.65 and 4.9 TB/s); fp32 4096 of 2048, four rows, 61 and 69: a
+// lane's 32 bytes leave as two stores, each half of every line.
 template <class T, bool DX, bool DW, int W, bool NT>
 __global__ __launch_bounds__(kThreads) void combine_grad_kernel(const T* __restrict__ dy, const T* __restrict__ x, T* __restrict__ dx, const RouteParams p) {
     __shared__ float sums[kWaves][4];
