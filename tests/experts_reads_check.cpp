@@ -1,7 +1,7 @@
 // Where the experts' kernels read by buffer, on the host: every load that may reach memory lies inside its tensor.
 //   experts_reads_check dw TYPE TILE J K lddy before rows behind      two experts with rows, and rows that nobody has behind them
 //   experts_reads_check dx TYPE TILE rows N K lddy                     one expert
-//   experts_reads_check few N K M blocks                               a layer of few rows
+//   experts_reads_check few N K M blocks                               a layer of few rows, from codes and, of up to 4096 values, quantised on the way
 //   experts_reads_check gemm TILE N K rows rows                        two experts, and the last of the weights' rows; plain, and with a bias, a residual and a kept form
 // Prints "ok <loads>" or what lies outside.  A load's offset has two parts.  Which of them meets the buffer's size is told in two ways: the vector part alone; or the
 // vector part against the size less the scalar part, in 32 bits without a sign.  A load that either of them lets through may reach memory.
@@ -116,11 +116,15 @@ static void with_kernel(const char* type, int tile, F&& f) {
     else tile == 128 ? f(__bf16{}, Middle{}) : f(__bf16{}, Small{});
 }
 
-template <int MT, int WAVES, bool SINGLE>
+template <class X, int WAVES, bool SINGLE>
 static void few(int N, int K, int M, int blocks) {
-    Tensor a(M * code_pitch(K, 4)), as(M * scale_pitch(K)), w(N * code_pitch(K, 4)), ws(N * scale_pitch(K)), y((int64_t)M * N * 4);
+    typedef std::conditional_t<std::is_void_v<X>, float, X> Value;
+    const int64_t ldx = K + 3;
+    Tensor x(((M - 1) * ldx + K) * sizeof(Value)), a(M * code_pitch(K, 4)), as(M * scale_pitch(K)), w(N * code_pitch(K, 4)), ws(N * scale_pitch(K)), y((int64_t)M * N * 4);
     tensors = {w, ws};
     ExpertFewParams p = {};
+    p.x = x.begin;
+    p.ldx = ldx;
     p.a = a.begin;
     p.as = as.begin;
     p.w = w.begin;
@@ -138,7 +142,7 @@ static void few(int N, int K, int M, int blocks) {
     p.epilogue.function = SPARQ_MX_NONE;
     const int all = (N + kFewColumns - 1) / kFewColumns;
     for (int block = 0; block < (all + blocks - 1) / blocks; ++block)
-        gpu::run_threads(WAVES * 64, dim3(block), [&] { experts_few_kernel<float, void, MT, WAVES, SINGLE>(reinterpret_cast<float*>(y.begin), p); });
+        gpu::run_threads(WAVES * 64, dim3(block), [&] { experts_few_kernel<float, X, 1, WAVES, SINGLE>(reinterpret_cast<float*>(y.begin), p); });
 }
 
 template <class O, int TILE>
@@ -190,7 +194,11 @@ int main(int argc, char** argv) {
         with_kernel(argv[2], n[3], [&](auto t, auto tile) { dx<decltype(t), decltype(tile)::value>(n[4], n[5], n[6], n[7]); });
     } else if (argc == 6 && !strcmp(argv[1], "few")) {
         const int groups = (n[3] + kScaleUnit - 1) / kScaleUnit;
-        (groups <= 4 ? few<1, 4, true> : groups <= 8 ? few<1, 8, true> : few<1, 8, false>)(n[2], n[3], n[4], n[5]);
+        (groups <= 4 ? few<void, 4, true> : groups <= 8 ? few<void, 8, true> : few<void, 8, false>)(n[2], n[3], n[4], n[5]);
+        if (groups <= 8) {
+            (groups <= 4 ? few<float, 4, true> : few<float, 8, true>)(n[2], n[3], n[4], n[5]);
+            (groups <= 4 ? few<__bf16, 4, true> : few<__bf16, 8, true>)(n[2], n[3], n[4], n[5]);
+        }
     } else if (argc == 7 && !strcmp(argv[1], "gemm")) {
         for (const bool epilogue : {false, true}) {
             (n[2] == 256 ? gemm<float, 256> : n[2] == 128 ? gemm<float, 128> : gemm<float, 64>)(n[3], n[4], n[5], n[6], epilogue);
